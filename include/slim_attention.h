@@ -294,6 +294,62 @@ int vanilla_attention_block(const void* x, const void* W_Q, const void* W_K, con
                             const void* W_O, void* Kcache, void* Vcache, void* y, int B, int H,
                             int T, int d, const slim_opts* opts);
 
+/* ---- a tree of drafted tokens (speculative decoding) --------------------------------------- */
+
+/* One step that checks several drafted tokens at once is three calls: slim_tree_decode (the attention of all of them, layer by layer),
+ * slim_tree_verify (which of them the target accepts, and the token after) and slim_tree_commit (the accepted ones' keys to their
+ * places, layer by layer).
+ *
+ * The tree of a sequence: N slots (1 <= N <= 64, the same for the batch), parents[b][i] the slot that node i hangs on.
+ *   -1 <= parents[b][i] < i : a root (-1), or the child of an earlier node; several roots are several trees
+ *   any other value         : the slot is unused, and so are those that hang on it (batches of trees of different sizes)
+ * A node sees the whole context, its ancestors and itself.  Slot i's key is row len_b + i of the cache, len_b = seq_lens[b] the rows
+ * of context: 0 <= len_b <= T <= t_stride - N.  (Unlike in slim_decode, a context may be empty.)  opts->t_stride: 0 => T + N.
+ * With opts->rope_table ([T + N][d_k/2][2] here: slim_rope_table(T + N)) node i sits at position len_b + its depth (a root's is 0);
+ * the keys are stored raw and rotated for the scores, q is taken as given, as in slim_decode.
+ * Both layouts of opts->k_layout (t_stride % 32 == 0 for the banded one), any H and d_k of whole 16-byte vectors.
+ * opts->variant and opts->wait_budget_us mean nothing to these calls: none of their kernels waits for another workgroup.
+ * They allocate nothing when given a workspace, and may be captured. */
+
+/* eq. 7 option 2 for the N nodes of each of B trees:
+ *   q       : device dtype [B][N][d]   projected, un-scaled queries of the nodes
+ *   Kcache  : device dtype [B][t_stride][d]; rows [0, len_b + N) of sequence b are read (rows of unused slots too, without any effect)
+ *   W_KV    : device dtype [d][d]
+ *   parents : device int32 [B][N]
+ *   out     : device dtype [B][N][d]   concat of heads, written; zeros for unused slots
+ * q and out have the cache's type (slim_decode's are fp32): N rows a sequence are inputs and outputs of matrix products.  Scores,
+ * softmax sums and weighted sums are fp32; the softmax numerators are rounded to dtype where they enter the weighted sum.
+ * A drafted key that is not finite makes NaN of the nodes that see it and changes nothing for the others.
+ * opts->stage_ms: scores, weighted sum, projection.  Scratch: slim_workspace_bytes_tree (0 on invalid arguments), else library-owned. */
+size_t slim_workspace_bytes_tree(int B, int N, int H, int T, int d, int dtype);
+int slim_tree_decode(const void* q, const void* Kcache, const void* W_KV, const int32_t* parents, void* out,
+                     int B, int N, int H, int T, int d, const slim_opts* opts);
+
+/* Which drafted tokens the target accepts (rejection sampling with given random numbers: the accepted tokens and the one after are
+ * distributed as the target's own), and the next token.  Slot 0 is the last token that stands already; the walk starts there.
+ *   tokens  : device int32 [B][N]      token of every node; one outside [0, V) is passed over
+ *   parents : device int32 [B][N]      as above (parents[b][0] is not looked at); the children of a node are tested in slot order
+ *   p       : device dtype [B][N][V]   the target's probabilities after each node
+ *   draft   : device dtype [B][N][V]   the distribution that the children of a node were drawn from, independently; nullable: they were
+ *                                      chosen, not drawn
+ *   u       : device fp32 [B][N]       uniform in [0, 1): u[b][i] decides on node i, u[b][0] draws the next token
+ *   path    : device int32 [B][N]      written: 0, the accepted nodes down the tree, then -1
+ *   n_path  : device int32 [B]         written: how many these are (1 <= n_path <= N)
+ *   next_token : device int32 [B]      written: drawn from what is left of p after the last node of the path
+ * With a draft: at a node with F = 1, a = 0, child x is accepted iff u F q(x) < p(x) - a q(x); if not, a += F and
+ * F = sum_v max(p(v) - a q(v), 0), the unnormalised residual.  Without: iff u R < p(x), R = 1; if not, R -= p(x) and x is excluded.
+ * The next token is the lowest v whose running sum of the residual is over u[b][0] times the whole sum (where rounding leaves none, the last
+ * v with any weight; where nothing has any, the likeliest of p, lowest first).  Sums and products are in 64 bits.
+ * opts: dtype, stream, stage_ms (one figure); cache options are SLIM_ERR_ARG.  No scratch. */
+int slim_tree_verify(const int32_t* tokens, const int32_t* parents, const void* p, const void* draft, const float* u,
+                     int32_t* path, int32_t* n_path, int32_t* next_token, int B, int N, int V, const slim_opts* opts);
+
+/* Row len_b + path[b][j] of the cache to row len_b + j, j < n_path[b], and new_lens[b] = len_b + n_path[b] (which may be
+ * opts->seq_lens itself; then it is the next step's).  path is strictly increasing, as slim_tree_verify writes it; entries that are
+ * no slot, or not past their place, move nothing.  path and n_path: device int32 [B][N], [B]. */
+int slim_tree_commit(void* Kcache, const int32_t* path, const int32_t* n_path, int32_t* new_lens, int B, int N, int H, int T, int d,
+                     const slim_opts* opts);
+
 #ifdef __cplusplus
 }
 #endif

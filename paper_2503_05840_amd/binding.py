@@ -25,7 +25,8 @@ DTYPES = {"f32": SLIM_F32, "bf16": SLIM_BF16}
 EXPORTS = ("slim_strerror", "slim_prepare_wkv", "slim_prepare_wkv_nonsquare", "slim_pack_weights", "slim_rope_table", "slim_workspace_bytes",
            "slim_workspace_bytes_xcache", "slim_workspace_bytes_block", "slim_attention_block", "vanilla_attention_block",
            "slim_variant_for", "slim_decode", "vanilla_kv_decode", "slim_decode_xcache", "slim_init", "slim_status",
-           "slim_read_probe", "slim_decode_static", "slim_static_scratch_bytes", "slim_band_kcache")
+           "slim_read_probe", "slim_decode_static", "slim_static_scratch_bytes", "slim_band_kcache",
+           "slim_workspace_bytes_tree", "slim_tree_decode", "slim_tree_verify", "slim_tree_commit")
 VARIANT_NAMES = {1: "generic", 2: "fused_split", 3: "fused"}
 
 
@@ -109,6 +110,14 @@ def load():
     lib.slim_static_scratch_bytes.argtypes = []
     lib.slim_band_kcache.restype = ci
     lib.slim_band_kcache.argtypes = [vp, vp, ci, ctypes.c_int64, ci, ci, ci]
+    lib.slim_workspace_bytes_tree.restype = ctypes.c_size_t
+    lib.slim_workspace_bytes_tree.argtypes = [ci, ci, ci, ci, ci, ci]
+    lib.slim_tree_decode.restype = ci
+    lib.slim_tree_decode.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, op]
+    lib.slim_tree_verify.restype = ci
+    lib.slim_tree_verify.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, op]
+    lib.slim_tree_commit.restype = ci
+    lib.slim_tree_commit.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, op]
     lib.slim_read_probe.restype = ci
     lib.slim_read_probe.argtypes = [vp, ctypes.c_size_t, vp]
     _lib = lib
@@ -192,6 +201,10 @@ def slim_workspace_bytes_xcache(B, H, T, d_model, d_k, dtype: str) -> int:
 
 def slim_workspace_bytes_block(B, H, T, d, dtype: str) -> int:
     return int(load().slim_workspace_bytes_block(B, H, T, d, DTYPES[dtype]))
+
+
+def slim_workspace_bytes_tree(B, N, H, T, d, dtype: str) -> int:
+    return int(load().slim_workspace_bytes_tree(B, N, H, T, d, DTYPES[dtype]))
 
 
 def auto_variant_name(B, H, T, d, dtype: str) -> str:
@@ -359,3 +372,73 @@ def vanilla_attention_block(x, W_Q, W_K, W_V, W_O, Kcache, Vcache, y, B, H, T, d
     if rc != SLIM_OK:
         raise SlimError(rc, "vanilla_attention_block")
     return y
+
+
+# ---- a tree of drafted tokens ----------------------------------------------------------------
+def _tree_ptr(t, shape, dtype):
+    """The address of a contiguous device tensor of exactly this shape and type (N rows a sequence are easily confused)."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"expected {tuple(shape)} {dtype}, got {tuple(t.shape)} {t.dtype}")
+    return _dev_ptr(t)
+
+
+def _element(dtype):
+    import torch
+    return torch.bfloat16 if dtype == "bf16" else torch.float32
+
+
+def _lens_ok(t, B, name):
+    import torch
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_cuda or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 device tensor of {B}")
+
+
+def _rows_of_tree(Kcache, B, N, T, d, t_stride, dtype):
+    rows = int(t_stride or 0) or T + N
+    return _tree_ptr(Kcache, (B, rows, d), _element(dtype))
+
+
+def slim_tree_decode(q, Kcache, W_KV, parents, out, B, N, H, T, d, dtype="bf16", seq_lens=None, seq_lens_host=None, t_stride=0,
+                     workspace=None, stage_ms=None, rope_table=None, k_layout=K_ROWMAJOR):
+    """Attention of B trees of N drafted tokens over their K-caches: q, out (B, N, d), Kcache (B, t_stride or T + N, d), parents (B, N) int32."""
+    import torch
+    el = _element(dtype)
+    _lens_ok(seq_lens, B, "seq_lens")
+    if rope_table is not None and (rope_table.dtype != torch.float32 or rope_table.numel() < (T + N) * (d // H)):
+        raise ValueError("rope_table must be float32 and hold T + N positions")
+    ptrs = (_tree_ptr(q, (B, N, d), el), _rows_of_tree(Kcache, B, N, T, d, t_stride, dtype), _tree_ptr(W_KV, (d, d), el),
+            _tree_ptr(parents, (B, N), torch.int32), _tree_ptr(out, (B, N, d), el))
+    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, workspace, VARIANT_AUTO, stage_ms, rope_table, 0, k_layout)
+    rc = load().slim_tree_decode(*ptrs, B, N, H, T, d, ctypes.byref(o))
+    if rc != SLIM_OK:
+        raise SlimError(rc, "slim_tree_decode")
+    return out
+
+
+def slim_tree_verify(tokens, parents, p, draft, u, path, n_path, next_token, B, N, V, dtype="f32", stage_ms=None):
+    """Which drafted tokens the target accepts: tokens, parents, path (B, N) int32, p and draft (B, N, V) or draft None, u (B, N) float32."""
+    import torch
+    el, i32 = _element(dtype), torch.int32
+    ptrs = (_tree_ptr(tokens, (B, N), i32), _tree_ptr(parents, (B, N), i32), _tree_ptr(p, (B, N, V), el),
+            None if draft is None else _tree_ptr(draft, (B, N, V), el), _tree_ptr(u, (B, N), torch.float32),
+            _tree_ptr(path, (B, N), i32), _tree_ptr(n_path, (B,), i32), _tree_ptr(next_token, (B,), i32))
+    o, keep = _opts(dtype, None, None, 0, None, VARIANT_AUTO, stage_ms)
+    rc = load().slim_tree_verify(*ptrs, B, N, V, ctypes.byref(o))
+    if rc != SLIM_OK:
+        raise SlimError(rc, "slim_tree_verify")
+    return path, n_path, next_token
+
+
+def slim_tree_commit(Kcache, path, n_path, new_lens, B, N, H, T, d, dtype="bf16", seq_lens=None, seq_lens_host=None, t_stride=0,
+                     stage_ms=None, k_layout=K_ROWMAJOR):
+    """The accepted path's keys to their places in the cache; new_lens (B,) int32 may be seq_lens itself."""
+    import torch
+    i32 = torch.int32
+    _lens_ok(seq_lens, B, "seq_lens")
+    ptrs = (_rows_of_tree(Kcache, B, N, T, d, t_stride, dtype), _tree_ptr(path, (B, N), i32), _tree_ptr(n_path, (B,), i32),
+            _tree_ptr(new_lens, (B,), i32))
+    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, None, VARIANT_AUTO, stage_ms, None, 0, k_layout)
+    rc = load().slim_tree_commit(*ptrs, B, N, H, T, d, ctypes.byref(o))
+    if rc != SLIM_OK:
+        raise SlimError(rc, "slim_tree_commit")
+    return new_lens

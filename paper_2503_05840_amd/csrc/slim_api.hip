@@ -808,3 +808,137 @@ extern "C" int vanilla_attention_block(const void* x, const void* W_Q, const voi
   BlockCall c{x, W_Q, W_K, W_V, nullptr, W_O, Kcache, Vcache, y};
   return attention_block(false, c, B, H, T, d, o);
 }
+
+// ---- a tree of drafted tokens ---------------------------------------------------------------------
+namespace {
+
+// Bounds that keep grids and 32-bit offsets inside their ranges
+constexpr int TREE_MAX_BATCH = 32768, TREE_MAX_ROWS = 1 << 20, TREE_MAX_WIDTH = 1 << 20, TREE_MAX_CONTEXT = 1 << 23, TREE_MAX_VOCABULARY = 1 << 24;
+
+struct TreePlan { size_t off_P, off_ref, off_lsum, off_C, off_sref, off_sl, off_part, total; };
+
+// Every term grows with T (tree_splits does).
+TreePlan tree_layout(TreeArgs& a, int dtype) {
+  const int vec = vec_elems(dtype), ch = 4 * vec, cw = 16 * vec;
+  a.MT = (a.H * a.N + 15) / 16;
+  a.NB = (a.T + a.N + TREE_BLOCK_ROWS - 1) / TREE_BLOCK_ROWS;
+  a.CT = a.NB * (TREE_BLOCK_ROWS / ch);
+  a.DB = (a.d + cw - 1) / cw;
+  a.S = tree_splits(dtype, a.B, a.N, a.H, a.T, a.d);
+  a.csw = tree_row_splits(dtype, a.B, a.N, a.H, a.d);
+  TreePlan p;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o += up(bytes); return at; };
+  const size_t rows = (size_t)a.B * a.MT * 16;
+  p.off_P = take((size_t)a.B * a.MT * a.CT * 1024);
+  p.off_ref = take(sizeof(float) * rows * a.NB);
+  p.off_lsum = take(sizeof(float) * rows * a.NB);
+  p.off_C = take(sizeof(float) * rows * a.S * a.DB * cw);
+  p.off_sref = take(sizeof(float) * rows * a.S);
+  p.off_sl = take(sizeof(float) * rows * a.S);
+  p.off_part = take(a.csw > 1 ? sizeof(float) * a.csw * (size_t)a.B * a.N * a.d : 0);
+  p.total = o;
+  return p;
+}
+
+// What slim_tree_decode and slim_tree_commit check alike: sizes, the cache's rows (context and drafted tokens) and layout.
+int check_tree(int B, int N, int H, int T, int d, const slim_opts* o, int* dtype, long* t_stride) {
+  if (B < 1 || B > TREE_MAX_BATCH || N < 1 || N > TREE_MAX_NODES || H < 1 || T < 0 || d < 1 || d % H != 0) return SLIM_ERR_SHAPE;
+  *dtype = o ? o->dtype : SLIM_F32;
+  if (*dtype != SLIM_F32 && *dtype != SLIM_BF16) return SLIM_ERR_DTYPE;
+  if (d / H % vec_elems(*dtype) != 0 || (long)H * N > TREE_MAX_ROWS || d > TREE_MAX_WIDTH || T > TREE_MAX_CONTEXT) return SLIM_ERR_SHAPE;
+  *t_stride = (o && o->t_stride) ? (long)o->t_stride : (long)T + N;
+  if (*t_stride < (long)T + N) return SLIM_ERR_SHAPE;
+  const int k_layout = o ? o->k_layout : SLIM_K_ROWMAJOR;
+  if (k_layout != SLIM_K_ROWMAJOR && k_layout != SLIM_K_BANDED) return SLIM_ERR_ARG;
+  if (k_layout == SLIM_K_BANDED && *t_stride % 32 != 0) return SLIM_ERR_LAYOUT;
+  if (o && o->seq_lens && (((uintptr_t)o->seq_lens) & 3)) return SLIM_ERR_ALIGN;
+  if (o && o->seq_lens_host)
+    for (int b = 0; b < B; ++b)
+      if (o->seq_lens_host[b] < 0 || o->seq_lens_host[b] > T) return SLIM_ERR_SEQLEN;
+  return SLIM_OK;
+}
+
+bool misaligned4(const void* p) { return (((uintptr_t)p) & 3) != 0; }
+
+}  // namespace
+
+extern "C" size_t slim_workspace_bytes_tree(int B, int N, int H, int T, int d, int dtype) {
+  slim_opts o{};
+  o.dtype = dtype;
+  long ts;
+  if (check_tree(B, N, H, T, d, &o, &dtype, &ts)) return 0;
+  TreeArgs a{};
+  a.B = B; a.N = N; a.H = H; a.T = T; a.d = d; a.d_k = d / H;
+  return tree_layout(a, dtype).total;
+}
+
+extern "C" int slim_tree_decode(const void* q, const void* Kcache, const void* W_KV, const int32_t* parents, void* out, int B, int N,
+                                int H, int T, int d, const slim_opts* o) {
+  if (!q || !Kcache || !W_KV || !parents || !out) return SLIM_ERR_ARG;
+  int dtype; long t_stride;
+  if (int rc = check_tree(B, N, H, T, d, o, &dtype, &t_stride)) return rc;
+  if (misaligned(q) || misaligned(Kcache) || misaligned(W_KV) || misaligned(out) || misaligned4(parents)) return SLIM_ERR_ALIGN;
+  const float* rope = o ? o->rope_table : nullptr;
+  if (rope && (d / H & 1)) return SLIM_ERR_SHAPE;
+  if (rope && misaligned(rope)) return SLIM_ERR_ALIGN;
+  TreeArgs a{};
+  a.B = B; a.N = N; a.H = H; a.T = T; a.d = d; a.d_k = d / H;
+  const TreePlan p = tree_layout(a, dtype);
+  char* ws;
+  if (int rc = get_workspace(o, p.total, &ws)) return rc;
+  hipStream_t st = o ? (hipStream_t)o->stream : nullptr;
+  a.q = q; a.K = Kcache; a.W = W_KV; a.parents = parents; a.out = out;
+  a.seq_lens = o ? o->seq_lens : nullptr;
+  a.rope = rope; a.k_bstride = t_stride * d;
+  a.banded = o && o->k_layout == SLIM_K_BANDED;
+  a.qscale = 1.4426950408889634f / sqrtf((float)a.d_k);
+  a.P = ws + p.off_P;
+  a.ref = (float*)(ws + p.off_ref); a.lsum = (float*)(ws + p.off_lsum);
+  a.C = (float*)(ws + p.off_C); a.sref = (float*)(ws + p.off_sref); a.sl = (float*)(ws + p.off_sl);
+  a.part = (float*)(ws + p.off_part);
+  StageTimer tm(o, st);
+  launch_tree_scores(dtype, a, st);
+  tm.mark();
+  launch_tree_weighted(dtype, a, st);
+  tm.mark();
+  launch_tree_project(dtype, a, st);
+  tm.mark();
+  tm.finish();
+  return launch_status();
+}
+
+extern "C" int slim_tree_verify(const int32_t* tokens, const int32_t* parents, const void* p, const void* draft, const float* u,
+                                int32_t* path, int32_t* n_path, int32_t* next_token, int B, int N, int V, const slim_opts* o) {
+  if (!tokens || !parents || !p || !u || !path || !n_path || !next_token) return SLIM_ERR_ARG;
+  if (o && (o->seq_lens || o->rope_table || o->k_layout || o->t_stride)) return SLIM_ERR_ARG;     // (there is no cache in this call)
+  if (B < 1 || B > TREE_MAX_BATCH || N < 1 || N > TREE_MAX_NODES || V < 1 || V > TREE_MAX_VOCABULARY) return SLIM_ERR_SHAPE;
+  const int dtype = o ? o->dtype : SLIM_F32;
+  if (dtype != SLIM_F32 && dtype != SLIM_BF16) return SLIM_ERR_DTYPE;
+  if (misaligned(p) || misaligned(draft) || misaligned4(tokens) || misaligned4(parents) || misaligned4(u) || misaligned4(path) ||
+      misaligned4(n_path) || misaligned4(next_token))
+    return SLIM_ERR_ALIGN;
+  hipStream_t st = o ? (hipStream_t)o->stream : nullptr;
+  VerifyArgs a{tokens, parents, p, draft, u, path, n_path, next_token, B, N, V};
+  StageTimer tm(o, st);
+  launch_tree_verify(dtype, a, st);
+  tm.mark();
+  tm.finish();
+  return launch_status();
+}
+
+extern "C" int slim_tree_commit(void* Kcache, const int32_t* path, const int32_t* n_path, int32_t* new_lens, int B, int N, int H, int T, int d,
+                                const slim_opts* o) {
+  if (!Kcache || !path || !n_path || !new_lens) return SLIM_ERR_ARG;
+  if (o && o->rope_table) return SLIM_ERR_ARG;        // keys are stored raw: moving one needs no rotation
+  int dtype; long t_stride;
+  if (int rc = check_tree(B, N, H, T, d, o, &dtype, &t_stride)) return rc;
+  if (misaligned(Kcache) || misaligned4(path) || misaligned4(n_path) || misaligned4(new_lens)) return SLIM_ERR_ALIGN;
+  hipStream_t st = o ? (hipStream_t)o->stream : nullptr;
+  StageTimer tm(o, st);
+  launch_tree_commit(dtype, Kcache, t_stride * d, path, n_path, o ? o->seq_lens : nullptr, new_lens, B, N, T, d, d / H,
+                     o && o->k_layout == SLIM_K_BANDED, st);
+  tm.mark();
+  tm.finish();
+  return launch_status();
+}

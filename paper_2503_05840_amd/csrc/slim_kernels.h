@@ -238,4 +238,43 @@ void launch_kweighted(const float* P, const float* blocks, const void* K, long k
 void launch_xweighted_full(const float* S, const void* K, long k_bstride, const int32_t* seq_lens, int T, int H, int d, int nsplit,
                            float* Cpart, float* mpart, float* lpart, int B, hipStream_t st);
 
+// ---- a tree of drafted tokens (kernels_tree.hip, kernels_verify.hip) -----------------------------------
+constexpr int TREE_MAX_NODES = 64;           // a node is a lane of a wave, a set of nodes 64 bits
+constexpr int TREE_BLOCK_ROWS = 256;         // cache rows that share a reference of the softmax numerators
+constexpr int TREE_MAX_SPLITS = 64;
+
+struct TreeArgs {
+  const void *q, *K, *W;                     // [B][N][d], the cache, [d][d]
+  const int32_t *seq_lens, *parents;         // rows of context (nullable: T each), [B][N]
+  const float* rope;                         // [T + N][d_k / 2][2], nullable
+  void* out;                                 // [B][N][d]
+  long k_bstride;                            // elements between the sequences' caches
+  int B, N, H, d, d_k, T, banded;
+  float qscale;                              // log2(e) / sqrt(d_k)
+  // work in between.  Query row m = h N + i; a tile is 16 of them, a fragment 64 x 16 bytes: a matrix operand
+  int MT, CT, NB, DB, S, csw;                // query tiles, fragments of a tile, row blocks, column blocks, context splits, row splits of W
+  void* P;                                   // [B][MT][CT] fragments: numerators
+  float *ref, *lsum;                         // [B][NB][MT * 16]: reference and sum of a block's numerators
+  float* C;                                  // [B][S][MT][DB] blocks of 16 rows x 16 VEC columns: weighted sums
+  float *sref, *sl;                          // [B][S][MT * 16]
+  float* part;                               // [csw][B][N][d], csw > 1
+};
+int tree_splits(int dtype, int B, int N, int H, int T, int d);
+int tree_row_splits(int dtype, int B, int N, int H, int d);
+void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st);
+void launch_tree_weighted(int dtype, const TreeArgs& a, hipStream_t st);
+void launch_tree_project(int dtype, const TreeArgs& a, hipStream_t st);
+
+struct VerifyArgs {
+  const int32_t *tokens, *parents;           // [B][N]
+  const void *p, *draft;                     // [B][N][V], draft nullable
+  const float* u;                            // [B][N]
+  int32_t *path, *n_path, *next;             // [B][N], [B], [B]
+  int B, N, V;
+};
+void launch_tree_verify(int dtype, const VerifyArgs& a, hipStream_t st);
+// rows of 16-byte pieces: len_b + path[j] -> len_b + j
+void launch_tree_commit(int dtype, void* K, long k_bstride, const int32_t* path, const int32_t* n_path, const int32_t* seq_lens, int32_t* new_lens,
+                        int B, int N, int T, int d, int d_k, int banded, hipStream_t st);
+
 }  // namespace slim
