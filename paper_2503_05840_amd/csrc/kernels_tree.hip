@@ -37,6 +37,27 @@ __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, f32x4 acc) 
   }
 }
 
+// Which drafted keys of sequence b hold anything that is not finite (bit j: node j), the same in every lane
+__device__ __forceinline__ uint64_t odd_keys(const TreeArgs& a, int b, int lane) {
+  uint64_t m = 0;
+  for (int i = lane; i < 2 * a.H; i += 64) m |= a.odd[(size_t)b * 2 * a.H + i];
+  if (!__any(m != 0)) return 0;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) m |= (uint64_t)__shfl_xor((unsigned)m, k) | (uint64_t)__shfl_xor((unsigned)(m >> 32), k) << 32;
+  return m;
+}
+
+// acc += a b, the accumulator staying where it is.  With as many accumulators as there are accumulation registers the compiler gives a product
+// another destination than its addend and moves hundreds of registers a step to put that right.  In an asm statement the wait states
+// are this code's: two between a vector instruction that writes an operand and the product (the s_nop), those of reading a result
+// in settle().
+template <int DT>
+__device__ __forceinline__ void mma_in_place(const u32x4& a, const u32x4& b, f32x4& acc) {
+  if constexpr (DT == DT_BF16) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+  else acc = mma<DT>(a, b, acc);
+}
+__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+
 // VEC rows x VEC columns per lane -> VEC operands (one per column), each VEC rows of that column
 template <int DT, int VEC = Elem<DT>::VEC>
 __device__ __forceinline__ void transpose(const u32x4 (&k)[VEC], u32x4 (&a)[VEC]) {
@@ -115,175 +136,6 @@ __device__ __forceinline__ void rotate_piece(u32x4 x, const f32x4* cs, u32x4& hi
   }
 }
 
-// ------------------------------------------------------------------------------------------------
-// Scores and numerators.  A workgroup of four waves takes 64 query rows (row m = h N + i: the nodes of head h one after the other, so
-// that small trees of many heads fill the tiles) and 256 rows of the cache, a wave 64 of these:
-// S^T = K_h q_h^T for every head of the query rows, with the query operand zero where a row is another head's.  As references the
-// numerators 2^(s - ref) take the block's maximum rounded up to a multiple of 32: a bf16 or fp32 numerator is as exact at 2^-32 as at 1,
-// and blocks whose maxima differ by less than that have the same reference, so that the weighted sum hardly ever rescales.  They
-// leave as operands of that sum (lane l of a 1 KB fragment: query row l % 16, cache rows slot_row(l / 16, j)).
-// ------------------------------------------------------------------------------------------------
-template <int DT, bool ROPE>
-__global__ __launch_bounds__(256) void tree_scores_kernel(TreeArgs a) {
-  constexpr int VEC = Elem<DT>::VEC, KW = 4 * VEC;
-  typedef typename Elem<DT>::T T;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
-  const int group = blockIdx.x, blk = blockIdx.y, b = blockIdx.z;
-  const int rows = a.N * a.H;
-  const int len = seq_len_of(a.seq_lens, b, a.T), L = len + a.N;
-  if (blk * TREE_BLOCK >= L) return;
-  __shared__ float red[2][4][64];
-  const T* K = (const T*)a.K + (size_t)b * a.k_bstride;
-  const int rp = a.banded ? a.d_k : a.d;
-  const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
-  const int depth = __popcll(anc) - 1;
-
-  const int t0 = blk * TREE_BLOCK + wave * 64;
-  int trow[4], pos[4];
-#pragma unroll
-  for (int ts = 0; ts < 4; ++ts) {
-    const int t = min(t0 + 16 * ts + n16, L - 1);          // (rows past the end: a valid address, masked below)
-    trow[ts] = t;
-    if constexpr (ROPE) {
-      const int dj = __shfl(depth, t - len & 63);
-      pos[ts] = t < len ? t : len + max(dj, 0);
-    }
-  }
-  f32x4 acc[4][4];
-  int head[4], qoff[4];
-#pragma unroll
-  for (int mt = 0; mt < 4; ++mt) {
-    const int m = min(group * 64 + mt * 16 + n16, rows - 1);
-    head[mt] = m / a.N;
-    qoff[mt] = (m % a.N) * a.d;
-#pragma unroll
-    for (int ts = 0; ts < 4; ++ts) acc[ts][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  const T* q = (const T*)a.q + (size_t)b * a.N * a.d;
-  const int h0 = group * 64 / a.N, h1 = min(group * 64 + 63, rows - 1) / a.N;
-  for (int h = h0; h <= h1; ++h) {
-    for (int kk = 0; kk * KW < a.d_k; ++kk) {
-      const int j = kk * KW + g * VEC;
-      const bool in = j < a.d_k;                           // (d_k is whole pieces, not whole steps)
-      const int col = h * a.d_k + (in ? j : 0), po = piece_at(col, a.d_k, a.banded);
-      u32x4 kf[4], kl[4];
-#pragma unroll
-      for (int ts = 0; ts < 4; ++ts) {
-        kf[ts] = *(const u32x4*)(K + row_at(trow[ts], rp, a.d) + po);
-        if constexpr (ROPE) {
-          f32x4 cs[VEC / 4];
-#pragma unroll
-          for (int i = 0; i < VEC / 4; ++i) cs[i] = *(const f32x4*)(a.rope + (size_t)pos[ts] * a.d_k + (in ? j : 0) + 4 * i);
-          rotate_piece<DT>(kf[ts], cs, kf[ts], kl[ts]);
-          if (!in) kl[ts] = u32x4{0, 0, 0, 0};
-        }
-        if (!in) kf[ts] = u32x4{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int mt = 0; mt < 4; ++mt) {
-        const int lo = group * 64 + mt * 16;
-        if (lo >= rows || lo / a.N > h || min(lo + 15, rows - 1) / a.N < h) continue;      // (no row of this head)
-        u32x4 qf = *(const u32x4*)(q + qoff[mt] + col);
-        if (head[mt] != h || !in) qf = u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int ts = 0; ts < 4; ++ts) {
-          acc[ts][mt] = mma<DT>(kf[ts], qf, acc[ts][mt]);
-          if constexpr (ROPE && DT == DT_BF16) acc[ts][mt] = mma<DT>(kl[ts], qf, acc[ts][mt]);
-        }
-      }
-    }
-  }
-  // a lane has query row n16 of each tile and the cache rows 4 g .. 4 g + 3 of each score tile
-  float mx[4];
-#pragma unroll
-  for (int mt = 0; mt < 4; ++mt) {
-    const int m = group * 64 + mt * 16 + n16;
-    const uint64_t mine = __shfl((unsigned)anc, m % a.N) | (uint64_t)__shfl((unsigned)(anc >> 32), m % a.N) << 32;
-    const uint64_t see = m < rows ? mine : 0;
-    mx[mt] = NEG_INF;
-#pragma unroll
-    for (int ts = 0; ts < 4; ++ts)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int j = t0 + 16 * ts + 4 * g + r - len;
-        const bool on = j < 0 ? see != 0 : j < a.N && (see >> (j & 63) & 1);
-        const float s = on ? acc[ts][mt][r] * a.qscale : NEG_INF;
-        acc[ts][mt][r] = s;
-        mx[mt] = fmaxf(mx[mt], s);
-      }
-    mx[mt] = max_over_groups(mx[mt]);
-    if (g == 0) red[0][wave][mt * 16 + n16] = mx[mt];
-  }
-  lds_barrier();
-  constexpr int FR = 64 / KW;                              // fragments of a wave's 64 rows
-#pragma unroll
-  for (int mt = 0; mt < 4; ++mt) {
-    const int at = mt * 16 + n16;
-    const float m4 = fmaxf(fmaxf(red[0][0][at], red[0][1][at]), fmaxf(red[0][2][at], red[0][3][at]));
-    const float ref = m4 == NEG_INF ? NEG_INF : REF_STEP * ceilf(m4 * (1.f / REF_STEP));
-    const float sub = m4 == NEG_INF ? 0.f : ref;           // (nothing visible: numerators of 0, and of NaN scores NaN)
-    mx[mt] = ref;
-    float l = 0.f;
-#pragma unroll
-    for (int ts = 0; ts < 4; ++ts)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float p = exp2_of(acc[ts][mt][r] - sub);
-        if constexpr (DT == DT_BF16) p = (float)(__bf16)p; // the weighted sum takes bf16 numerators; their sum is of the same values
-        acc[ts][mt][r] = p;
-        l += p;
-      }
-    l = sum_over_row_groups(l);
-    if (g == 0) red[1][wave][at] = l;
-    const int tile = group * 4 + mt;
-    if (tile * 16 >= rows) continue;
-    u32x4* P = (u32x4*)a.P + (((size_t)b * a.MT + tile) * a.CT + (size_t)blk * (TREE_BLOCK / KW) + wave * FR) * 64 + lane;
-    if constexpr (DT == DT_BF16) {
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        u32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          v[i] = __float_as_uint(acc[2 * f + (i >> 1)][mt][2 * (i & 1)]) >> 16 | (__float_as_uint(acc[2 * f + (i >> 1)][mt][2 * (i & 1) + 1]) & 0xffff0000u);
-        P[f * 64] = v;
-      }
-    } else {
-#pragma unroll
-      for (int f = 0; f < 4; ++f) P[f * 64] = __builtin_bit_cast(u32x4, acc[f][mt]);
-    }
-  }
-  lds_barrier();
-  if (wave == 0) {
-    const int tile = group * 4 + lane / 16;
-    if (tile * 16 < rows) {
-      const size_t at = ((size_t)b * a.NB + blk) * a.MT * 16 + group * 64 + lane;
-      a.lsum[at] = red[1][0][lane] + red[1][1][lane] + red[1][2][lane] + red[1][3][lane];
-      const float m4 = fmaxf(fmaxf(red[0][0][lane], red[0][1][lane]), fmaxf(red[0][2][lane], red[0][3][lane]));
-      a.ref[at] = m4 == NEG_INF ? NEG_INF : REF_STEP * ceilf(m4 * (1.f / REF_STEP));
-    }
-  }
-}
-
-// Blocks of sequence b that split s sums: the sequence's own blocks, cut evenly
-__device__ __forceinline__ void split_blocks(const TreeArgs& a, int L, int s, int& first, int& end) {
-  const int nb = (L + TREE_BLOCK - 1) / TREE_BLOCK, per = (nb + a.S - 1) / a.S;
-  first = min(nb, s * per);
-  end = min(nb, first + per);
-}
-
-template <int DT>
-__device__ __forceinline__ u32x4 scaled(u32x4 p, float f) {
-  if constexpr (DT == DT_BF16) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      p[i] = (unsigned)bf16_bits(bf16_value(p[i] & 0xffffu) * f) | (unsigned)bf16_bits(__uint_as_float(p[i] & 0xffff0000u) * f) << 16;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = __float_as_uint(__uint_as_float(p[i]) * f);
-  }
-  return p;
-}
-
 template <int DT>
 __device__ __forceinline__ bool not_finite(u32x4 x) {
   bool bad = false;
@@ -296,159 +148,403 @@ __device__ __forceinline__ bool not_finite(u32x4 x) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// Weighted sum: C^T = K^T P^T over a split of the context, for all heads together: every query row sums whole rows of K.  A wave owns
-// 16 VEC columns of K (128 in bf16) and NT tiles of 16 query rows; a workgroup's four waves are four neighbouring column blocks of the same query
-// rows.  K goes from memory to the wave's registers and is transposed there (no other wave of the workgroup needs it); the numerators arrive as
-// operands.  Rows of the context need no mask; the chunks that hold drafted tokens or the cache's end are taken one by one behind them.
+// Scores and numerators.  A workgroup takes one head and 256 rows of the cache, a wave 16 TS of these: S^T = K_h q_h^T.  The head's
+// query rows (m = h N + i: the nodes of a head one after the other, so that small trees of many heads fill the tiles of the weighted sum) lie in up
+// to MAXT tiles of 16, whose other rows are other heads': zero in the query operand and written by their own workgroups.  As references the
+// numerators 2^(s - ref) take the block's maximum rounded up to a multiple of 32: a bf16 or fp32 numerator is as exact at 2^-32 as at 1,
+// and blocks whose maxima differ by less than that have the same reference, so that the weighted sum hardly ever needs a factor.  They
+// leave as operands of that sum (lane l of a 1 KB fragment: query row l % 16, cache rows slot_row(l / 16, j)).
 // ------------------------------------------------------------------------------------------------
-template <int DT, int NT>
-__global__ __launch_bounds__(256, NT > 4 ? 1 : 2) void tree_weighted_kernel(TreeArgs a) {
-  constexpr int VEC = Elem<DT>::VEC, CW = 16 * VEC, CH = 4 * VEC, CPB = TREE_BLOCK / CH;
+template <int DT, bool ROPE, int TS, int MAXT>
+__global__ __launch_bounds__(1024 / TS) void tree_scores_kernel(TreeArgs a) {
+  constexpr int VEC = Elem<DT>::VEC, KW = 4 * VEC, WV = 16 / TS, KU = 4;
   typedef typename Elem<DT>::T T;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
-  const int mgroups = (a.MT + NT - 1) / NT, dgroups = (a.DB + 3) / 4;
-  int unit, mg;
-  if (!unit_of_workgroup(blockIdx.x, mgroups, a.B * a.S * dgroups, true, unit, mg)) return;
-  const int block = unit % dgroups * 4 + wave, s = unit / dgroups % a.S, b = unit / dgroups / a.S;
-  if (block >= a.DB) return;
-  const int len = seq_len_of(a.seq_lens, b, a.T), L = len + a.N;
-  int first, end;
-  split_blocks(a, L, s, first, end);
-  if (first >= end) return;
-
-  const int col = min(block * CW + n16 * VEC, a.d - VEC);  // (columns past the row's end are not used by anybody)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x, blk = blockIdx.y, b = blockIdx.z;
+  const int len = __builtin_amdgcn_readfirstlane(seq_len_of(a.seq_lens, b, a.T)), L = len + a.N;
+  if (blk * TREE_BLOCK >= L) return;
+  __shared__ float red[2][WV][MAXT * 16];
+  __shared__ uint64_t odd[WV];
+  const T* K = (const T*)a.K + (size_t)b * a.k_bstride + piece_at(h * a.d_k, a.d_k, a.banded);
   const int rp = a.banded ? a.d_k : a.d;
-  const T* K = (const T*)a.K + (size_t)b * a.k_bstride + piece_at(col, a.d_k, a.banded);
-  const u32x4* P[NT];
-  int tile[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    tile[nt] = min(mg * NT + nt, a.MT - 1);
-    P[nt] = (const u32x4*)a.P + ((size_t)b * a.MT + tile[nt]) * a.CT * 64 + lane;
-  }
-  f32x4 acc[VEC][NT];
-  float ref[NT], l[NT], fac[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    ref[nt] = NEG_INF;
-    l[nt] = 0.f;
-    fac[nt] = 1.f;
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) acc[c][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  bool rescaled = false;                                   // whether some numerators of the present block need a factor
-  auto next_block = [&](int blk) {
-    float nref[NT], nl[NT];
-    bool differ = false;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const size_t at = (((size_t)b * a.NB + blk) * a.MT + tile[nt]) * 16 + n16;
-      nref[nt] = a.ref[at];
-      nl[nt] = a.lsum[at];
-      differ |= nref[nt] != ref[nt];
-    }
-    rescaled = __any(differ);
-    if (rescaled) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float top = fmaxf(ref[nt], nref[nt]);
-        const float old = top == ref[nt] ? 1.f : exp2_of(ref[nt] - top);
-        fac[nt] = top == nref[nt] ? 1.f : exp2_of(nref[nt] - top);
-        ref[nt] = top;
-        l[nt] = l[nt] * old + nl[nt] * fac[nt];
-#pragma unroll
-        for (int c = 0; c < VEC; ++c) acc[c][nt] *= old;
-      }
-      bool less = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) less |= fac[nt] != 1.f;
-      rescaled = __any(less);
-    } else {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) l[nt] += nl[nt];
-    }
-  };
-  auto load = [&](int chunk, u32x4 (&k)[VEC], u32x4 (&p)[NT]) {
-    const T* at = K + row_at(chunk * CH, rp, a.d);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) k[j] = *(const u32x4*)(at + slot_row(g, j) * rp);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) p[nt] = P[nt][(size_t)chunk * 64];
-  };
-  auto sum = [&](const u32x4 (&k)[VEC], u32x4 (&p)[NT]) {
-    u32x4 kt[VEC];
-    transpose<DT>(k, kt);
-    if (rescaled) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) p[nt] = scaled<DT>(p[nt], fac[nt]);
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int c = 0; c < VEC; ++c) acc[c][nt] = mma<DT>(kt[c], p[nt], acc[c][nt]);
-  };
+  const int m0 = h * a.N, m1 = h + 1 == a.H ? a.MT * 16 : m0 + a.N;      // the last head also has the rows that fill its last tile
+  const int tile0 = m0 / 16, ntiles = (m1 + 15) / 16 - tile0;
 
-  const int c0 = first * CPB, cend = min(end * CPB, (L + CH - 1) / CH), cfull = min(cend, max(c0, len / CH));
-  u32x4 k[2][VEC], p[2][NT];
-  if (c0 < cfull) load(c0, k[0], p[0]);
-  auto step = [&](int chunk, auto I) {
-    if (chunk % CPB == 0) next_block(chunk / CPB);
-    load(min(chunk + 1, cfull - 1), k[1 - I], p[1 - I]);
-    sum(k[I], p[I]);
-  };
-  int chunk = c0;
-  for (; chunk < cfull; chunk += 2) unrolled_steps<0, 2>(chunk, cfull, step);
-  for (chunk = max(c0, cfull); chunk < cend; ++chunk) {
-    if (chunk % CPB == 0) next_block(chunk / CPB);
-    // rows past the last drafted token are no part of the cache; a drafted key that is not finite must not reach nodes that do not see it
-    // (0 times infinity is no 0): it enters the sum as 0, and nodes that do see it get NaN
-    bool bad = false;
+  const int t0 = blk * TREE_BLOCK + wave * 16 * TS;
+  int trow[TS], pos[TS];
+  const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
+  const int depth = __popcll(anc) - 1;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      const int t = chunk * CH + slot_row(g, j);
-      k[0][j] = *(const u32x4*)(K + row_at(min(t, L - 1), rp, a.d));
-      if (t >= L) k[0][j] = u32x4{0, 0, 0, 0};
-      if (t >= len && not_finite<DT>(k[0][j])) {
-        bad = true;
-        k[0][j] = u32x4{0, 0, 0, 0};
-      }
+  for (int ts = 0; ts < TS; ++ts) {
+    const int t = min(t0 + 16 * ts + n16, L - 1);          // (rows past the end: a valid address, masked below)
+    trow[ts] = t;
+    if constexpr (ROPE) {
+      const int dj = __shfl(depth, t - len & 63);
+      pos[ts] = t < len ? t : len + max(dj, 0);
+    }
+  }
+  f32x4 acc[TS][MAXT];
+  const T* q[MAXT];
+  bool mine[MAXT];
+#pragma unroll
+  for (int mt = 0; mt < MAXT; ++mt) {
+    const int i = (tile0 + mt) * 16 + n16 - m0;
+    mine[mt] = i >= 0 && i < a.N;
+    q[mt] = (const T*)a.q + ((size_t)b * a.N + (mine[mt] ? i : 0)) * a.d + h * a.d_k;
+#pragma unroll
+    for (int ts = 0; ts < TS; ++ts) acc[ts][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  bool bad[TS] = {};                                       // whether the piece of a drafted key is not finite
+  for (int k0 = 0; k0 * KW < a.d_k; k0 += KU) {
+    u32x4 kf[KU][TS], kl[KU][TS];
+#pragma unroll
+    for (int ku = 0; ku < KU; ++ku) {
+      if ((k0 + ku) * KW >= a.d_k) break;
+      const int j = (k0 + ku) * KW + g * VEC;
+      const int at = j < a.d_k ? j : 0;                    // (d_k is whole pieces, not whole steps)
+#pragma unroll
+      for (int ts = 0; ts < TS; ++ts) kf[ku][ts] = *(const u32x4*)(K + row_at(trow[ts], rp, a.d) + at);
     }
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) p[0][nt] = P[nt][(size_t)chunk * 64];
-    if (__any(bad)) {
-      const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
-      for (int t = max(len, chunk * CH); t < min(L, chunk * CH + CH); ++t) {
-        if (!__any(not_finite<DT>(*(const u32x4*)(K + row_at(t, rp, a.d))))) continue;
+    for (int ku = 0; ku < KU; ++ku) {
+      if ((k0 + ku) * KW >= a.d_k) break;
+      const int j = (k0 + ku) * KW + g * VEC;
+      const bool in = j < a.d_k;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const int m = tile[nt] * 16 + n16, i = m % a.N, j = t - len;
-          const unsigned half = __shfl(j < 32 ? (unsigned)anc : (unsigned)(anc >> 32), i);
-          const bool sees = m < a.N * a.H && (half >> (j & 31) & 1);
+      for (int ts = 0; ts < TS; ++ts) {
+        if (t0 + 16 * ts + 16 > len) bad[ts] |= trow[ts] >= len && not_finite<DT>(kf[ku][ts]);
+        if constexpr (ROPE) {
+          f32x4 cs[VEC / 4];
 #pragma unroll
-          for (int c = 0; c < VEC; ++c)
+          for (int i = 0; i < VEC / 4; ++i) cs[i] = *(const f32x4*)(a.rope + (size_t)pos[ts] * a.d_k + (in ? j : 0) + 4 * i);
+          rotate_piece<DT>(kf[ku][ts], cs, kf[ku][ts], kl[ku][ts]);
+          if (!in) kl[ku][ts] = u32x4{0, 0, 0, 0};
+        }
+        if (!in) kf[ku][ts] = u32x4{0, 0, 0, 0};
+      }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[c][nt][r] = sees ? __builtin_nanf("") : acc[c][nt][r];
+      for (int mt = 0; mt < MAXT; ++mt) {
+        if (mt >= ntiles) break;
+        u32x4 qf = *(const u32x4*)(q[mt] + (in ? j : 0));
+        if (!mine[mt] || !in) qf = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int ts = 0; ts < TS; ++ts) {
+          acc[ts][mt] = mma<DT>(kf[ku][ts], qf, acc[ts][mt]);
+          if constexpr (ROPE && DT == DT_BF16) acc[ts][mt] = mma<DT>(kl[ku][ts], qf, acc[ts][mt]);
         }
       }
     }
-    sum(k[0], p[0]);
+  }
+  // a lane has query row n16 of each tile and the cache rows 4 g .. 4 g + 3 of each score tile
+#pragma unroll
+  for (int mt = 0; mt < MAXT; ++mt) {
+    if (mt >= ntiles) break;
+    const int i = (tile0 + mt) * 16 + n16 - m0;
+    const uint64_t own = __shfl((unsigned)anc, i & 63) | (uint64_t)__shfl((unsigned)(anc >> 32), i & 63) << 32;
+    const uint64_t see = mine[mt] ? own : 0;
+    float mx = NEG_INF;
+#pragma unroll
+    for (int ts = 0; ts < TS; ++ts)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = t0 + 16 * ts + 4 * g + r - len;
+        const bool on = j < 0 ? see != 0 : j < a.N && (see >> (j & 63) & 1);
+        const float s = on ? acc[ts][mt][r] * a.qscale : NEG_INF;
+        acc[ts][mt][r] = s;
+        mx = fmaxf(mx, s);
+      }
+    mx = max_over_groups(mx);
+    if (g == 0) red[0][wave][mt * 16 + n16] = mx;
+  }
+  uint64_t mask = 0;                                       // drafted rows of the wave that are not finite
+#pragma unroll
+  for (int ts = 0; ts < TS; ++ts) {
+    uint64_t m = __ballot(bad[ts]);
+    m = (m | m >> 16 | m >> 32 | m >> 48) & 0xffff;
+    const int at = t0 + 16 * ts - len;
+    mask |= at >= 64 || at <= -16 ? 0 : at >= 0 ? m << at : m >> -at;
+  }
+  if (lane == 0) odd[wave] = mask;
+  lds_barrier();
+  auto block_ref = [&](int at) {
+    float m = red[0][0][at];
+#pragma unroll
+    for (int w = 1; w < WV; ++w) m = fmaxf(m, red[0][w][at]);
+    return m == NEG_INF ? NEG_INF : REF_STEP * ceilf(m * (1.f / REF_STEP));
+  };
+#pragma unroll
+  for (int mt = 0; mt < MAXT; ++mt) {
+    if (mt >= ntiles) break;
+    const int at = mt * 16 + n16, m = (tile0 + mt) * 16 + n16;
+    const float ref = block_ref(at), sub = ref == NEG_INF ? 0.f : ref;     // (nothing visible: numerators of 0, and of NaN scores NaN)
+    float l = 0.f;
+#pragma unroll
+    for (int ts = 0; ts < TS; ++ts)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float p = exp2_of(acc[ts][mt][r] - sub);
+        if constexpr (DT == DT_BF16) p = (float)(__bf16)p; // the weighted sum takes bf16 numerators; their sum is of the same values
+        acc[ts][mt][r] = p;
+        l += p;
+      }
+    l = sum_over_row_groups(l);
+    if (g == 0) red[1][wave][at] = l;
+    if (m < m0 || m >= m1) continue;
+    // (a wave of one score tile has half of a bf16 fragment's rows: 8 of the lane's 16 bytes)
+    char* P = (char*)a.P + ((((size_t)b * a.MT + tile0 + mt) * a.CT + (size_t)blk * (TREE_BLOCK / KW)) * 64 + lane) * 16;
+#pragma unroll
+    for (int ts = 0; ts < TS; ++ts) {
+      const int sub16 = wave * TS + ts;
+      if constexpr (DT == DT_BF16) {
+        const uint2 v = {__float_as_uint(acc[ts][mt][0]) >> 16 | (__float_as_uint(acc[ts][mt][1]) & 0xffff0000u),
+                         __float_as_uint(acc[ts][mt][2]) >> 16 | (__float_as_uint(acc[ts][mt][3]) & 0xffff0000u)};
+        if constexpr (TS % 2 == 0) {
+          if (ts % 2 == 0) continue;
+          const uint2 u = {__float_as_uint(acc[ts - 1][mt][0]) >> 16 | (__float_as_uint(acc[ts - 1][mt][1]) & 0xffff0000u),
+                           __float_as_uint(acc[ts - 1][mt][2]) >> 16 | (__float_as_uint(acc[ts - 1][mt][3]) & 0xffff0000u)};
+          *(u32x4*)(P + sub16 / 2 * 1024) = u32x4{u.x, u.y, v.x, v.y};
+        } else {
+          *(uint2*)(P + sub16 / 2 * 1024 + sub16 % 2 * 8) = v;
+        }
+      } else {
+        *(u32x4*)(P + sub16 * 1024) = __builtin_bit_cast(u32x4, acc[ts][mt]);
+      }
+    }
+  }
+  lds_barrier();
+  for (int at = threadIdx.x; at < ntiles * 16; at += WV * 64) {
+    const int m = tile0 * 16 + at;
+    if (m < m0 || m >= m1) continue;
+    float l = red[1][0][at];
+#pragma unroll
+    for (int w = 1; w < WV; ++w) l += red[1][w][at];
+    const size_t to = ((size_t)b * a.NB + blk) * a.MT * 16 + m;
+    a.lsum[to] = l;
+    a.ref[to] = block_ref(at);
+  }
+  // which drafted keys are not finite in this head's columns: they lie in this block, or in this and the next
+  const int at = blk - len / TREE_BLOCK;
+  if (threadIdx.x == 0 && at >= 0) {
+    uint64_t any = 0;
+    for (int w = 0; w < WV; ++w) any |= odd[w];
+    a.odd[((size_t)b * 2 + at) * a.H + h] = any;
+    if (at == 0 && (L - 1) / TREE_BLOCK == blk) a.odd[((size_t)b * 2 + 1) * a.H + h] = 0;
+  }
+}
+
+// Chunks [first, end) of sequence b that split s sums: the sequence's steps of 64 rows, cut evenly.  `splits`: how many splits have any.
+constexpr int TREE_STEP = 64;
+struct Share { int first, end, splits; };
+__device__ __forceinline__ Share split_share(int L, int S, int s, int ch) {
+  const int steps = (L + TREE_STEP - 1) / TREE_STEP, per = (steps + S - 1) / S;
+  return {min(steps, s * per) * (TREE_STEP / ch), min(min(steps, (s + 1) * per) * (TREE_STEP / ch), (L + ch - 1) / ch), (steps + per - 1) / per};
+}
+
+// Numerators times 2^-e, e >= 0 a whole number: e off their exponents, down to 0.  (They are >= 0; one that is NaN is no longer, but then its row's
+// sum is, and the row's result with it.)
+__device__ __forceinline__ float lower_by(float ref, float fin) { return fin == ref ? 0.f : fminf(fin - ref, 255.f); }
+template <int DT>
+__device__ __forceinline__ u32x4 lowered(u32x4 p, float e) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const unsigned by = DT == DT_BF16 ? ((unsigned)e << 7) * 0x10001u : (unsigned)e << 23;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned x = p[i];                               // (a bit cast of the element itself takes element 0)
+    if constexpr (DT == DT_BF16)
+      p[i] = __builtin_bit_cast(unsigned, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, by)));
+    else
+      p[i] = __builtin_elementwise_sub_sat(x, by);
+  }
+  return p;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Weighted sum: C^T = K^T P^T over a split of the context, for all heads together: every query row sums whole rows of K.  A wave owns
+// 16 VEC columns of K (128 in bf16) and NT tiles of 16 query rows; a workgroup's four waves, one per SIMD, are four neighbouring column blocks
+// of the same query rows.  K goes from memory to the wave's registers and is transposed there (no other wave of the workgroup needs it), RK
+// steps of 64 rows ahead; the numerators are the same for the four waves and go through LDS, a step ahead, one barrier a step.
+// ------------------------------------------------------------------------------------------------
+template <int DT, int NT> struct Weighted {
+  static constexpr int VEC = Elem<DT>::VEC, CH = 4 * VEC, SC = TREE_STEP / CH;    // chunks of a step
+  static constexpr int PF = (SC * NT + 3) / 4;                                    // fragments of a step that a wave brings
+  static constexpr int KR = VEC * NT > 48 ? 3 : 2 * SC;                           // chunks of K in registers
+  static constexpr int UN = 2 * SC == KR ? 2 : 3;                                 // steps after which the registers' roles are the same again
+  static_assert(UN * SC % KR == 0, "");
+};
+
+template <int DT, int NT>
+__global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
+  typedef Weighted<DT, NT> G;
+  constexpr int VEC = G::VEC, CW = 16 * VEC, CH = G::CH, SC = G::SC, PF = G::PF, KR = G::KR, UN = G::UN, CPB = TREE_BLOCK / CH, ROWS = NT * 16, SUB = 256 / ROWS;
+  typedef typename Elem<DT>::T T;
+  __shared__ u32x4 ring[2][SC * NT * 64];
+  __shared__ float red[SUB][ROWS], fin[ROWS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+  const int mgroups = (a.MT + NT - 1) / NT, dgroups = (a.DB + 3) / 4;
+  int unit, mg;
+  if (!unit_of_workgroup(blockIdx.x, mgroups, a.B * a.S * dgroups, true, unit, mg)) return;
+  const int dg = unit % dgroups, block = dg * 4 + wave, s = unit / dgroups % a.S, b = unit / dgroups / a.S;
+  const int len = __builtin_amdgcn_readfirstlane(seq_len_of(a.seq_lens, b, a.T)), L = len + a.N;
+  const Share share = split_share(L, a.S, s, CH);
+  if (share.first >= share.end) return;
+  const int c0 = share.first;
+
+  const int rp = a.banded ? a.d_k : a.d;
+  const T* K = (const T*)a.K + (size_t)b * a.k_bstride;
+  const int piece = piece_at(min(block * CW + n16 * VEC, a.d - VEC), a.d_k, a.banded);     // (columns past the row's end are not used by anybody)
+  unsigned voff[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) voff[j] = (unsigned)(piece + slot_row(g, j) * rp) * sizeof(T);
+  const u32x4* pp[PF];
+#pragma unroll
+  for (int i = 0; i < PF; ++i) {
+    const int f = min(wave + 4 * i, SC * NT - 1);          // (the last wave may bring a fragment twice)
+    pp[i] = (const u32x4*)a.P + (((size_t)b * a.MT + min(mg * NT + f / SC, a.MT - 1)) * a.CT + f % SC) * 64;
+  }
+  // drafted keys that are not finite: the steps that hold drafted ones are taken one by one behind the others
+  const uint64_t odd = odd_keys(a, b, lane);
+  const int cend = odd ? min(share.end, max(c0, len / TREE_STEP * SC)) : share.end, nsteps = (cend - c0 + SC - 1) / SC;
+
+  u32x4 k[KR][VEC], pr[PF];
+  float rr[PF];
+  auto load_k = [&](int i, u32x4 (&to)[VEC]) {
+    const int chunk = min(c0 + i, cend - 1);
+    const T* base = K + row_at(chunk * CH, rp, a.d);
+    const unsigned lim = (unsigned)(piece + min(L - 1 - chunk * CH, CH - 1) * rp) * sizeof(T);     // (rows past the cache's end: its last row, whose numerators there are 0)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) to[j] = *(const u32x4*)((const char*)base + min(voff[j], lim));
+  };
+  auto frag_row = [&](int i) { return min(mg * NT + min(wave + 4 * i, SC * NT - 1) / SC, a.MT - 1) * 16 + n16; };
+  auto load_p = [&](int step) {
+    const int chunk = c0 + min(step, nsteps - 1) * SC;
+#pragma unroll
+    for (int i = 0; i < PF; ++i) {
+      pr[i] = pp[i][(size_t)chunk * 64 + lane];
+      rr[i] = a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + frag_row(i)];
+    }
+  };
+  if (nsteps > 0) {
+    load_p(0);
+#pragma unroll
+    for (int i = 0; i < KR; ++i) load_k(i, k[i]);
   }
 
+  // the split's reference and sum of every row
+  {
+    const int row = threadIdx.x % ROWS, sub = threadIdx.x / ROWS;
+    const int b0 = c0 / CPB, b1 = (share.end - 1) / CPB + 1;
+    const size_t at = (size_t)b * a.NB * a.MT * 16 + min(mg * NT + row / 16, a.MT - 1) * 16 + row % 16;
+    const size_t pitch = (size_t)a.MT * 16;
+    float top = NEG_INF;
+    if (sub < SUB) {
+#pragma unroll 4
+      for (int blk = b0 + sub; blk < b1; blk += SUB) top = fmaxf(top, a.ref[at + blk * pitch]);
+      red[sub][row] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SUB; ++i) top = fmaxf(top, red[i][row]);
+    if (sub == 0) fin[row] = top;
+    __syncthreads();
+    if (dg == 0) {                                         // (the first column blocks' workgroups note them for the projection)
+      float l = 0.f;
+      if (sub < SUB) {
+#pragma unroll 4
+        for (int blk = b0 + sub; blk < b1; blk += SUB) {
+          const float r = a.ref[at + blk * pitch];
+          if (blk * CPB >= c0) l += a.lsum[at + blk * pitch] * (r == top ? 1.f : exp2_of(r - top));   // (a block's sum: with its first row)
+        }
+        red[sub][row] = l;
+      }
+      __syncthreads();
+      const size_t to = (((size_t)b * a.S + s) * a.MT + mg * NT + row / 16) * 16 + row % 16;
+      l = 0.f;
+#pragma unroll
+      for (int i = 0; i < SUB; ++i) l += red[i][row];
+      if (sub == 0 && mg * NT + row / 16 < a.MT) {
+        a.sref[to] = top;
+        a.sl[to] = l;
+      }
+    }
+  }
+  f32x4 acc[VEC][NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) acc[c][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  float fr[PF];
+#pragma unroll
+  for (int i = 0; i < PF; ++i) fr[i] = fin[min(wave + 4 * i, SC * NT - 1) / SC * 16 + n16];
+  auto park_p = [&](int slot) {
+#pragma unroll
+    for (int i = 0; i < PF; ++i) ring[slot][min(wave + 4 * i, SC * NT - 1) * 64 + lane] = lowered<DT>(pr[i], lower_by(rr[i], fr[i]));
+  };
+  if (nsteps > 0) {
+    park_p(0);
+    load_p(1);
+  }
+  auto step = [&](int st, auto I) {
+    lds_barrier();                                         // (everybody has parked this step's numerators and read the last step's)
+#pragma unroll
+    for (int c = 0; c < SC; ++c) {
+      u32x4 (&kc)[VEC] = k[(I * SC + c) % KR], kt[VEC];
+      transpose<DT>(kc, kt);
+      load_k(st * SC + c + KR, kc);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const u32x4 pf = ring[st & 1][(nt * SC + c) * 64 + lane];
+#pragma unroll
+        for (int cc = 0; cc < VEC; ++cc) mma_in_place<DT>(kt[cc], pf, acc[cc][nt]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    park_p(st + 1 & 1);
+    load_p(st + 2);
+  };
+  int st = 0;
+  for (; st + UN <= nsteps; st += UN) full_steps<0, UN>(st, step);
+  unrolled_steps<0, UN>(st, nsteps, step);
+
+  if (odd) {
+    // A drafted key that is not finite must not reach nodes that do not see it (0 times infinity is no 0): it enters the sum as 0, and the
+    // projection makes NaN of the nodes that do see it.
+    for (int chunk = max(c0, len / TREE_STEP * SC); chunk < share.end; ++chunk) {
+      u32x4 kt[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const int t = min(chunk * CH + slot_row(g, j), L - 1);
+        k[0][j] = *(const u32x4*)(K + piece + row_at(t, rp, a.d));
+        if (t >= len && (odd >> (t - len) & 1)) k[0][j] = u32x4{0, 0, 0, 0};
+      }
+      transpose<DT>(k[0], kt);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        u32x4 pf = ((const u32x4*)a.P)[(((size_t)b * a.MT + min(mg * NT + nt, a.MT - 1)) * a.CT + chunk) * 64 + lane];
+        pf = lowered<DT>(pf, lower_by(a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + min(mg * NT + nt, a.MT - 1) * 16 + n16], fin[nt * 16 + n16]));
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) mma_in_place<DT>(kt[c], pf, acc[c][nt]);
+      }
+    }
+  }
+
+  settle();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) asm volatile("" : "+a"(acc[c][nt]));      // (nothing reads them before that wait)
   // a lane has query row n16 of each tile and the columns 4 VEC g + VEC r + c of the block, which the projection reads as operands
+  if (block >= a.DB) return;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     if (mg * NT + nt >= a.MT) continue;
-    const size_t row = ((size_t)b * a.S + s) * a.MT + tile[nt];
+    const size_t row = ((size_t)b * a.S + s) * a.MT + mg * NT + nt;
     f32x4* C = (f32x4*)a.C + (row * a.DB + block) * VEC * 64 + lane;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int hf = 0; hf < VEC / 4; ++hf)
         C[(r * (VEC / 4) + hf) * 64] = f32x4{acc[hf * 4][nt][r], acc[hf * 4 + 1][nt][r], acc[hf * 4 + 2][nt][r], acc[hf * 4 + 3][nt][r]};
-    if (block == 0 && g == 0) {
-      a.sref[row * 16 + n16] = ref[nt];
-      a.sl[row * 16 + n16] = l[nt];
-    }
   }
 }
 
@@ -477,10 +573,14 @@ __global__ __launch_bounds__(512) void tree_project_kernel(TreeArgs a) {
     tt[i] = tile0 + x % ntiles;
   }
   // weights of the splits: 2^(ref_s - max) over the whole sum; 0 where a split or a row has nothing (its C may be unwritten)
-  for (int e = threadIdx.x; e < NM * 16; e += 512) {
-    const int i = e / 16, x = min(x0 + i, a.B * ntiles - 1), b = x / ntiles, t = tile0 + x % ntiles;
-    const int L = seq_len_of(a.seq_lens, b, a.T) + a.N;
-    const int nb = (L + TREE_BLOCK - 1) / TREE_BLOCK, per = (nb + a.S - 1) / a.S, ns = (nb + per - 1) / per;
+  if (wave < NM) {
+    const int i = wave, e = i * 16 + n16, x = min(x0 + i, a.B * ntiles - 1), b = x / ntiles, t = tile0 + x % ntiles;
+    bool nan = false;                                      // (a node that sees a drafted key that is not finite)
+    if (const uint64_t odd = odd_keys(a, b, lane)) {
+      const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
+      nan = __shfl((anc & odd) != 0 ? 1 : 0, (t * 16 + n16) % a.N);
+    }
+    const int ns = split_share(seq_len_of(a.seq_lens, b, a.T) + a.N, a.S, 0, 4 * VEC).splits;
     float top = NEG_INF, sum = 0.f;
     for (int s = 0; s < ns; ++s) top = fmaxf(top, a.sref[(((size_t)b * a.S + s) * a.MT + t) * 16 + e % 16]);
     for (int s = 0; s < ns; ++s) {
@@ -490,7 +590,7 @@ __global__ __launch_bounds__(512) void tree_project_kernel(TreeArgs a) {
     for (int s = 0; s < a.S; ++s) {
       float w = 0.f;
       if (s < ns && sum != 0.f) w = (top == NEG_INF ? 1.f : exp2_of(a.sref[(((size_t)b * a.S + s) * a.MT + t) * 16 + e % 16] - top)) / sum;
-      weight[(i * a.S + s) * 16 + e % 16] = w;
+      weight[(i * a.S + s) * 16 + e % 16] = nan ? __builtin_nanf("") : w;
     }
   }
   lds_barrier();
@@ -596,11 +696,17 @@ __global__ __launch_bounds__(256) void tree_sum_kernel(const float* part, int cs
     ((f32x4*)out)[i] = v;
 }
 
+template <int DT, bool ROPE, int TS>
+void launch_tree_scores_s(const TreeArgs& a, hipStream_t st) {
+  const dim3 grid(a.H, a.NB, a.B), block(1024 / TS);
+  if (a.N <= 17) hipLaunchKernelGGL((tree_scores_kernel<DT, ROPE, TS, 2>), grid, block, 0, st, a);      // (a head's rows touch two tiles at most)
+  else hipLaunchKernelGGL((tree_scores_kernel<DT, ROPE, TS, 5>), grid, block, 0, st, a);
+}
 template <int DT>
 void launch_tree_scores_t(const TreeArgs& a, hipStream_t st) {
-  const dim3 grid((a.N * a.H + 63) / 64, a.NB, a.B);
-  if (a.rope) hipLaunchKernelGGL((tree_scores_kernel<DT, true>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((tree_scores_kernel<DT, false>), grid, dim3(256), 0, st, a);
+  const bool few = (long)a.H * a.NB * a.B <= 512;          // few workgroups: more waves of fewer rows
+  if (a.rope) few ? launch_tree_scores_s<DT, true, 1>(a, st) : launch_tree_scores_s<DT, true, 4>(a, st);
+  else few ? launch_tree_scores_s<DT, false, 1>(a, st) : launch_tree_scores_s<DT, false, 4>(a, st);
 }
 
 template <int DT>
@@ -610,7 +716,9 @@ void launch_tree_weighted_t(const TreeArgs& a, int nt, hipStream_t st) {
   switch (nt) {
     case 1: hipLaunchKernelGGL((tree_weighted_kernel<DT, 1>), grid, dim3(256), 0, st, a); break;
     case 2: hipLaunchKernelGGL((tree_weighted_kernel<DT, 2>), grid, dim3(256), 0, st, a); break;
+    case 3: hipLaunchKernelGGL((tree_weighted_kernel<DT, 3>), grid, dim3(256), 0, st, a); break;
     case 4: hipLaunchKernelGGL((tree_weighted_kernel<DT, 4>), grid, dim3(256), 0, st, a); break;
+    case 6: hipLaunchKernelGGL((tree_weighted_kernel<DT, 6>), grid, dim3(256), 0, st, a); break;
     default: hipLaunchKernelGGL((tree_weighted_kernel<DT, 8>), grid, dim3(256), 0, st, a); break;
   }
 }
@@ -630,18 +738,14 @@ void launch_tree_project_t(const TreeArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Query tiles of 16 rows that a wave of the weighted sum takes together: as many as there are, up to eight (all 512 registers).
-int tree_tiles(int H, int N) {
-  const int mt = (H * N + 15) / 16;
-  return mt >= 5 ? 8 : mt >= 3 ? 4 : mt;
-}
-
-// Context splits of the weighted sum: until there is a workgroup for every compute unit, a block of rows each at least.  Grows with T.
-int tree_splits(int dtype, int B, int N, int H, int T, int d) {
-  const int nt = tree_tiles(H, N), mt = (H * N + 15) / 16, cw = 16 * vec_elems(dtype);
-  const long wgs = (long)B * ((mt + nt - 1) / nt) * ((d + 4 * cw - 1) / (4 * cw));
-  const int nb = (T + N + TREE_BLOCK_ROWS - 1) / TREE_BLOCK_ROWS;
-  return (int)std::max(1l, std::min<long>({(256 + wgs - 1) / wgs, nb, TREE_MAX_SPLITS}));
+// How the weighted sum is cut: NT query tiles of 16 rows to a wave, S splits of the context.  The fewest tiles of the sizes that
+// there are in the fewest groups of eight at most; splits until there is a workgroup for every compute unit, a step of rows each at least.
+void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* splits) {
+  const int mt = (H * N + 15) / 16, groups = (mt + 7) / 8, each = (mt + groups - 1) / groups, cw = 16 * vec_elems(dtype);
+  *nt = each > 6 ? 8 : each > 4 ? 6 : each;
+  const long wgs = (long)B * ((mt + *nt - 1) / *nt) * ((d + 4 * cw - 1) / (4 * cw));
+  const int steps = (T + N + TREE_STEP - 1) / TREE_STEP;
+  *splits = (int)std::max(1l, std::min<long>({(256 + wgs - 1) / wgs, (steps + 3) / 4, TREE_MAX_SPLITS}));
 }
 
 // Row splits of W_KV in the projection: until there is a workgroup for every compute unit, a block of rows for each wave at least.
@@ -656,9 +760,8 @@ void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st) {
   else launch_tree_scores_t<DT_F32>(a, st);
 }
 void launch_tree_weighted(int dtype, const TreeArgs& a, hipStream_t st) {
-  const int nt = tree_tiles(a.H, a.N);
-  if (dtype == DT_BF16) launch_tree_weighted_t<DT_BF16>(a, nt, st);
-  else launch_tree_weighted_t<DT_F32>(a, nt, st);
+  if (dtype == DT_BF16) launch_tree_weighted_t<DT_BF16>(a, a.NT, st);
+  else launch_tree_weighted_t<DT_F32>(a, a.NT, st);
 }
 void launch_tree_project(int dtype, const TreeArgs& a, hipStream_t st) {
   if (dtype == DT_BF16) launch_tree_project_t<DT_BF16>(a, st);

@@ -813,18 +813,18 @@ extern "C" int vanilla_attention_block(const void* x, const void* W_Q, const voi
 namespace {
 
 // Bounds that keep grids and 32-bit offsets inside their ranges
-constexpr int TREE_MAX_BATCH = 32768, TREE_MAX_ROWS = 1 << 20, TREE_MAX_WIDTH = 1 << 20, TREE_MAX_CONTEXT = 1 << 23, TREE_MAX_VOCABULARY = 1 << 24;
+constexpr int TREE_MAX_BATCH = 32768, TREE_MAX_ROWS = 1 << 20, TREE_MAX_WIDTH = 1 << 20, TREE_MAX_CONTEXT = (TREE_MAX_BLOCKS - 1) * TREE_BLOCK_ROWS, TREE_MAX_VOCABULARY = 1 << 24;
 
-struct TreePlan { size_t off_P, off_ref, off_lsum, off_C, off_sref, off_sl, off_part, total; };
+struct TreePlan { size_t off_P, off_ref, off_lsum, off_C, off_sref, off_sl, off_odd, off_part, total; };
 
-// Every term grows with T (tree_splits does).
+// Every term grows with T (tree_cut's splits do).
 TreePlan tree_layout(TreeArgs& a, int dtype) {
   const int vec = vec_elems(dtype), ch = 4 * vec, cw = 16 * vec;
   a.MT = (a.H * a.N + 15) / 16;
   a.NB = (a.T + a.N + TREE_BLOCK_ROWS - 1) / TREE_BLOCK_ROWS;
   a.CT = a.NB * (TREE_BLOCK_ROWS / ch);
   a.DB = (a.d + cw - 1) / cw;
-  a.S = tree_splits(dtype, a.B, a.N, a.H, a.T, a.d);
+  tree_cut(dtype, a.B, a.N, a.H, a.T, a.d, &a.NT, &a.S);
   a.csw = tree_row_splits(dtype, a.B, a.N, a.H, a.d);
   TreePlan p;
   size_t o = 0;
@@ -836,6 +836,7 @@ TreePlan tree_layout(TreeArgs& a, int dtype) {
   p.off_C = take(sizeof(float) * rows * a.S * a.DB * cw);
   p.off_sref = take(sizeof(float) * rows * a.S);
   p.off_sl = take(sizeof(float) * rows * a.S);
+  p.off_odd = take(sizeof(uint64_t) * 2 * (size_t)a.B * a.H);
   p.off_part = take(a.csw > 1 ? sizeof(float) * a.csw * (size_t)a.B * a.N * a.d : 0);
   p.total = o;
   return p;
@@ -896,6 +897,7 @@ extern "C" int slim_tree_decode(const void* q, const void* Kcache, const void* W
   a.P = ws + p.off_P;
   a.ref = (float*)(ws + p.off_ref); a.lsum = (float*)(ws + p.off_lsum);
   a.C = (float*)(ws + p.off_C); a.sref = (float*)(ws + p.off_sref); a.sl = (float*)(ws + p.off_sl);
+  a.odd = (uint64_t*)(ws + p.off_odd);
   a.part = (float*)(ws + p.off_part);
   StageTimer tm(o, st);
   launch_tree_scores(dtype, a, st);
