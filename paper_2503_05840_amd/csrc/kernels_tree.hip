@@ -49,13 +49,14 @@ __device__ __forceinline__ uint64_t odd_keys(const TreeArgs& a, int b, int lane)
 
 // acc += a b, the accumulator staying where it is.  With as many accumulators as there are accumulation registers the compiler gives a product
 // another destination than its addend and moves hundreds of registers a step to put that right.  In an asm statement the wait states
-// are this code's: two between a vector instruction that writes an operand and the product (the s_nop), those of reading a result
-// in settle().
+// are this code's: two between a vector instruction that writes an operand and the product -- operands_ready() where operands may be that
+// new --, those of reading a result in settle().
 template <int DT>
 __device__ __forceinline__ void mma_in_place(const u32x4& a, const u32x4& b, f32x4& acc) {
-  if constexpr (DT == DT_BF16) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+  if constexpr (DT == DT_BF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
   else acc = mma<DT>(a, b, acc);
 }
+__device__ __forceinline__ void operands_ready() { asm volatile("s_nop 1"); }
 __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
 // VEC rows x VEC columns per lane -> VEC operands (one per column), each VEC rows of that column
@@ -69,6 +70,13 @@ __device__ __forceinline__ void transpose(const u32x4 (&k)[VEC], u32x4 (&a)[VEC]
 #pragma unroll
       for (int j = 0; j < 4; ++j) a[c][j] = k[j][c];
   }
+}
+
+// The same, element pair by element pair: what rows 2 jp and 2 jp + 1 (bf16) or row jp (fp32) give operand c.
+template <int DT, int VEC = Elem<DT>::VEC>
+__device__ __forceinline__ void transpose_one(const u32x4 (&k)[VEC], u32x4 (&a)[VEC], int jp, int c) {
+  if constexpr (DT == DT_BF16) a[c][jp] = __builtin_amdgcn_perm(k[2 * jp + 1][c / 2], k[2 * jp][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+  else a[c][jp] = k[jp][c];
 }
 
 // Row of a chunk (4 * VEC rows) that slot (g, j) of an operand stands for: the rows that a score tile leaves in lane group g, so that numerators
@@ -367,9 +375,9 @@ __device__ __forceinline__ u32x4 lowered(u32x4 p, float e) {
 template <int DT, int NT> struct Weighted {
   static constexpr int VEC = Elem<DT>::VEC, CH = 4 * VEC, SC = TREE_STEP / CH;    // chunks of a step
   static constexpr int PF = (SC * NT + 3) / 4;                                    // fragments of a step that a wave brings
-  static constexpr int KR = VEC * NT > 48 ? 3 : 2 * SC;                           // chunks of K in registers
-  static constexpr int UN = 2 * SC == KR ? 2 : 3;                                 // steps after which the registers' roles are the same again
-  static_assert(UN * SC % KR == 0, "");
+  static constexpr int KR = VEC * NT > 48 ? 2 : 2 * SC;                           // chunks of K in registers, besides the one in use
+  static constexpr int UN = 2 * SC == KR ? 2 : 1;                                 // steps after which the registers' roles are the same again
+  static_assert(UN * SC % KR == 0 && SC % 2 == 0, "");
 };
 
 template <int DT, int NT>
@@ -403,30 +411,29 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   }
   // drafted keys that are not finite: the steps that hold drafted ones are taken one by one behind the others
   const uint64_t odd = odd_keys(a, b, lane);
-  const int cend = odd ? min(share.end, max(c0, len / TREE_STEP * SC)) : share.end, nsteps = (cend - c0 + SC - 1) / SC;
+  const int cend = __builtin_amdgcn_readfirstlane(odd ? min(share.end, max(c0, len / TREE_STEP * SC)) : share.end), nsteps = (cend - c0 + SC - 1) / SC;
 
-  u32x4 k[KR][VEC], pr[PF];
+  u32x4 k[KR][VEC], kt[2][VEC], pr[PF];
   float rr[PF];
-  auto load_k = [&](int i, u32x4 (&to)[VEC]) {
+  // (rows past the cache's end: its last row, whose numerators there are 0)
+  auto load_row = [&](int i, int j) {
     const int chunk = min(c0 + i, cend - 1);
-    const T* base = K + row_at(chunk * CH, rp, a.d);
-    const unsigned lim = (unsigned)(piece + min(L - 1 - chunk * CH, CH - 1) * rp) * sizeof(T);     // (rows past the cache's end: its last row, whose numerators there are 0)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) to[j] = *(const u32x4*)((const char*)base + min(voff[j], lim));
+    const unsigned lim = (unsigned)(piece + min(L - 1 - chunk * CH, CH - 1) * rp) * sizeof(T);
+    return *(const u32x4*)((const char*)(K + row_at(chunk * CH, rp, a.d)) + min(voff[j], lim));
   };
   auto frag_row = [&](int i) { return min(mg * NT + min(wave + 4 * i, SC * NT - 1) / SC, a.MT - 1) * 16 + n16; };
-  auto load_p = [&](int step) {
+  auto load_p = [&](int step, int i) {
     const int chunk = c0 + min(step, nsteps - 1) * SC;
-#pragma unroll
-    for (int i = 0; i < PF; ++i) {
-      pr[i] = pp[i][(size_t)chunk * 64 + lane];
-      rr[i] = a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + frag_row(i)];
-    }
+    pr[i] = pp[i][(size_t)chunk * 64 + lane];
+    rr[i] = a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + frag_row(i)];
   };
   if (nsteps > 0) {
-    load_p(0);
 #pragma unroll
-    for (int i = 0; i < KR; ++i) load_k(i, k[i]);
+    for (int i = 0; i < PF; ++i) load_p(0, i);
+#pragma unroll
+    for (int i = 0; i < KR; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) k[i][j] = load_row(i, j);
   }
 
   // the split's reference and sum of every row
@@ -476,31 +483,58 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   float fr[PF];
 #pragma unroll
   for (int i = 0; i < PF; ++i) fr[i] = fin[min(wave + 4 * i, SC * NT - 1) / SC * 16 + n16];
-  auto park_p = [&](int slot) {
-#pragma unroll
-    for (int i = 0; i < PF; ++i) ring[slot][min(wave + 4 * i, SC * NT - 1) * 64 + lane] = lowered<DT>(pr[i], lower_by(rr[i], fr[i]));
-  };
+  u32x4 pf[2];
   if (nsteps > 0) {
-    park_p(0);
-    load_p(1);
+#pragma unroll
+    for (int i = 0; i < PF; ++i) {
+      ring[0][min(wave + 4 * i, SC * NT - 1) * 64 + lane] = lowered<DT>(pr[i], lower_by(rr[i], fr[i]));
+      load_p(1, i);
+    }
+    transpose<DT>(k[0], kt[0]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) k[0][j] = load_row(KR, j);
+    lds_barrier();
+    pf[0] = ring[0][lane];
   }
+  // One step: its products, and between them, an instruction or two behind each, what the next ones need -- the next chunk's keys transposed, those of
+  // the chunk KR later requested into their registers, the next step's numerators parked and those of the step after requested.  Each
+  // tile's operand is read a tile ahead; before the last tile the waves meet, so that the next step's first can be.
   auto step = [&](int st, auto I) {
-    lds_barrier();                                         // (everybody has parked this step's numerators and read the last step's)
 #pragma unroll
     for (int c = 0; c < SC; ++c) {
-      u32x4 (&kc)[VEC] = k[(I * SC + c) % KR], kt[VEC];
-      transpose<DT>(kc, kt);
-      load_k(st * SC + c + KR, kc);
+      u32x4 (&next)[VEC] = k[(I * SC + c + 1) % KR], (&ktn)[VEC] = kt[(c + 1) & 1];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const u32x4 pf = ring[st & 1][(nt * SC + c) * 64 + lane];
+        const int at = c * NT + nt;                        // of SC NT tiles
+        if (at + 1 < SC * NT) {
+          pf[(at + 1) & 1] = ring[st & 1][((nt + 1) % NT * SC + (nt + 1) / NT + c) * 64 + lane];
+        } else {
+          lds_barrier();
+          pf[(at + 1) & 1] = ring[st + 1 & 1][lane];
+        }
+        operands_ready();
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int cc = 0; cc < VEC; ++cc) mma_in_place<DT>(kt[cc], pf, acc[cc][nt]);
+        for (int cc = 0; cc < VEC; ++cc) {
+          mma_in_place<DT>(kt[c & 1][cc], pf[at & 1], acc[cc][nt]);
+#pragma unroll
+          for (int jp = 4 * nt / NT; jp < 4 * (nt + 1) / NT; ++jp) {
+            transpose_one<DT>(next, ktn, jp, cc);
+            if (cc == VEC - 1) {
+#pragma unroll
+              for (int j = jp * VEC / 4; j < (jp + 1) * VEC / 4; ++j) next[j] = load_row(st * SC + c + 1 + KR, j);
+            }
+          }
+#pragma unroll
+          for (int i = PF * at / (SC * NT - 1); i < PF * (at + 1) / (SC * NT - 1) && i < PF; ++i) {     // (before the last tile)
+            if (cc == 0) pr[i] = lowered<DT>(pr[i], lower_by(rr[i], fr[i]));
+            if (cc == VEC / 2) ring[st + 1 & 1][min(wave + 4 * i, SC * NT - 1) * 64 + lane] = pr[i];
+            if (cc == VEC - 1) load_p(st + 2, i);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
-    park_p(st + 1 & 1);
-    load_p(st + 2);
   };
   int st = 0;
   for (; st + UN <= nsteps; st += UN) full_steps<0, UN>(st, step);
@@ -510,20 +544,20 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
     // A drafted key that is not finite must not reach nodes that do not see it (0 times infinity is no 0): it enters the sum as 0, and the
     // projection makes NaN of the nodes that do see it.
     for (int chunk = max(c0, len / TREE_STEP * SC); chunk < share.end; ++chunk) {
-      u32x4 kt[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const int t = min(chunk * CH + slot_row(g, j), L - 1);
         k[0][j] = *(const u32x4*)(K + piece + row_at(t, rp, a.d));
         if (t >= len && (odd >> (t - len) & 1)) k[0][j] = u32x4{0, 0, 0, 0};
       }
-      transpose<DT>(k[0], kt);
+      transpose<DT>(k[0], kt[0]);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         u32x4 pf = ((const u32x4*)a.P)[(((size_t)b * a.MT + min(mg * NT + nt, a.MT - 1)) * a.CT + chunk) * 64 + lane];
         pf = lowered<DT>(pf, lower_by(a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + min(mg * NT + nt, a.MT - 1) * 16 + n16], fin[nt * 16 + n16]));
+        operands_ready();
 #pragma unroll
-        for (int c = 0; c < VEC; ++c) mma_in_place<DT>(kt[c], pf, acc[c][nt]);
+        for (int c = 0; c < VEC; ++c) mma_in_place<DT>(kt[0][c], pf, acc[c][nt]);
       }
     }
   }
