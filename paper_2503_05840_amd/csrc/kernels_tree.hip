@@ -340,11 +340,12 @@ __global__ __launch_bounds__(1024 / TS) void tree_scores_kernel(TreeArgs a) {
   }
 }
 
-// Chunks [first, end) of sequence b that split s sums: the sequence's steps of 64 rows, cut evenly.  `splits`: how many splits have any.
+// Chunks [first, end) of sequence b that split s sums, and how many splits have any: the same number of steps of 64 rows in every split of every
+// sequence (but its last), so that ragged batches are cut as evenly as others.
 constexpr int TREE_STEP = 64;
 struct Share { int first, end, splits; };
-__device__ __forceinline__ Share split_share(int L, int S, int s, int ch) {
-  const int steps = (L + TREE_STEP - 1) / TREE_STEP, per = (steps + S - 1) / S;
+__device__ __forceinline__ Share split_share(const TreeArgs& a, int L, int s, int ch) {
+  const int all = (a.T + a.N + TREE_STEP - 1) / TREE_STEP, per = (all + a.S - 1) / a.S, steps = (L + TREE_STEP - 1) / TREE_STEP;
   return {min(steps, s * per) * (TREE_STEP / ch), min(min(steps, (s + 1) * per) * (TREE_STEP / ch), (L + ch - 1) / ch), (steps + per - 1) / per};
 }
 
@@ -380,6 +381,32 @@ template <int DT, int NT> struct Weighted {
   static_assert(UN * SC % KR == 0 && SC % 2 == 0, "");
 };
 
+// Workgroup i -> its query tiles (mg), column blocks (dg), split and sequence.  An XCD's workgroups at one time share rows of K (same dg) and
+// numerators (same mg) through its L2: it gets blocks of up to 8 mg x 4 dg.  Four neighbouring dg are 4 KB of every row, all channels of
+// the L2 where rows are a multiple of that long; the 16 mg x 2 dg of before drew on a quarter of them.
+struct WeightedPlace { bool any; int mg, dg, s, b; };
+__host__ __device__ __forceinline__ int weighted_units(const TreeArgs& a, int NT, int* mblocks, int* dblocks) {
+  *mblocks = ((a.MT + NT - 1) / NT + 7) / 8;
+  *dblocks = ((a.DB + 3) / 4 + 3) / 4;
+  return a.B * a.S * *mblocks * *dblocks;
+}
+__device__ __forceinline__ WeightedPlace weighted_place(const TreeArgs& a, int NT, int i) {
+  const int mgroups = (a.MT + NT - 1) / NT, dgroups = (a.DB + 3) / 4;
+  int mblocks, dblocks;
+  const int units = weighted_units(a, NT, &mblocks, &dblocks);
+  const int mper = (mgroups + mblocks - 1) / mblocks, dper = (dgroups + dblocks - 1) / dblocks;
+  int unit, inner;
+  WeightedPlace p;
+  p.any = unit_of_workgroup(i, mper * dper, units, colocate_units(units), unit, inner);
+  const int block = unit % (mblocks * dblocks);
+  p.s = unit / (mblocks * dblocks) % a.S;
+  p.b = unit / (mblocks * dblocks) / a.S;
+  p.mg = block / dblocks * mper + inner / dper;
+  p.dg = block % dblocks * dper + inner % dper;
+  p.any = p.any && p.mg < mgroups && p.dg < dgroups;
+  return p;
+}
+
 template <int DT, int NT>
 __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   typedef Weighted<DT, NT> G;
@@ -388,12 +415,11 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   __shared__ u32x4 ring[2][SC * NT * 64];
   __shared__ float red[SUB][ROWS], fin[ROWS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-  const int mgroups = (a.MT + NT - 1) / NT, dgroups = (a.DB + 3) / 4;
-  int unit, mg;
-  if (!unit_of_workgroup(blockIdx.x, mgroups, a.B * a.S * dgroups, true, unit, mg)) return;
-  const int dg = unit % dgroups, block = dg * 4 + wave, s = unit / dgroups % a.S, b = unit / dgroups / a.S;
+  const WeightedPlace at = weighted_place(a, NT, blockIdx.x);
+  if (!at.any) return;
+  const int mg = at.mg, dg = at.dg, block = dg * 4 + wave, s = at.s, b = at.b;
   const int len = __builtin_amdgcn_readfirstlane(seq_len_of(a.seq_lens, b, a.T)), L = len + a.N;
-  const Share share = split_share(L, a.S, s, CH);
+  const Share share = split_share(a, L, s, CH);
   if (share.first >= share.end) return;
   const int c0 = share.first;
 
@@ -440,12 +466,12 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   {
     const int row = threadIdx.x % ROWS, sub = threadIdx.x / ROWS;
     const int b0 = c0 / CPB, b1 = (share.end - 1) / CPB + 1;
-    const size_t at = (size_t)b * a.NB * a.MT * 16 + min(mg * NT + row / 16, a.MT - 1) * 16 + row % 16;
+    const size_t first = (size_t)b * a.NB * a.MT * 16 + min(mg * NT + row / 16, a.MT - 1) * 16 + row % 16;
     const size_t pitch = (size_t)a.MT * 16;
     float top = NEG_INF;
     if (sub < SUB) {
 #pragma unroll 4
-      for (int blk = b0 + sub; blk < b1; blk += SUB) top = fmaxf(top, a.ref[at + blk * pitch]);
+      for (int blk = b0 + sub; blk < b1; blk += SUB) top = fmaxf(top, a.ref[first + blk * pitch]);
       red[sub][row] = top;
     }
     __syncthreads();
@@ -458,8 +484,8 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
       if (sub < SUB) {
 #pragma unroll 4
         for (int blk = b0 + sub; blk < b1; blk += SUB) {
-          const float r = a.ref[at + blk * pitch];
-          if (blk * CPB >= c0) l += a.lsum[at + blk * pitch] * (r == top ? 1.f : exp2_of(r - top));   // (a block's sum: with its first row)
+          const float r = a.ref[first + blk * pitch];
+          if (blk * CPB >= c0) l += a.lsum[first + blk * pitch] * (r == top ? 1.f : exp2_of(r - top));   // (a block's sum: with its first row)
         }
         red[sub][row] = l;
       }
@@ -614,7 +640,7 @@ __global__ __launch_bounds__(512) void tree_project_kernel(TreeArgs a) {
       const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
       nan = __shfl((anc & odd) != 0 ? 1 : 0, (t * 16 + n16) % a.N);
     }
-    const int ns = split_share(seq_len_of(a.seq_lens, b, a.T) + a.N, a.S, 0, 4 * VEC).splits;
+    const int ns = split_share(a, seq_len_of(a.seq_lens, b, a.T) + a.N, 0, 4 * VEC).splits;
     float top = NEG_INF, sum = 0.f;
     for (int s = 0; s < ns; ++s) top = fmaxf(top, a.sref[(((size_t)b * a.S + s) * a.MT + t) * 16 + e % 16]);
     for (int s = 0; s < ns; ++s) {
@@ -745,8 +771,10 @@ void launch_tree_scores_t(const TreeArgs& a, hipStream_t st) {
 
 template <int DT>
 void launch_tree_weighted_t(const TreeArgs& a, int nt, hipStream_t st) {
-  const int mgroups = (a.MT + nt - 1) / nt, units = a.B * a.S * ((a.DB + 3) / 4);
-  const dim3 grid((units + 7) / 8 * 8 * mgroups);
+  int mblocks, dblocks;
+  const int units = weighted_units(a, nt, &mblocks, &dblocks);
+  const int mper = ((a.MT + nt - 1) / nt + mblocks - 1) / mblocks, dper = ((a.DB + 3) / 4 + dblocks - 1) / dblocks;
+  const dim3 grid(unit_grid(units, mper * dper, colocate_units(units)));
   switch (nt) {
     case 1: hipLaunchKernelGGL((tree_weighted_kernel<DT, 1>), grid, dim3(256), 0, st, a); break;
     case 2: hipLaunchKernelGGL((tree_weighted_kernel<DT, 2>), grid, dim3(256), 0, st, a); break;
@@ -779,7 +807,7 @@ void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* splits
   *nt = each > 6 ? 8 : each > 4 ? 6 : each;
   const long wgs = (long)B * ((mt + *nt - 1) / *nt) * ((d + 4 * cw - 1) / (4 * cw));
   const int steps = (T + N + TREE_STEP - 1) / TREE_STEP;
-  *splits = (int)std::max(1l, std::min<long>({(256 + wgs - 1) / wgs, (steps + 3) / 4, TREE_MAX_SPLITS}));
+  *splits = (int)std::max(1l, std::min<long>({std::max(1l, 256 / wgs), (steps + 3) / 4, TREE_MAX_SPLITS}));
 }
 
 // Row splits of W_KV in the projection: until there is a workgroup for every compute unit, a block of rows for each wave at least.

@@ -217,7 +217,7 @@ void launch_xweighted(const float* S, const void* X, long x_bstride, const int32
 
 // ---- launches whose units of workgroups share what they read (unit_of_workgroup) -----------------------
 // Units dealt to the 8 XCDs (unit_of_workgroup): only when they spread evenly, within a quarter
-inline int colocate_units(int nunits) { return (nunits % 8 == 0 || nunits >= 32) ? 1 : 0; }
+__host__ __device__ inline int colocate_units(int nunits) { return (nunits % 8 == 0 || nunits >= 32) ? 1 : 0; }
 inline unsigned unit_grid(int nunits, int ninner, int colocate) {
   return colocate ? 8u * (unsigned)ninner * (unsigned)((nunits + 7) / 8) : (unsigned)nunits * (unsigned)ninner;
 }
