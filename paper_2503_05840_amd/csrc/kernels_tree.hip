@@ -25,6 +25,9 @@ template <> struct Elem<DT_F32> {
 constexpr int TREE_BLOCK = TREE_BLOCK_ROWS;      // rows that share a reference of the numerators
 constexpr float REF_STEP = 32.f;                 // references are multiples of this (log2 domain)
 
+__device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ float bf16_value(unsigned bits) { return __uint_as_float(bits << 16); }
+
 template <int DT>
 __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, f32x4 acc) {
   if constexpr (DT == DT_BF16) {
@@ -45,6 +48,27 @@ __device__ __forceinline__ uint64_t odd_keys(const TreeArgs& a, int b, int lane)
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) m |= (uint64_t)__shfl_xor((unsigned)m, k) | (uint64_t)__shfl_xor((unsigned)(m >> 32), k) << 32;
   return m;
+}
+
+// VEC consecutive columns of a row of C as the projection's operand, 64 lanes apart: in bf16 hi and lo, since W_KV = W_K^-1 W_V can make a rounding
+// of C larger
+template <int DT, int VEC = Elem<DT>::VEC>
+__device__ __forceinline__ void store_operand(const float (&v)[VEC], u32x4* out) {
+  u32x4 hi, lo;
+  if constexpr (DT == DT_BF16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned h1 = bf16_bits(v[2 * j]), h2 = bf16_bits(v[2 * j + 1]);
+      hi[j] = h1 | h2 << 16;
+      lo[j] = (unsigned)bf16_bits(v[2 * j] - bf16_value(h1)) | (unsigned)bf16_bits(v[2 * j + 1] - bf16_value(h2)) << 16;
+    }
+    out[0] = hi;
+    out[64] = lo;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) hi[j] = __float_as_uint(v[j]);
+    out[0] = hi;
+  }
 }
 
 // acc += a b, the accumulator staying where it is.  With as many accumulators as there are accumulation registers the compiler gives a product
@@ -116,8 +140,6 @@ __device__ __forceinline__ float max_over_groups(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-__device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-__device__ __forceinline__ float bf16_value(unsigned bits) { return __uint_as_float(bits << 16); }
 
 // A rotated piece of a key row (adjacent pairs, VEC / 2 of them; cs: their cos and sin).  bf16: the rotated values as hi + lo, so that
 // rounding them costs no accuracy that the stored keys have.
@@ -340,6 +362,198 @@ __global__ __launch_bounds__(1024 / TS) void tree_scores_kernel(TreeArgs a) {
   }
 }
 
+// ------------------------------------------------------------------------------------------------
+// The same for many rows: a workgroup of eight waves walks a range of 256-row blocks of one head, a wave 32 rows of each, with the
+// head's queries resident as operands (heads of up to four steps: 128 columns in bf16, 64 in fp32) and the next block's keys in flight
+// while this one's are scored.  One barrier a block, for the maxima; the sums of a block are put together behind the next one's, and its
+// numerators stored behind the wait for the next one's keys, which would else be a wait for them as well.  Blocks of context alone need
+// no mask.
+// ------------------------------------------------------------------------------------------------
+template <int DT, int MAXT>
+__global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, int per) {
+  constexpr int VEC = Elem<DT>::VEC, KW = 4 * VEC, WV = 8, TS = 2, KU = 4;
+  typedef typename Elem<DT>::T T;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x, b = blockIdx.z;
+  const int len = __builtin_amdgcn_readfirstlane(seq_len_of(a.seq_lens, b, a.T)), L = len + a.N;
+  const int blk0 = blockIdx.y * per, blk1 = min(blk0 + per, (L + TREE_BLOCK - 1) / TREE_BLOCK);
+  if (blk0 >= blk1) return;
+  __shared__ float red[2][2][WV][MAXT * 16];               // [block parity][maximum, sum]
+  __shared__ uint64_t odd[2][WV];
+  const int rp = a.banded ? a.d_k : a.d, nk = (a.d_k + KW - 1) / KW;
+  const T* K = (const T*)a.K + (size_t)b * a.k_bstride + piece_at(h * a.d_k, a.d_k, a.banded);
+  const int m0 = h * a.N, m1 = h + 1 == a.H ? a.MT * 16 : m0 + a.N;
+  const int tile0 = m0 / 16, ntiles = (m1 + 15) / 16 - tile0;
+
+  u32x4 kf[2][KU][TS];
+  auto load = [&](int blk, u32x4 (&to)[KU][TS]) {
+#pragma unroll
+    for (int ts = 0; ts < TS; ++ts) {
+      const int t = min(blk * TREE_BLOCK + (wave * TS + ts) * 16 + n16, L - 1);
+      const T* at = K + row_at(t, rp, a.d);
+#pragma unroll
+      for (int ku = 0; ku < KU; ++ku) {
+        const int j = ku * KW + g * VEC;
+        to[ku][ts] = *(const u32x4*)(at + (j < a.d_k ? j : 0));
+      }
+    }
+  };
+  load(blk0, kf[0]);
+  const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
+  u32x4 qf[MAXT][KU];
+  uint64_t see[MAXT];
+#pragma unroll
+  for (int mt = 0; mt < MAXT; ++mt) {
+    const int i = (tile0 + mt) * 16 + n16 - m0;
+    const bool mine = i >= 0 && i < a.N;
+    const T* q = (const T*)a.q + ((size_t)b * a.N + (mine ? i : 0)) * a.d + h * a.d_k;
+#pragma unroll
+    for (int ku = 0; ku < KU; ++ku) {
+      const int j = ku * KW + g * VEC;
+      qf[mt][ku] = *(const u32x4*)(q + (j < a.d_k ? j : 0));
+      if (!mine || j >= a.d_k) qf[mt][ku] = u32x4{0, 0, 0, 0};
+    }
+    const uint64_t own = __shfl((unsigned)anc, i & 63) | (uint64_t)__shfl((unsigned)(anc >> 32), i & 63) << 32;
+    see[mt] = mine ? own : 0;
+  }
+  // the sums, references and odd keys of a block whose waves are all past it
+  auto finish = [&](int blk, int par) {
+    for (int at = threadIdx.x; at < ntiles * 16; at += WV * 64) {
+      const int m = tile0 * 16 + at;
+      if (m < m0 || m >= m1) continue;
+      float l = red[par][1][0][at], top = red[par][0][0][at];
+#pragma unroll
+      for (int w = 1; w < WV; ++w) {
+        l += red[par][1][w][at];
+        top = fmaxf(top, red[par][0][w][at]);
+      }
+      const size_t to = ((size_t)b * a.NB + blk) * a.MT * 16 + m;
+      a.lsum[to] = l;
+      a.ref[to] = top == NEG_INF ? NEG_INF : REF_STEP * ceilf(top * (1.f / REF_STEP));
+    }
+    const int at = blk - len / TREE_BLOCK;
+    if (threadIdx.x == 0 && at >= 0) {
+      uint64_t any = 0;
+      for (int w = 0; w < WV; ++w) any |= odd[par][w];
+      a.odd[((size_t)b * 2 + at) * a.H + h] = any;
+      if (at == 0 && (L - 1) / TREE_BLOCK == blk) a.odd[((size_t)b * 2 + 1) * a.H + h] = 0;
+    }
+  };
+  constexpr int PF = TS * 16 / KW;
+  u32x4 pend[MAXT][PF];                                    // the last block's numerators
+  auto store = [&](int blk) {
+#pragma unroll
+    for (int mt = 0; mt < MAXT; ++mt) {
+      const int m = (tile0 + mt) * 16 + n16;
+      if (m < m0 || m >= m1) continue;
+      u32x4* P = (u32x4*)a.P + (((size_t)b * a.MT + tile0 + mt) * a.CT + (size_t)blk * (TREE_BLOCK / KW) + wave * PF) * 64 + lane;
+#pragma unroll
+      for (int f = 0; f < PF; ++f) P[f * 64] = pend[mt][f];
+    }
+  };
+  auto step = [&](int blk, auto I) {
+    const int par = I, t0 = blk * TREE_BLOCK + wave * 16 * TS;
+#pragma unroll
+    for (int ku = 0; ku < KU; ++ku)
+#pragma unroll
+      for (int ts = 0; ts < TS; ++ts) asm volatile("" : "+v"(kf[I][ku][ts]));      // (this block's keys are waited for here)
+    if (blk > blk0) store(blk - 1);
+    load(min(blk + 1, blk1 - 1), kf[1 - I]);
+    f32x4 acc[TS][MAXT];
+#pragma unroll
+    for (int ts = 0; ts < TS; ++ts)
+#pragma unroll
+      for (int mt = 0; mt < MAXT; ++mt) acc[ts][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const bool drafted = t0 + 16 * TS > len;               // (uniform) some rows are drafted ones, or past the end
+    bool bad[TS] = {};
+#pragma unroll
+    for (int ku = 0; ku < KU; ++ku) {
+      if (ku >= nk) break;
+      const int j = ku * KW + g * VEC;
+      const bool in = j < a.d_k;
+#pragma unroll
+      for (int ts = 0; ts < TS; ++ts) {
+        u32x4 kx = kf[I][ku][ts];
+        const int t = min(t0 + 16 * ts + n16, L - 1);
+        if (drafted) bad[ts] |= t >= len && not_finite<DT>(kx);
+        if (!in) kx = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int mt = 0; mt < MAXT; ++mt) {
+          acc[ts][mt] = mma<DT>(kx, qf[mt][ku], acc[ts][mt]);
+        }
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MAXT; ++mt) {
+      float mx = NEG_INF;
+#pragma unroll
+      for (int ts = 0; ts < TS; ++ts)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (drafted) {
+            const int j = t0 + 16 * ts + 4 * g + r - len;
+            if (j >= 0 && !(j < a.N && (see[mt] >> (j & 63) & 1))) acc[ts][mt][r] = NEG_INF;
+          }
+          mx = fmaxf(mx, acc[ts][mt][r]);
+        }
+      mx = max_over_groups(mx);
+      if (g == 0) red[par][0][wave][mt * 16 + n16] = see[mt] ? mx * a.qscale : NEG_INF;
+    }
+    if (drafted) {
+      uint64_t mask = 0;
+#pragma unroll
+      for (int ts = 0; ts < TS; ++ts) {
+        uint64_t m = __ballot(bad[ts]);
+        m = (m | m >> 16 | m >> 32 | m >> 48) & 0xffff;
+        const int at = t0 + 16 * ts - len;
+        mask |= at >= 64 || at <= -16 ? 0 : at >= 0 ? m << at : m >> -at;
+      }
+      if (lane == 0) odd[par][wave] = mask;
+    } else if (lane == 0) {
+      odd[par][wave] = 0;
+    }
+    lds_barrier();
+    if (blk > blk0) finish(blk - 1, 1 - par);
+#pragma unroll
+    for (int mt = 0; mt < MAXT; ++mt) {
+      const int at = mt * 16 + n16;
+      float top = red[par][0][0][at];
+#pragma unroll
+      for (int w = 1; w < WV; ++w) top = fmaxf(top, red[par][0][w][at]);
+      const float ref = REF_STEP * ceilf(top * (1.f / REF_STEP));
+      // (an unused slot: 2^-inf; nothing visible, or nothing but NaN: numerators of 0 or NaN)
+      const float sub = !see[mt] ? INFINITY : top == NEG_INF ? 0.f : ref;
+      u32x4 (&v)[PF] = pend[mt];
+      float l = 0.f;
+#pragma unroll
+      for (int ts = 0; ts < TS; ++ts) {
+        float p[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = exp2_of(fmaf(acc[ts][mt][r], a.qscale, -sub));
+        if constexpr (DT == DT_BF16) {
+          // (the weighted sum takes bf16 numerators; their sum is of the same values)
+          v[0][2 * ts] = (unsigned)bf16_bits(p[0]) | (unsigned)bf16_bits(p[1]) << 16;
+          v[0][2 * ts + 1] = (unsigned)bf16_bits(p[2]) | (unsigned)bf16_bits(p[3]) << 16;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) l += bf16_value(v[0][2 * ts + i] & 0xffffu) + __uint_as_float(v[0][2 * ts + i] & 0xffff0000u);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            v[ts][r] = __float_as_uint(p[r]);
+            l += p[r];
+          }
+        }
+      }
+      l = sum_over_row_groups(l);
+      if (g == 0) red[par][1][wave][at] = l;
+    }
+  };
+  for (int blk = blk0; blk < blk1; blk += 2) unrolled_steps<0, 2>(blk, blk1, step);
+  store(blk1 - 1);
+  lds_barrier();
+  finish(blk1 - 1, (blk1 - 1 - blk0) & 1);
+}
+
 // Chunks [first, end) of sequence b that split s sums, and how many splits have any: the same number of steps of 64 rows in every split of every
 // sequence (but its last), so that ragged batches are cut as evenly as others.
 constexpr int TREE_STEP = 64;
@@ -413,7 +627,7 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   constexpr int VEC = G::VEC, CW = 16 * VEC, CH = G::CH, SC = G::SC, PF = G::PF, KR = G::KR, UN = G::UN, CPB = TREE_BLOCK / CH, ROWS = NT * 16, SUB = 256 / ROWS;
   typedef typename Elem<DT>::T T;
   __shared__ u32x4 ring[2][SC * NT * 64];
-  __shared__ float red[SUB][ROWS], fin[ROWS];
+  __shared__ float red[SUB][ROWS], fin[ROWS], wrow[ROWS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
   const WeightedPlace at = weighted_place(a, NT, blockIdx.x);
   if (!at.any) return;
@@ -479,7 +693,8 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
     for (int i = 0; i < SUB; ++i) top = fmaxf(top, red[i][row]);
     if (sub == 0) fin[row] = top;
     __syncthreads();
-    if (dg == 0) {                                         // (the first column blocks' workgroups note them for the projection)
+    // (one split: its sum makes the weights; more: the first column blocks' workgroups note reference and sum for the merge)
+    if (a.S == 1 || dg == 0) {
       float l = 0.f;
       if (sub < SUB) {
 #pragma unroll 4
@@ -490,14 +705,15 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
         red[sub][row] = l;
       }
       __syncthreads();
-      const size_t to = (((size_t)b * a.S + s) * a.MT + mg * NT + row / 16) * 16 + row % 16;
       l = 0.f;
 #pragma unroll
       for (int i = 0; i < SUB; ++i) l += red[i][row];
-      if (sub == 0 && mg * NT + row / 16 < a.MT) {
+      if (a.S > 1 && sub == 0 && mg * NT + row / 16 < a.MT) {
+        const size_t to = (((size_t)b * a.S + s) * a.MT + mg * NT + row / 16) * 16 + row % 16;
         a.sref[to] = top;
         a.sl[to] = l;
       }
+      if (a.S == 1 && sub == 0) wrow[row] = l != 0.f ? 1.f / l : 0.f;
     }
   }
   f32x4 acc[VEC][NT];
@@ -595,125 +811,153 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
     for (int c = 0; c < VEC; ++c) asm volatile("" : "+a"(acc[c][nt]));      // (nothing reads them before that wait)
   // a lane has query row n16 of each tile and the columns 4 VEC g + VEC r + c of the block, which the projection reads as operands
   if (block >= a.DB) return;
+  uint64_t anc = 0;
+  if (odd && a.S == 1) anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     if (mg * NT + nt >= a.MT) continue;
     const size_t row = ((size_t)b * a.S + s) * a.MT + mg * NT + nt;
-    f32x4* C = (f32x4*)a.C + (row * a.DB + block) * VEC * 64 + lane;
+    if (a.S == 1) {
+      float w = wrow[nt * 16 + n16];
+      if (odd && __shfl((anc & odd) != 0 ? 1 : 0, ((mg * NT + nt) * 16 + n16) % a.N)) w = __builtin_nanf("");
+      u32x4* out = (u32x4*)a.Cop + (row * a.DB + block) * VEC * 64 + lane;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < 4; ++r) {
+        float v[VEC];
 #pragma unroll
-      for (int hf = 0; hf < VEC / 4; ++hf)
-        C[(r * (VEC / 4) + hf) * 64] = f32x4{acc[hf * 4][nt][r], acc[hf * 4 + 1][nt][r], acc[hf * 4 + 2][nt][r], acc[hf * 4 + 3][nt][r]};
+        for (int c = 0; c < VEC; ++c) v[c] = w == 0.f ? 0.f : acc[c][nt][r] * w;
+        store_operand<DT>(v, out + r * (VEC / 4) * 64);
+      }
+    } else {
+      f32x4* C = (f32x4*)a.C + (row * a.DB + block) * VEC * 64 + lane;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int hf = 0; hf < VEC / 4; ++hf)
+          C[(r * (VEC / 4) + hf) * 64] = f32x4{acc[hf * 4][nt][r], acc[hf * 4 + 1][nt][r], acc[hf * 4 + 2][nt][r], acc[hf * 4 + 3][nt][r]};
+    }
   }
 }
 
 // ------------------------------------------------------------------------------------------------
-// Merge of the splits and projection: out[i, h] = (sum_s w_s C_s[h N + i]) W_KV[:, h].  A workgroup of eight waves takes one head (or 16 VEC
-// columns of one), NM of the query tiles that hold rows of it (of any sequence) and a range of rows of W_KV, which the waves share out in
-// blocks of 16 VEC; their sums meet in LDS.  In bf16 C enters as hi + lo: W_KV = W_K^-1 W_V can make a rounding of C larger.
+// Merge of the splits: C = sum_s w_s C_s, w_s = 2^(ref_s - max) over the whole sum, into operands of the projection.  A workgroup takes one query
+// tile and `per` column blocks of it.  (The projection itself read a tile once for every head that has rows in it, every split of it: 1 x 2
+// nodes x 16384 x 32 x 128 54 us.)
+// ------------------------------------------------------------------------------------------------
+template <int DT>
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
+  constexpr int VEC = Elem<DT>::VEC;
+  const int lane = threadIdx.x & 63, n16 = lane & 15, r = threadIdx.x >> 6, tile = blockIdx.x, b = blockIdx.z;
+  __shared__ float weight[TREE_MAX_SPLITS][16];
+  const int ns = split_share(a, seq_len_of(a.seq_lens, b, a.T) + a.N, 0, 4 * VEC).splits;
+  if (r == 0) {
+    bool nan = false;                                      // (a node that sees a drafted key that is not finite)
+    if (const uint64_t odd = odd_keys(a, b, lane)) {
+      const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
+      nan = __shfl((anc & odd) != 0 ? 1 : 0, (tile * 16 + n16) % a.N);
+    }
+    const size_t at = ((size_t)b * a.S * a.MT + tile) * 16 + n16, pitch = (size_t)a.MT * 16;
+    float top = NEG_INF, sum = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < ns; ++s) top = fmaxf(top, a.sref[at + s * pitch]);
+#pragma unroll 4
+    for (int s = 0; s < ns; ++s) sum += a.sl[at + s * pitch] * (top == NEG_INF ? 1.f : exp2_of(a.sref[at + s * pitch] - top));
+    for (int s = lane >> 4; s < ns; s += 4) {
+      const float w = sum == 0.f ? 0.f : (top == NEG_INF ? 1.f : exp2_of(a.sref[at + s * pitch] - top)) / sum;
+      weight[s][n16] = nan ? __builtin_nanf("") : w;
+    }
+  }
+  lds_barrier();
+  const int end = min(a.DB, (int)(blockIdx.y + 1) * per);
+  for (int blk = blockIdx.y * per; blk < end; ++blk) {
+    const f32x4* C = (const f32x4*)a.C + (((size_t)b * a.S * a.MT + tile) * a.DB + blk) * VEC * 64 + r * (VEC / 4) * 64 + lane;
+    const size_t pitch = (size_t)a.MT * a.DB * VEC * 64;
+    float v[VEC] = {};
+#pragma unroll 4
+    for (int s = 0; s < ns; ++s) {
+      const float w = weight[s][n16];
+#pragma unroll
+      for (int hf = 0; hf < VEC / 4; ++hf) {
+        const f32x4 x = C[s * pitch + hf * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[hf * 4 + j] += w == 0.f ? 0.f : x[j] * w;      // (0: a row without weight, whose sum may be anything)
+      }
+    }
+    store_operand<DT>(v, (u32x4*)a.Cop + (((size_t)b * a.MT + tile) * a.DB + blk) * VEC * 64 + r * (VEC / 4) * 64 + lane);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Projection: out[i, h] = C[h N + i] W_KV[:, h].  A workgroup of four waves, one per SIMD, takes one head (or 16 VEC columns of one), NM of the query
+// tiles that hold rows of it (of any sequence) and a range of rows of W_KV, which the waves share out 4 VEC at a time; what they load lies
+// RD turns ahead in registers, and their sums meet in LDS.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int NM>
-__global__ __launch_bounds__(512) void tree_project_kernel(TreeArgs a) {
-  constexpr int VEC = Elem<DT>::VEC, CW = 16 * VEC, PITCH = CW + 4;
+__global__ __launch_bounds__(256, 1) void tree_project_kernel(TreeArgs a) {
+  constexpr int VEC = Elem<DT>::VEC, CW = 16 * VEC, PITCH = CW + 4, OPS = VEC / 4, RD = NM == 4 ? 2 : 4;
   typedef typename Elem<DT>::T T;
-  __shared__ float weight[NM * TREE_MAX_SPLITS * 16];      // [tile][split][row]
-  __shared__ __align__(16) float sums[8 * 16 * PITCH];     // [wave][row][column]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
+  __shared__ __align__(16) float sums[4 * 16 * PITCH];     // [wave][row][column]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
   const int cblocks = (a.d_k + CW - 1) / CW;               // column blocks of a head
   const int cs = blockIdx.x % a.csw, hc = blockIdx.x / a.csw, h = hc / cblocks, cb = hc % cblocks;
   const int tile0 = h * a.N / 16, ntiles = (h * a.N + a.N - 1) / 16 - tile0 + 1;
   const int x0 = blockIdx.y * NM;
   if (x0 >= a.B * ntiles) return;
   int tb[NM], tt[NM];
+  const u32x4* C[NM];
 #pragma unroll
   for (int i = 0; i < NM; ++i) {
     const int x = min(x0 + i, a.B * ntiles - 1);
     tb[i] = x / ntiles;
     tt[i] = tile0 + x % ntiles;
+    C[i] = (const u32x4*)a.Cop + ((size_t)tb[i] * a.MT + tt[i]) * a.DB * VEC * 64 + lane;
   }
-  // weights of the splits: 2^(ref_s - max) over the whole sum; 0 where a split or a row has nothing (its C may be unwritten)
-  if (wave < NM) {
-    const int i = wave, e = i * 16 + n16, x = min(x0 + i, a.B * ntiles - 1), b = x / ntiles, t = tile0 + x % ntiles;
-    bool nan = false;                                      // (a node that sees a drafted key that is not finite)
-    if (const uint64_t odd = odd_keys(a, b, lane)) {
-      const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
-      nan = __shfl((anc & odd) != 0 ? 1 : 0, (t * 16 + n16) % a.N);
-    }
-    const int ns = split_share(a, seq_len_of(a.seq_lens, b, a.T) + a.N, 0, 4 * VEC).splits;
-    float top = NEG_INF, sum = 0.f;
-    for (int s = 0; s < ns; ++s) top = fmaxf(top, a.sref[(((size_t)b * a.S + s) * a.MT + t) * 16 + e % 16]);
-    for (int s = 0; s < ns; ++s) {
-      const size_t at = (((size_t)b * a.S + s) * a.MT + t) * 16 + e % 16;
-      sum += a.sl[at] * (top == NEG_INF ? 1.f : exp2_of(a.sref[at] - top));
-    }
-    for (int s = 0; s < a.S; ++s) {
-      float w = 0.f;
-      if (s < ns && sum != 0.f) w = (top == NEG_INF ? 1.f : exp2_of(a.sref[(((size_t)b * a.S + s) * a.MT + t) * 16 + e % 16] - top)) / sum;
-      weight[(i * a.S + s) * 16 + e % 16] = nan ? __builtin_nanf("") : w;
-    }
-  }
-  lds_barrier();
   const int hcol = cb * CW + n16 * VEC;                    // column of the head that the lane loads
-  const bool in = hcol < a.d_k;
-  const T* W = (const T*)a.W + h * a.d_k + (in ? hcol : 0);
+  const T* W = (const T*)a.W + h * a.d_k + (hcol < a.d_k ? hcol : 0);
+  const int turns = a.DB * 4, per = (turns + a.csw * 4 - 1) / (a.csw * 4) * 4, first = cs * per + wave, end = min(turns, cs * per + per);
+  u32x4 w[RD][VEC], c[RD][NM][OPS];
+  auto load = [&](int turn, u32x4 (&wr)[VEC], u32x4 (&cr)[NM][OPS]) {
+    const int t = min(turn, turns - 1);
+    const int row = t / 4 * CW + 4 * VEC * g + VEC * (t % 4);      // of W_KV, column of C
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) wr[j] = *(const u32x4*)(W + (size_t)((row < a.d ? row : 0) + j) * a.d);   // (d is whole pieces)
+#pragma unroll
+    for (int i = 0; i < NM; ++i)
+#pragma unroll
+      for (int o = 0; o < OPS; ++o) cr[i][o] = C[i][(size_t)t * OPS * 64 + o * 64];
+  };
   f32x4 acc[NM][VEC];
 #pragma unroll
   for (int i = 0; i < NM; ++i)
 #pragma unroll
-    for (int c = 0; c < VEC; ++c) acc[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int per = (a.DB + a.csw - 1) / a.csw, first = cs * per, end = min(a.DB, first + per);
-  for (int blk = first + wave; blk < end; blk += 8) {
+    for (int k = 0; k < VEC; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = blk * CW + 4 * VEC * g + VEC * r;    // of W_KV, column of C
-      u32x4 w[VEC], wt[VEC];
-      const bool there = row < a.d;                        // (d is whole pieces)
+  for (int i = 0; i < RD; ++i) load(first + 4 * i, w[i], c[i]);
+  auto step = [&](int n, auto I) {
+    const int t = first + 4 * n;
+    const bool there = t / 4 * CW + 4 * VEC * g + VEC * (t % 4) < a.d;
+    u32x4 wt[VEC], x[NM][OPS];
+    transpose<DT>(w[I], wt);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        w[j] = *(const u32x4*)(W + (size_t)((there ? row : 0) + j) * a.d);
-        if (!there) w[j] = u32x4{0, 0, 0, 0};
-      }
-      transpose<DT>(w, wt);
+    for (int i = 0; i < NM; ++i)
 #pragma unroll
-      for (int i = 0; i < NM; ++i) {
-        float c[VEC];
+      for (int o = 0; o < OPS; ++o) x[i][o] = there ? c[I][i][o] : u32x4{0, 0, 0, 0};      // (columns past C's end may hold anything)
+    load(t + 4 * RD, w[I], c[I]);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) c[j] = 0.f;
-        for (int s = 0; s < a.S; ++s) {
-          const float f = weight[(i * a.S + s) * 16 + n16];
-          const f32x4* C = (const f32x4*)a.C + ((((size_t)tb[i] * a.S + s) * a.MT + tt[i]) * a.DB + blk) * VEC * 64 + lane;
+    for (int i = 0; i < NM; ++i)
 #pragma unroll
-          for (int hf = 0; hf < VEC / 4; ++hf) {
-            const f32x4 v = C[(r * (VEC / 4) + hf) * 64];
+      for (int o = 0; o < OPS; ++o)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) c[hf * 4 + j] += f == 0.f || !there ? 0.f : v[j] * f;
-          }
-        }
-        if constexpr (DT == DT_BF16) {
-          u32x4 hi, lo;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const unsigned h1 = bf16_bits(c[2 * j]), h2 = bf16_bits(c[2 * j + 1]);
-            hi[j] = h1 | h2 << 16;
-            lo[j] = (unsigned)bf16_bits(c[2 * j] - bf16_value(h1)) | (unsigned)bf16_bits(c[2 * j + 1] - bf16_value(h2)) << 16;
-          }
-#pragma unroll
-          for (int cc = 0; cc < VEC; ++cc) acc[i][cc] = mma<DT>(wt[cc], lo, mma<DT>(wt[cc], hi, acc[i][cc]));
-        } else {
-          u32x4 v;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(c[j]);
-#pragma unroll
-          for (int cc = 0; cc < VEC; ++cc) acc[i][cc] = mma<DT>(wt[cc], v, acc[i][cc]);
-        }
-      }
-    }
-  }
+        for (int k = 0; k < VEC; ++k) acc[i][k] = mma<DT>(wt[k], x[i][o], acc[i][k]);
+  };
+  const int nsteps = (end - first + 3) / 4;
+  int n = 0;
+  for (; n + RD <= nsteps; n += RD) full_steps<0, RD>(n, step);
+  unrolled_steps<0, RD>(n, nsteps, step);
 #pragma unroll
   for (int i = 0; i < NM; ++i) {
     if (x0 + i >= a.B * ntiles) break;
-    // (a lane has query row n16 and the columns VEC (4 g + r) + c)
+    // (a lane has query row n16 and the columns VEC (4 g + r) + k)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -721,12 +965,12 @@ __global__ __launch_bounds__(512) void tree_project_kernel(TreeArgs a) {
         *(f32x4*)(sums + (wave * 16 + n16) * PITCH + VEC * (4 * g + r) + hf * 4) =
             f32x4{acc[i][hf * 4][r], acc[i][hf * 4 + 1][r], acc[i][hf * 4 + 2][r], acc[i][hf * 4 + 3][r]};
     lds_barrier();
-    for (int e = threadIdx.x; e < 16 * CW / 4; e += 512) {
+    for (int e = threadIdx.x; e < 16 * CW / 4; e += 256) {
       const int row = e / (CW / 4), c4 = e % (CW / 4) * 4, m = tt[i] * 16 + row;
       if (m / a.N == h && cb * CW + c4 < a.d_k) {
         f32x4 v = *(const f32x4*)(sums + row * PITCH + c4);
 #pragma unroll
-        for (int w = 1; w < 8; ++w) v += *(const f32x4*)(sums + (w * 16 + row) * PITCH + c4);
+        for (int w = 1; w < 4; ++w) v += *(const f32x4*)(sums + (w * 16 + row) * PITCH + c4);
         const size_t node = (size_t)tb[i] * a.N + m % a.N;
         const int at = h * a.d_k + cb * CW + c4;
         if (a.csw > 1) {
@@ -756,17 +1000,44 @@ __global__ __launch_bounds__(256) void tree_sum_kernel(const float* part, int cs
     ((f32x4*)out)[i] = v;
 }
 
+// Tiles of 16 query rows that a head's rows can lie in at most: they begin at multiples of the common divisor of N and 16.
+int tree_head_tiles(int N) {
+  int div = 16;
+  while (N % div) div /= 2;
+  return (16 - div + N + 15) / 16;
+}
+// Query tiles that a workgroup of the projection takes together.
+int tree_project_tiles(long tiles) { return tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4; }
+
 template <int DT, bool ROPE, int TS>
 void launch_tree_scores_s(const TreeArgs& a, hipStream_t st) {
   const dim3 grid(a.H, a.NB, a.B), block(1024 / TS);
   if (a.N <= 17) hipLaunchKernelGGL((tree_scores_kernel<DT, ROPE, TS, 2>), grid, block, 0, st, a);      // (a head's rows touch two tiles at most)
   else hipLaunchKernelGGL((tree_scores_kernel<DT, ROPE, TS, 5>), grid, block, 0, st, a);
 }
+template <int DT, bool ROPE>
+void launch_tree_scores_r(const TreeArgs& a, hipStream_t st) {
+  const long blocks = (long)a.H * a.NB * a.B;
+  if (blocks <= 512) return launch_tree_scores_s<DT, ROPE, 1>(a, st);     // few workgroups: more waves of fewer rows
+  // The walk where its four steps of a row are all used, there is no rotation to wait for, and a round of workgroups holds every head: 8 x 64
+  // nodes x 4096 x 32 x 128 175 -> 105 us, 4 ragged x 32 x 8000 86 -> 62, 1 x 2 x 16384 40 -> 31; but heads of 64 columns 34 -> 38 (16 x 21 x
+  // 1504 x 20), rotary ones 72 -> 100 (8 x 16 x 5000 x 24 x 96), 384 heads in a batch 112 -> 119 (24 x 5 x 6000 x 16 x 128).
+  constexpr int W = 16 * Elem<DT>::VEC;
+  const int tiles = tree_head_tiles(a.N);
+  if (ROPE || a.d_k > W || a.d_k <= W * 3 / 4 || tiles > 4 || a.H * a.B > 256) return launch_tree_scores_s<DT, ROPE, 4>(a, st);
+  const int z = std::min(a.NB, 256 / (a.H * a.B)), per = (a.NB + z - 1) / z;
+  const dim3 grid(a.H, (a.NB + per - 1) / per, a.B);
+  switch (tiles) {
+    case 1: hipLaunchKernelGGL((tree_scores_stream_kernel<DT, 1>), grid, dim3(512), 0, st, a, per); break;
+    case 2: hipLaunchKernelGGL((tree_scores_stream_kernel<DT, 2>), grid, dim3(512), 0, st, a, per); break;
+    case 3: hipLaunchKernelGGL((tree_scores_stream_kernel<DT, 3>), grid, dim3(512), 0, st, a, per); break;
+    default: hipLaunchKernelGGL((tree_scores_stream_kernel<DT, 4>), grid, dim3(512), 0, st, a, per); break;
+  }
+}
 template <int DT>
 void launch_tree_scores_t(const TreeArgs& a, hipStream_t st) {
-  const bool few = (long)a.H * a.NB * a.B <= 512;          // few workgroups: more waves of fewer rows
-  if (a.rope) few ? launch_tree_scores_s<DT, true, 1>(a, st) : launch_tree_scores_s<DT, true, 4>(a, st);
-  else few ? launch_tree_scores_s<DT, false, 1>(a, st) : launch_tree_scores_s<DT, false, 4>(a, st);
+  if (a.rope) launch_tree_scores_r<DT, true>(a, st);
+  else launch_tree_scores_r<DT, false>(a, st);
 }
 
 template <int DT>
@@ -786,12 +1057,19 @@ void launch_tree_weighted_t(const TreeArgs& a, int nt, hipStream_t st) {
 }
 
 template <int DT>
+void launch_tree_merge_t(const TreeArgs& a, hipStream_t st) {
+  const int per = (int)std::max(1l, (long)a.B * a.MT * a.DB / 2048);
+  hipLaunchKernelGGL(tree_merge_kernel<DT>, dim3(a.MT, (a.DB + per - 1) / per, a.B), dim3(256), 0, st, a, per);
+}
+
+template <int DT>
 void launch_tree_project_t(const TreeArgs& a, hipStream_t st) {
   constexpr int CW = 16 * Elem<DT>::VEC;
-  const int heads = a.H * ((a.d_k + CW - 1) / CW);
-  const int tiles = a.B * ((a.N + 14) / 16 + 1);
-  if (tiles > 2) hipLaunchKernelGGL((tree_project_kernel<DT, 4>), dim3(heads * a.csw, (tiles + 3) / 4), dim3(512), 0, st, a);
-  else hipLaunchKernelGGL((tree_project_kernel<DT, 1>), dim3(heads * a.csw, tiles), dim3(512), 0, st, a);
+  const int heads = a.H * ((a.d_k + CW - 1) / CW), tiles = a.B * tree_head_tiles(a.N), nm = tree_project_tiles(tiles);
+  const dim3 grid(heads * a.csw, (tiles + nm - 1) / nm), block(256);
+  if (nm == 1) hipLaunchKernelGGL((tree_project_kernel<DT, 1>), grid, block, 0, st, a);
+  else if (nm == 2) hipLaunchKernelGGL((tree_project_kernel<DT, 2>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((tree_project_kernel<DT, 4>), grid, block, 0, st, a);
   if (a.csw > 1) {
     const size_t n4 = (size_t)a.B * a.N * a.d / 4;
     hipLaunchKernelGGL(tree_sum_kernel<DT>, dim3((n4 + 255) / 256), dim3(256), 0, st, a.part, a.csw, n4, a.out);
@@ -810,11 +1088,11 @@ void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* splits
   *splits = (int)std::max(1l, std::min<long>({std::max(1l, 256 / wgs), (steps + 3) / 4, TREE_MAX_SPLITS}));
 }
 
-// Row splits of W_KV in the projection: until there is a workgroup for every compute unit, a block of rows for each wave at least.
+// Row splits of W_KV in the projection: until there is a workgroup for every compute unit, a turn for each wave at least.
 int tree_row_splits(int dtype, int B, int N, int H, int d) {
   const int cw = 16 * vec_elems(dtype), d_k = d / H, db = (d + cw - 1) / cw;
-  const long tiles = (long)B * ((N + 14) / 16 + 1), wgs = (long)H * ((d_k + cw - 1) / cw) * (tiles > 2 ? (tiles + 3) / 4 : tiles);
-  return (int)std::max(1l, std::min<long>({(256 + wgs - 1) / wgs, (db + 7) / 8, 16}));
+  const long tiles = (long)B * tree_head_tiles(N), nm = tree_project_tiles(tiles), wgs = (long)H * ((d_k + cw - 1) / cw) * ((tiles + nm - 1) / nm);
+  return (int)std::max(1l, std::min<long>({(256 + wgs - 1) / wgs, db, 16}));
 }
 
 void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st) {
@@ -824,6 +1102,10 @@ void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st) {
 void launch_tree_weighted(int dtype, const TreeArgs& a, hipStream_t st) {
   if (dtype == DT_BF16) launch_tree_weighted_t<DT_BF16>(a, a.NT, st);
   else launch_tree_weighted_t<DT_F32>(a, a.NT, st);
+}
+void launch_tree_merge(int dtype, const TreeArgs& a, hipStream_t st) {
+  if (dtype == DT_BF16) launch_tree_merge_t<DT_BF16>(a, st);
+  else launch_tree_merge_t<DT_F32>(a, st);
 }
 void launch_tree_project(int dtype, const TreeArgs& a, hipStream_t st) {
   if (dtype == DT_BF16) launch_tree_project_t<DT_BF16>(a, st);

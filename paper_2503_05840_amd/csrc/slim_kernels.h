@@ -256,7 +256,8 @@ struct TreeArgs {
   int MT, CT, NB, DB, S, csw, NT;            // query tiles, fragments of a tile, row blocks, column blocks, context splits, row splits of W, tiles of a wave
   void* P;                                   // [B][MT][CT] fragments: numerators
   float *ref, *lsum;                         // [B][NB][MT * 16]: reference and sum of a block's numerators
-  float* C;                                  // [B][S][MT][DB] blocks of 16 rows x 16 VEC columns: weighted sums
+  float* C;                                  // [B][S][MT][DB] blocks of 16 rows x 16 VEC columns: weighted sums, S > 1
+  void* Cop;                                 // [B][MT][DB] the same divided by the softmax sums, as operands of the projection
   float *sref, *sl;                          // [B][S][MT * 16]
   uint64_t* odd;                             // [B][2][H]: drafted keys that are not finite in a head's columns (bit j: node j)
   float* part;                               // [csw][B][N][d], csw > 1
@@ -265,6 +266,7 @@ void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* splits
 int tree_row_splits(int dtype, int B, int N, int H, int d);
 void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st);
 void launch_tree_weighted(int dtype, const TreeArgs& a, hipStream_t st);
+void launch_tree_merge(int dtype, const TreeArgs& a, hipStream_t st);
 void launch_tree_project(int dtype, const TreeArgs& a, hipStream_t st);
 
 struct VerifyArgs {
