@@ -8,17 +8,24 @@ namespace slim {
 namespace {
 
 constexpr int VW = 16;                       // waves of a verifying workgroup
+constexpr int RUN = 4;                       // pieces of 16 bytes that a thread takes at most where the next token is looked for
 
 template <int DT> struct Prob;
 template <> struct Prob<DT_F32> {
   static constexpr int VEC = 4;
   typedef float T;
   static __device__ __forceinline__ float value(float x) { return x; }
+  static __device__ __forceinline__ float get(const u32x4& x, int j) { return __uint_as_float(x[j]); }
+  static __device__ __forceinline__ void clear(u32x4& x, int j) { x[j] = 0; }
+  static __device__ __forceinline__ void set(u32x4& x, int j, float v) { x[j] = __float_as_uint(v); }
 };
 template <> struct Prob<DT_BF16> {
   static constexpr int VEC = 8;
   typedef uint16_t T;
   static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float((unsigned)x << 16); }
+  static __device__ __forceinline__ float get(const u32x4& x, int j) { return __uint_as_float(j & 1 ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16); }
+  static __device__ __forceinline__ void clear(u32x4& x, int j) { x[j >> 1] &= j & 1 ? 0xffffu : 0xffff0000u; }
+  static __device__ __forceinline__ void set(u32x4& x, int j, uint16_t v) { x[j >> 1] |= (unsigned)v << (j & 1 ? 16 : 0); }
 };
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -27,171 +34,323 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
-// Sum over the workgroup, the same bits in every thread.
-__device__ double group_sum(double v, double* red) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  v = wave_sum(v);
-  if (lane == 0) red[wave] = v;
-  __syncthreads();
-  double s = 0;
+// What is left of a node's distribution: max(p - a q, 0) with a draft, p without the excluded tokens else.  The rows are read in pieces of 16 bytes
+// on 16-byte boundaries (p and draft are aligned, so a row of p and its row of the draft begin alike): the first may begin with `skip` elements of the
+// row before, which count as 0, and what does not fill the last is read one by one.
+template <int DT, bool DRAFT>
+struct Residual {
+  typedef Prob<DT> E;
+  typedef typename E::T T;
+  static constexpr int VEC = E::VEC, U = DRAFT ? 4 : 8;     // pieces of each that a lane has in flight
+  const T *p, *q;                            // the row's first piece
+  int skip, V, full, pieces;                 // whole pieces, all pieces
+  double am;
+  int lane, tok;                             // excluded: tokens of the lanes in `out`
+  uint64_t out, near;                        // near: bit piece / 64 % 64 of every excluded one
+
+  __device__ Residual(const VerifyArgs& a, int b, int node, double am_, uint64_t out_, int tok_) : am(am_), tok(tok_), out(out_), near(0) {
+    const size_t at = ((size_t)b * a.N + node) * a.V;
+    lane = threadIdx.x & 63;
+    skip = (int)(at % VEC);
+    V = a.V;
+    p = (const T*)a.p + at - skip;
+    q = DRAFT ? (const T*)a.draft + at - skip : nullptr;
+    full = (skip + V) / VEC;
+    pieces = (skip + V + VEC - 1) / VEC;
+    if constexpr (!DRAFT)
+      for (uint64_t m = out; m; m &= m - 1) near |= 1ull << (__builtin_amdgcn_readlane(tok, __ffsll((unsigned long long)m) - 1) + skip) / VEC / 64 % 64;
+  }
+  __device__ __forceinline__ void mask(int k, u32x4& x, u32x4& y) const {
+    if (k == 0) {
 #pragma unroll
-  for (int w = 0; w < VW; ++w) s += red[w];
+      for (int j = 0; j < VEC; ++j)
+        if (j < skip) {
+          E::clear(x, j);
+          E::clear(y, j);
+        }
+    }
+    if constexpr (!DRAFT) {
+      if (near >> (k / 64 % 64) & 1)
+        for (uint64_t m = out; m; m &= m - 1) {
+          const int v = __builtin_amdgcn_readlane(tok, __ffsll((unsigned long long)m) - 1) + skip - k * VEC;
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if (j == v) E::clear(x, j);
+        }
+    }
+  }
+  template <bool USEQ>
+  __device__ __forceinline__ double value(const u32x4& x, const u32x4& y, int j) const {
+    if constexpr (USEQ) return fmax((double)E::get(x, j) - am * (double)E::get(y, j), 0.0);
+    else return (double)E::get(x, j);
+  }
+  // piece k of the two rows, zeros past the end
+  template <bool USEQ>
+  __device__ __forceinline__ void piece(int k, u32x4& x, u32x4& y) const {
+    x = y = u32x4{0, 0, 0, 0};
+    if (k < full) {
+      x = ((const u32x4*)p)[k];
+      if constexpr (USEQ) y = ((const u32x4*)q)[k];
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        if (k * VEC + j < skip + V) {
+          E::set(x, j, p[k * VEC + j]);
+          if constexpr (USEQ) E::set(y, j, q[k * VEC + j]);
+        }
+    }
+    mask(k, x, y);
+  }
+  // sum over the pieces [ka, kb), the same in every lane of the wave
+  template <bool USEQ>
+  __device__ double sum(int ka, int kb) const {
+    const int fb = min(kb, full);
+    double s = 0;
+    for (int k = ka; k < fb; k += 64 * U) {
+      u32x4 x[U], y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = min(k + u * 64 + lane, fb - 1);
+        x[u] = ((const u32x4*)p)[at];
+        if constexpr (USEQ) y[u] = ((const u32x4*)q)[at];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = k + u * 64 + lane;
+        if (at >= fb) break;
+        mask(at, x[u], y[u]);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s += value<USEQ>(x[u], y[u], j);
+      }
+    }
+    if (kb > full && ka <= full && lane == 0) {
+      u32x4 x, y;
+      piece<USEQ>(full, x, y);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) s += value<USEQ>(x, y, j);
+    }
+    return wave_sum(s);
+  }
+};
+
+// The pieces [k0, k1) in VW parts, one a wave; their sums into part[].  Returns the whole sum.
+template <bool USEQ, class R>
+__device__ double sum_parts(const R& r, int k0, int k1, double* part) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = (k1 - k0 + VW - 1) / VW, ka = k0 + wave * per;
+  const double s = ka < k1 ? r.template sum<USEQ>(ka, min(k1, ka + per)) : 0.0;
+  __syncthreads();                           // (what part[] held has been read)
+  if (r.lane == 0) part[wave] = s;
   __syncthreads();
-  return s;
+  double all = 0;
+#pragma unroll
+  for (int w = 0; w < VW; ++w) all += part[w];
+  return all;
+}
+
+// The lowest token whose running sum is over u times the whole sum, or the last with any weight where there is none; -1 where nothing has weight.
+// The sums of a pass over the row say which of VW parts holds it; a part of up to 1024 RUN pieces (a vocabulary of 262144 in fp32, 524288 in bf16) is then scanned,
+// a few pieces a thread, a larger one is summed in parts again.
+template <bool USEQ, class R>
+__device__ int draw(const R& r, double u, double* part) {
+  constexpr int VEC = R::VEC;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int k0 = 0, k1 = r.pieces;
+  double run = 0, border = 0;
+  for (bool first = true;; first = false) {
+    const double all = sum_parts<USEQ>(r, k0, k1, part);
+    if (first) {
+      if (!(all > 0)) return -1;
+      border = u * all;
+    }
+    const int per = (k1 - k0 + VW - 1) / VW;
+    int at = -1, with = 0;
+    double before = run, acc = run;
+    for (int w = 0; w < VW; ++w) {
+      const double s = part[w];
+      if (s > 0 && at < 0) {
+        with = w;
+        before = acc;
+        if (acc + s > border) at = w;
+      }
+      acc += s;
+    }
+    if (at < 0) at = with;                   // (rounding, or u = 1: the last part with any weight)
+    run = before;
+    const int lo = k0 + at * per;
+    k1 = min(k1, lo + per);
+    k0 = lo;
+    if (k1 - k0 <= VW * 64 * RUN) break;
+  }
+  // a thread's neighbouring pieces, the running sum before and after them
+  const int each = (k1 - k0 + VW * 64 - 1) / (VW * 64);
+  u32x4 x[RUN], y[RUN];
+  double own = 0;
+#pragma unroll
+  for (int i = 0; i < RUN; ++i) {
+    const int k = k0 + tid * each + i;
+    x[i] = y[i] = u32x4{0, 0, 0, 0};
+    if (i < each && k < k1) r.template piece<USEQ>(k, x[i], y[i]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) own += r.template value<USEQ>(x[i], y[i], j);
+  }
+  double incl = own;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const double o = __shfl_up(incl, k);
+    if (lane >= k) incl += o;
+  }
+  double excl = __shfl_up(incl, 1);
+  if (lane == 0) excl = 0;
+  __syncthreads();
+  if (lane == 63) part[wave] = incl;
+  __syncthreads();
+  double base = run;
+  for (int w = 0; w < wave; ++w) base += part[w];
+  incl += base;
+  excl += base;
+  // the first thread over the border, the last with any weight; of the one that counts, the token
+  __shared__ int over[VW], any[VW], found;
+  const unsigned long long mo = __ballot(own > 0 && incl > border), ma = __ballot(own > 0);
+  if (lane == 0) {
+    over[wave] = mo ? wave * 64 + __ffsll(mo) - 1 : VW * 64;
+    any[wave] = ma ? wave * 64 + 63 - __clzll(ma) : -1;
+  }
+  __syncthreads();
+  int to = VW * 64, ta = -1;
+#pragma unroll
+  for (int w = 0; w < VW; ++w) {
+    to = min(to, over[w]);
+    ta = max(ta, any[w]);
+  }
+  if (tid == (to < VW * 64 ? to : ta)) {
+    int hit = -1, last = 0;
+    double s = excl;
+#pragma unroll
+    for (int i = 0; i < RUN; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const double v = r.template value<USEQ>(x[i], y[i], j);
+        const int at = (k0 + tid * each + i) * VEC + j - r.skip;
+        s += v;
+        if (v > 0) {
+          last = at;
+          if (hit < 0 && s > border) hit = at;
+        }
+      }
+    found = hit >= 0 ? hit : last;
+  }
+  __syncthreads();
+  return found;
 }
 
 // ------------------------------------------------------------------------------------------------
 // One workgroup per sequence.  After k rejections at a node the residual distribution is max(p - a_k q, 0) / F(a_k) with F(a) = sum max(p - a q, 0),
 // a_0 = 0, F(a_0) = 1 and a_{k+1} = a_k + F(a_k): one scalar stands for the chain of residual vectors, and only F of the last one needs
-// a pass over the vocabulary.  Every product and sum in 64 bits.
+// a pass over the vocabulary.  Every product and sum in 64 bits.  A node is a lane of every wave, which has asked for the node's p and q
+// before the walk begins, so that the walk itself reads registers.
 // ------------------------------------------------------------------------------------------------
 template <int DT, bool DRAFT>
 __global__ __launch_bounds__(VW * 64) void tree_verify_kernel(VerifyArgs a) {
   typedef Prob<DT> E;
   typedef typename E::T T;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  __shared__ int tok[TREE_MAX_NODES], par[TREE_MAX_NODES], out[TREE_MAX_NODES];
-  __shared__ float un[TREE_MAX_NODES];
-  __shared__ double red[VW], before[VW];
-  __shared__ int found[VW];
-  if (tid < a.N) {
-    tok[tid] = a.tokens[(size_t)b * a.N + tid];
-    par[tid] = a.parents[(size_t)b * a.N + tid];
-    un[tid] = a.u[(size_t)b * a.N + tid];
+  typedef Residual<DT, DRAFT> R;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  __shared__ double part[VW];
+  const size_t mine = (size_t)b * a.N + min(lane, a.N - 1);
+  const int tok = a.tokens[mine], par = a.parents[mine];
+  const float un = a.u[mine];
+  const bool there = lane > 0 && lane < a.N && par >= 0 && par < lane && tok >= 0 && tok < a.V;
+  float pn = 0.f, qn = 0.f;
+  if (there) {
+    const size_t at = ((size_t)b * a.N + par) * a.V + tok;
+    pn = E::value(((const T*)a.p)[at]);
+    if constexpr (DRAFT) qn = E::value(((const T*)a.draft)[at]);
   }
-  __syncthreads();
-  const T* P = (const T*)a.p + (size_t)b * a.N * a.V;
-  const T* Q = DRAFT ? (const T*)a.draft + (size_t)b * a.N * a.V : nullptr;
-  int cur = 0, n = 1, nout = 0;
+  auto of = [](float v, int i) { return (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), i)); };
+  int cur = 0;
+  uint64_t path = 1, out = 0;
   double am = 0.0, F = 1.0;
   bool have = true;                          // whether F is that of am
-  if (tid == 0) a.path[(size_t)b * a.N] = 0;
-  for (int i = 1; i < a.N; ++i) {
-    const int x = tok[i];
-    if (par[i] != cur || x < 0 || x >= a.V) continue;
-    const double px = E::value(P[(size_t)cur * a.V + x]);
+  for (uint64_t next = __ballot(there && par == 0); next;) {
+    const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)next) - 1);
+    next &= next - 1;
+    const double px = of(pn, i), ui = of(un, i);
     bool yes;
     if constexpr (DRAFT) {
-      const double qx = E::value(Q[(size_t)cur * a.V + x]);
+      const double qx = of(qn, i);
       if (!have) {
-        double s = 0;
-        for (int v = tid; v < a.V; v += VW * 64)
-          s += fmax((double)E::value(P[(size_t)cur * a.V + v]) - am * (double)E::value(Q[(size_t)cur * a.V + v]), 0.0);
-        F = group_sum(s, red);
+        const R r(a, b, cur, am, 0, tok);
+        F = sum_parts<true>(r, 0, r.pieces, part);
         have = true;
       }
-      yes = (double)un[i] * F * qx < px - am * qx;
+      yes = ui * F * qx < px - am * qx;
       if (!yes) {
         am += F;
         have = false;
       }
     } else {
-      double left = px;
-      for (int k = 0; k < nout; ++k) left = out[k] == x ? 0.0 : left;
-      yes = (double)un[i] * F < left;
+      const bool gone = __any((out >> lane & 1) && tok == __builtin_amdgcn_readlane(tok, i));
+      const double left = gone ? 0.0 : px;
+      yes = ui * F < left;
       if (!yes) {
         F -= left;
-        __syncthreads();
-        if (tid == 0) out[nout] = x;
-        ++nout;
-        __syncthreads();
+        out |= 1ull << i;
       }
     }
     if (yes) {
-      if (tid == 0) a.path[(size_t)b * a.N + n] = i;
-      ++n;
+      path |= 1ull << i;
       cur = i;
       am = 0.0;
       F = 1.0;
       have = true;
-      nout = 0;
+      out = 0;
+      next = __ballot(there && par == i);
     }
   }
-  for (int i = n + tid; i < a.N; i += VW * 64) a.path[(size_t)b * a.N + i] = -1;
-  if (tid == 0) a.n_path[b] = n;
-
-  // the next token: the waves have neighbouring stretches of the vocabulary, sum them, and the wave whose stretch holds the border looks for it
-  const T* Pc = P + (size_t)cur * a.V;
-  const T* Qc = DRAFT ? Q + (size_t)cur * a.V : nullptr;
-  auto residual = [&](int v) -> double {
-    const double pv = E::value(Pc[v]);
-    if constexpr (DRAFT) return am == 0.0 ? pv : fmax(pv - am * (double)E::value(Qc[v]), 0.0);
-    for (int k = 0; k < nout; ++k)
-      if (out[k] == v) return 0.0;
-    return pv;
-  };
-  const int per = (a.V + VW - 1) / VW, v0 = wave * per, v1 = min(a.V, v0 + per);
-  double s = 0;
-  for (int v = v0 + lane; v < v1; v += 64) s += residual(v);
-  s = wave_sum(s);
-  if (lane == 0) red[wave] = s;
-  __syncthreads();
-  double total = 0, mine = 0;
-  for (int w = 0; w < VW; ++w) {
-    if (w == wave) mine = total;
-    total += red[w];
+  const int n = __popcll(path);
+  if (tid < 64) {
+    if (path >> lane & 1) a.path[(size_t)b * a.N + __popcll(path & ((1ull << lane) - 1))] = lane;
+    if (lane >= n && lane < a.N) a.path[(size_t)b * a.N + lane] = -1;
+    if (lane == 0) a.n_path[b] = n;
   }
-  const double border = (double)un[0] * total;
-  // first token past the border in the own stretch; the last one with any weight stands in where rounding leaves none
-  int hit = 0x7fffffff, last = -1;
-  if (total > 0 && mine + s > border && mine <= border) {
-    double run = mine;
-    for (int v = v0; v < v1 && hit == 0x7fffffff; v += 64) {
-      const int at = v + lane;
-      double r = at < v1 ? residual(at) : 0.0;
-#pragma unroll
-      for (int k = 1; k < 64; k <<= 1) {
-        const double o = __shfl_up(r, k);
-        if (lane >= k) r += o;
-      }
-      const unsigned long long over = __ballot(at < v1 && run + r > border);
-      if (over) hit = v + __ffsll(over) - 1;
-      run += __shfl(r, 63);
-    }
-  }
-  __shared__ int hits[VW];
-  if (lane == 0) hits[wave] = hit;
-  __syncthreads();
-  hit = 0x7fffffff;
-  for (int w = 0; w < VW; ++w) hit = min(hit, hits[w]);
-  if (hit == 0x7fffffff) {
-    // nothing past the border: the last token with any weight, or, where nothing has any, the likeliest of the target's
+  const R r(a, b, cur, am, out, tok);
+  const double u0 = of(un, 0);
+  int hit;
+  if (DRAFT && am != 0.0) hit = draw<DRAFT>(r, u0, part);
+  else hit = draw<false>(r, u0, part);
+  if (hit < 0) {
+    // nothing has any weight: the likeliest of the target's, lowest first
+    const T* row = (const T*)a.p + ((size_t)b * a.N + cur) * a.V;
     float top = -1.f;
     int arg = 0x7fffffff;
     for (int v = tid; v < a.V; v += VW * 64) {
-      if (residual(v) > 0) last = v;
-      const float pv = E::value(Pc[v]);
+      const float pv = E::value(row[v]);
       if (pv > top) {
         top = pv;
         arg = v;
       }
     }
+    __shared__ float tops[VW];
+    __shared__ int args[VW];
+    auto take = [&](float t, int v) {
+      if (t > top || (t == top && v < arg)) {
+        top = t;
+        arg = v;
+      }
+    };
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) {
-      last = max(last, __shfl_xor(last, k));
-      const float t2 = __shfl_xor(top, k);
-      const int a2 = __shfl_xor(arg, k);
-      if (t2 > top || (t2 == top && a2 < arg)) {
-        top = t2;
-        arg = a2;
-      }
+      const float t = __shfl_xor(top, k);
+      const int v = __shfl_xor(arg, k);
+      take(t, v);
     }
-    __shared__ float tops[VW];
-    __shared__ int args[VW], lasts[VW];
     if (lane == 0) {
-      tops[wave] = top;
-      args[wave] = arg;
-      lasts[wave] = last;
+      tops[tid >> 6] = top;
+      args[tid >> 6] = arg;
     }
     __syncthreads();
-    for (int w = 0; w < VW; ++w) {
-      last = max(last, lasts[w]);
-      if (tops[w] > top || (tops[w] == top && args[w] < arg)) {
-        top = tops[w];
-        arg = args[w];
-      }
-    }
-    hit = total > 0 && last >= 0 ? last : arg == 0x7fffffff ? 0 : arg;
+    for (int w = 0; w < VW; ++w) take(tops[w], args[w]);
+    hit = arg == 0x7fffffff ? 0 : arg;
   }
   if (tid == 0) a.next[b] = hit;
 }
@@ -212,11 +371,19 @@ __global__ __launch_bounds__(1024) void tree_commit_kernel(u32x4* K, long bstrid
   __syncthreads();
   if (threadIdx.x == 0) new_lens[b] = len + n;
   const int rp = banded ? head_pieces : pieces;
+  constexpr int AHEAD = 8;
+  auto moves = [&](int j) { return j < n && from[j] > j && from[j] < N; };      // (else in place already, or no slot)
   for (int piece = threadIdx.x; piece < pieces; piece += blockDim.x) {
     u32x4* base = K + (size_t)b * bstride + (banded ? piece / head_pieces * (32 * head_pieces) + piece % head_pieces : piece);
     auto row = [&](int t) { return base + (size_t)(t >> 5) * 32 * pieces + (size_t)(t & 31) * rp; };
-    for (int j = 0; j < n; ++j)
-      if (from[j] > j && from[j] < N) *row(len + j) = *row(len + from[j]);      // (else in place already, or no slot)
+    for (int j = 0; j < n; j += AHEAD) {
+      u32x4 x[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) x[i] = *row(len + (moves(j + i) ? from[j + i] : 0));
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (moves(j + i)) *row(len + j + i) = x[i];
+    }
   }
 }
 
