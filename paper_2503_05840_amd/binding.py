@@ -376,9 +376,9 @@ def vanilla_attention_block(x, W_Q, W_K, W_V, W_O, Kcache, Vcache, y, B, H, T, d
 
 # ---- a tree of drafted tokens ----------------------------------------------------------------
 def _tree_ptr(t, shape, dtype):
-    """The address of a contiguous device tensor of exactly this shape and type (N rows a sequence are easily confused)."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"expected {tuple(shape)} {dtype}, got {tuple(t.shape)} {t.dtype}")
+    """The address of a contiguous device tensor of exactly this shape (a tuple) and type (N rows a sequence are easily confused)."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"expected {shape} {dtype}, got {tuple(t.shape)} {t.dtype}")
     return _dev_ptr(t)
 
 

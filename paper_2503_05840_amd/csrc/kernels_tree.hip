@@ -569,7 +569,7 @@ __device__ __forceinline__ float lower_by(float ref, float fin) { return fin == 
 template <int DT>
 __device__ __forceinline__ u32x4 lowered(u32x4 p, float e) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  const unsigned by = DT == DT_BF16 ? ((unsigned)e << 7) * 0x10001u : (unsigned)e << 23;
+  const unsigned n = (unsigned)e, by = DT == DT_BF16 ? n << 7 | n << 23 : n << 23;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const unsigned x = p[i];                               // (a bit cast of the element itself takes element 0)
@@ -621,6 +621,14 @@ __device__ __forceinline__ WeightedPlace weighted_place(const TreeArgs& a, int N
   return p;
 }
 
+template <int PART, int N, class I, class F>
+__device__ __forceinline__ void every_part(int st, I i, F& f) {
+  if constexpr (PART < N) {
+    f(st, i, std::integral_constant<int, PART>{});
+    every_part<PART + 1, N>(st, i, f);
+  }
+}
+
 template <int DT, int NT>
 __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   typedef Weighted<DT, NT> G;
@@ -643,12 +651,16 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   unsigned voff[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) voff[j] = (unsigned)(piece + slot_row(g, j) * rp) * sizeof(T);
-  const u32x4* pp[PF];
+  // (addresses of loads: a uniform pointer and 32 bits of a lane)
+  const char *pp[PF], *rfp[PF];
 #pragma unroll
   for (int i = 0; i < PF; ++i) {
-    const int f = min(wave + 4 * i, SC * NT - 1);          // (the last wave may bring a fragment twice)
-    pp[i] = (const u32x4*)a.P + (((size_t)b * a.MT + min(mg * NT + f / SC, a.MT - 1)) * a.CT + f % SC) * 64;
+    const int f = min(wave + 4 * i, SC * NT - 1), tile = min(mg * NT + f / SC, a.MT - 1);      // (the last wave may bring a fragment twice)
+    pp[i] = (const char*)a.P + (((size_t)b * a.MT + tile) * a.CT + f % SC) * 1024;
+    rfp[i] = (const char*)(a.ref + ((size_t)b * a.NB * a.MT + tile) * 16);
   }
+  const unsigned lane16 = lane * 16, row4 = n16 * 4;
+  const size_t ref_pitch = (size_t)a.MT * 64;
   // drafted keys that are not finite: the steps that hold drafted ones are taken one by one behind the others
   const uint64_t odd = odd_keys(a, b, lane);
   const int cend = __builtin_amdgcn_readfirstlane(odd ? min(share.end, max(c0, len / TREE_STEP * SC)) : share.end), nsteps = (cend - c0 + SC - 1) / SC;
@@ -656,24 +668,28 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   u32x4 k[KR][VEC], kt[2][VEC], pr[PF];
   float rr[PF];
   // (rows past the cache's end: its last row, whose numerators there are 0)
-  auto load_row = [&](int i, int j) {
+  const char* kp = nullptr;                                // the chunk that is loaded
+  unsigned lim = 0;
+  auto load_chunk = [&](int i) {
     const int chunk = min(c0 + i, cend - 1);
-    const unsigned lim = (unsigned)(piece + min(L - 1 - chunk * CH, CH - 1) * rp) * sizeof(T);
-    return *(const u32x4*)((const char*)(K + row_at(chunk * CH, rp, a.d)) + min(voff[j], lim));
+    kp = (const char*)(K + row_at(chunk * CH, rp, a.d));
+    lim = (unsigned)(piece + min(L - 1 - chunk * CH, CH - 1) * rp) * sizeof(T);
   };
-  auto frag_row = [&](int i) { return min(mg * NT + min(wave + 4 * i, SC * NT - 1) / SC, a.MT - 1) * 16 + n16; };
+  auto load_row = [&](int j) { return *(const u32x4*)(kp + min(voff[j], lim)); };
   auto load_p = [&](int step, int i) {
     const int chunk = c0 + min(step, nsteps - 1) * SC;
-    pr[i] = pp[i][(size_t)chunk * 64 + lane];
-    rr[i] = a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + frag_row(i)];
+    pr[i] = *(const u32x4*)(pp[i] + (size_t)chunk * 1024 + lane16);
+    rr[i] = *(const float*)(rfp[i] + chunk / CPB * ref_pitch + row4);
   };
   if (nsteps > 0) {
 #pragma unroll
     for (int i = 0; i < PF; ++i) load_p(0, i);
 #pragma unroll
-    for (int i = 0; i < KR; ++i)
+    for (int i = 0; i < KR; ++i) {
+      load_chunk(i);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) k[i][j] = load_row(i, j);
+      for (int j = 0; j < VEC; ++j) k[i][j] = load_row(j);
+    }
   }
 
   // the split's reference and sum of every row
@@ -725,7 +741,11 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   float fr[PF];
 #pragma unroll
   for (int i = 0; i < PF; ++i) fr[i] = fin[min(wave + 4 * i, SC * NT - 1) / SC * 16 + n16];
-  u32x4 pf[2];
+  // Operands of the tiles to come: read AHEAD tiles early
+  constexpr int TILES = SC * NT, AHEAD = TILES > 2 ? 2 : 1, PQ = TILES == 2 ? 2 : TILES % 3 == 0 ? 3 : 4;
+  static_assert(TILES % PQ == 0, "");
+  u32x4 pf[PQ];
+  auto fragment = [](int at) constexpr { return at % NT * SC + at / NT; };
   if (nsteps > 0) {
 #pragma unroll
     for (int i = 0; i < PF; ++i) {
@@ -733,51 +753,50 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
       load_p(1, i);
     }
     transpose<DT>(k[0], kt[0]);
+    load_chunk(KR);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) k[0][j] = load_row(KR, j);
+    for (int j = 0; j < VEC; ++j) k[0][j] = load_row(j);
     lds_barrier();
-    pf[0] = ring[0][lane];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) pf[i] = ring[0][fragment(i) * 64 + lane];
   }
-  // One step: its products, and between them, an instruction or two behind each, what the next ones need -- the next chunk's keys transposed, those of
-  // the chunk KR later requested into their registers, the next step's numerators parked and those of the step after requested.  Each
-  // tile's operand is read a tile ahead; before the last tile the waves meet, so that the next step's first can be.
-  auto step = [&](int st, auto I) {
-#pragma unroll
-    for (int c = 0; c < SC; ++c) {
-      u32x4 (&next)[VEC] = k[(I * SC + c + 1) % KR], (&ktn)[VEC] = kt[(c + 1) & 1];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int at = c * NT + nt;                        // of SC NT tiles
-        if (at + 1 < SC * NT) {
-          pf[(at + 1) & 1] = ring[st & 1][((nt + 1) % NT * SC + (nt + 1) / NT + c) * 64 + lane];
-        } else {
-          lds_barrier();
-          pf[(at + 1) & 1] = ring[st + 1 & 1][lane];
-        }
-        operands_ready();
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int cc = 0; cc < VEC; ++cc) {
-          mma_in_place<DT>(kt[c & 1][cc], pf[at & 1], acc[cc][nt]);
-#pragma unroll
-          for (int jp = 4 * nt / NT; jp < 4 * (nt + 1) / NT; ++jp) {
-            transpose_one<DT>(next, ktn, jp, cc);
-            if (cc == VEC - 1) {
-#pragma unroll
-              for (int j = jp * VEC / 4; j < (jp + 1) * VEC / 4; ++j) next[j] = load_row(st * SC + c + 1 + KR, j);
-            }
-          }
-#pragma unroll
-          for (int i = PF * at / (SC * NT - 1); i < PF * (at + 1) / (SC * NT - 1) && i < PF; ++i) {     // (before the last tile)
-            if (cc == 0) pr[i] = lowered<DT>(pr[i], lower_by(rr[i], fr[i]));
-            if (cc == VEC / 2) ring[st + 1 & 1][min(wave + 4 * i, SC * NT - 1) * 64 + lane] = pr[i];
-            if (cc == VEC - 1) load_p(st + 2, i);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+  // One step: its products, and between them, an instruction or three behind each -- what fits beside a product of 16 cycles --, what the next
+  // ones need: the next chunk's keys transposed, those of the chunk KR later requested into their registers, the next step's numerators parked and
+  // those of the step after requested.  A tile's operand is read AHEAD tiles early; AHEAD tiles before the end the waves meet, so that the next
+  // step's first can be.
+  // the PART-th of the places of a step: product CC of its tile AT
+  auto place = [&](int st, auto I, auto PART) __attribute__((always_inline)) {
+    constexpr int at = PART / VEC, cc = PART % VEC, c = at / NT, nt = at % NT;
+    u32x4 (&next)[VEC] = k[(I * SC + c + 1) % KR], (&ktn)[VEC] = kt[(c + 1) & 1];
+    if constexpr (cc == 0) {
+      if constexpr (at == TILES - AHEAD) lds_barrier();
+      if constexpr (at + AHEAD < TILES) pf[(at + AHEAD) % PQ] = ring[st & 1][fragment(at + AHEAD) * 64 + lane];
+      else pf[(at + AHEAD) % PQ] = ring[st + 1 & 1][fragment(at + AHEAD - TILES) * 64 + lane];
+      operands_ready();
+      __builtin_amdgcn_sched_barrier(0);
     }
+    mma_in_place<DT>(kt[c & 1][cc], pf[at % PQ], acc[cc][nt]);
+    if constexpr (nt == 0 && cc == 0) load_chunk(st * SC + c + 1 + KR);
+    // of this tile: row groups [j0, j1) of the next chunk, transposed in the first `slots` places, their registers filled again in the others
+    constexpr int j0 = 4 * nt / NT, n = 4 * (nt + 1) / NT - j0, slots = n <= 1 ? VEC / 2 : n <= 2 ? VEC * 3 / 4 : VEC, rows = n * VEC / 4;
+    if constexpr (cc < slots) {
+#pragma unroll
+      for (int t = n * VEC * cc / slots; t < n * VEC * (cc + 1) / slots; ++t) transpose_one<DT>(next, ktn, j0 + t / VEC, t % VEC);
+    }
+#pragma unroll
+    for (int r = 0; r < rows; ++r)
+      if (cc == (slots < VEC ? slots + r * (VEC - slots) / rows : VEC - 1)) next[j0 * VEC / 4 + r] = load_row(j0 * VEC / 4 + r);
+    // fragments parked beside this tile
+    constexpr int i0 = PF * at / (TILES - AHEAD), i1 = at < TILES - AHEAD ? PF * (at + 1) / (TILES - AHEAD) : i0;
+#pragma unroll
+    for (int i = i0; i < i1; ++i) {
+      if constexpr (cc == 0) pr[i] = lowered<DT>(pr[i], lower_by(rr[i], fr[i]));
+      if constexpr (cc == VEC / 2) ring[st + 1 & 1][min(wave + 4 * i, TILES - 1) * 64 + lane] = pr[i];
+      if constexpr (cc == VEC - 1) load_p(st + 2, i);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
+  auto step = [&](int st, auto I) __attribute__((always_inline)) { every_part<0, TILES * VEC>(st, I, place); };
   int st = 0;
   for (; st + UN <= nsteps; st += UN) full_steps<0, UN>(st, step);
   unrolled_steps<0, UN>(st, nsteps, step);
