@@ -6,6 +6,7 @@
 #include "device_common.h"
 
 #include <algorithm>
+#include <climits>
 
 namespace slim {
 namespace {
@@ -129,6 +130,54 @@ __device__ __forceinline__ uint64_t ancestors(const int32_t* parents, int N, int
   return bad ? 0 : anc;
 }
 
+// How the sequences share the slots of the weighted sum: the fewest steps of 64 rows a slot that leave enough of them (ragged batches: 8 sequences of 600
+// to 5000 rows in 16 slots take 27 steps, where as many slots for each take 40).  By one wave, which has up to four sequences a lane.
+__device__ void plan_splits(const TreeArgs& a, int lane) {
+  int steps[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int b = i * 64 + lane;
+    steps[i] = b < a.B ? (seq_len_of(a.seq_lens, b, a.T) + a.N + TREE_STEP_ROWS - 1) / TREE_STEP_ROWS : 0;
+  }
+  auto total = [](int v) {
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) v += __shfl_xor(v, k);
+    return v;
+  };
+  int lo = a.per_min, hi = (a.T + a.N + TREE_STEP_ROWS - 1) / TREE_STEP_ROWS;      // (as many a slot as the longest may have: B slots)
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += (steps[i] + mid - 1) / mid;
+    if (total(n) <= a.slots) hi = mid;
+    else lo = mid + 1;
+  }
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = (steps[i] + lo - 1) / lo;
+    int upto = n;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const int o = __shfl_up(upto, k);
+      if (lane >= k) upto += o;
+    }
+    const int b = i * 64 + lane, first = at + upto - n;
+    if (b < a.B) {
+      a.plan[1 + a.slots + b] = first * 2 * TREE_MAX_SPLITS + n;
+      for (int s = 0; s < n; ++s) a.plan[1 + first + s] = b * TREE_MAX_SPLITS + s;
+    }
+    at += __shfl(upto, 63);
+  }
+  for (int i = at + lane; i < a.slots; i += 64) a.plan[1 + i] = -1;
+  if (lane == 0) a.plan[0] = lo;
+}
+// (called by every workgroup of the scores' launch)
+__device__ __forceinline__ void plan_once(const TreeArgs& a, int lane, int wave) {
+  if (a.slots > a.B && wave == 0 && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) plan_splits(a, lane);
+}
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // max / sum over the four lanes that share lane % 16, the same in all four
@@ -192,6 +241,7 @@ __global__ __launch_bounds__(1024 / TS) void tree_scores_kernel(TreeArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.x, blk = blockIdx.y, b = blockIdx.z;
   const int len = __builtin_amdgcn_readfirstlane(seq_len_of(a.seq_lens, b, a.T)), L = len + a.N;
+  plan_once(a, lane, wave);
   if (blk * TREE_BLOCK >= L) return;
   __shared__ float red[2][WV][MAXT * 16];
   __shared__ uint64_t odd[WV];
@@ -377,6 +427,7 @@ __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, 
   const int h = blockIdx.x, b = blockIdx.z;
   const int len = __builtin_amdgcn_readfirstlane(seq_len_of(a.seq_lens, b, a.T)), L = len + a.N;
   const int blk0 = blockIdx.y * per, blk1 = min(blk0 + per, (L + TREE_BLOCK - 1) / TREE_BLOCK);
+  plan_once(a, lane, wave);
   if (blk0 >= blk1) return;
   __shared__ float red[2][2][WV][MAXT * 16];               // [block parity][maximum, sum]
   __shared__ uint64_t odd[2][WV];
@@ -554,13 +605,12 @@ __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, 
   finish(blk1 - 1, (blk1 - 1 - blk0) & 1);
 }
 
-// Chunks [first, end) of sequence b that split s sums, and how many splits have any: the same number of steps of 64 rows in every split of every
-// sequence (but its last), so that ragged batches are cut as evenly as others.
-constexpr int TREE_STEP = 64;
-struct Share { int first, end, splits; };
-__device__ __forceinline__ Share split_share(const TreeArgs& a, int L, int s, int ch) {
-  const int all = (a.T + a.N + TREE_STEP - 1) / TREE_STEP, per = (all + a.S - 1) / a.S, steps = (L + TREE_STEP - 1) / TREE_STEP;
-  return {min(steps, s * per) * (TREE_STEP / ch), min(min(steps, (s + 1) * per) * (TREE_STEP / ch), (L + ch - 1) / ch), (steps + per - 1) / per};
+// Chunks [first, end) of a sequence of L rows that its split s sums, `per` steps of 64 rows each.
+constexpr int TREE_STEP = TREE_STEP_ROWS;
+struct Share { int first, end; };
+__device__ __forceinline__ Share split_share(int L, int s, int per, int ch) {
+  const int steps = (L + TREE_STEP - 1) / TREE_STEP;
+  return {min(steps, s * per) * (TREE_STEP / ch), min(min(steps, (s + 1) * per) * (TREE_STEP / ch), (L + ch - 1) / ch)};
 }
 
 // Numerators times 2^-e, e >= 0 a whole number: e off their exponents, down to 0.  (They are >= 0; one that is NaN is no longer, but then its row's
@@ -596,13 +646,14 @@ template <int DT, int NT> struct Weighted {
 };
 
 // Workgroup i -> its query tiles (mg), column blocks (dg), split and sequence.  An XCD's workgroups at one time share rows of K (same dg) and
-// numerators (same mg) through its L2: it gets blocks of up to 8 mg x 4 dg.  Four neighbouring dg are 4 KB of every row, all channels of
-// the L2 where rows are a multiple of that long; the 16 mg x 2 dg of before drew on a quarter of them.
-struct WeightedPlace { bool any; int mg, dg, s, b; };
+// numerators (same mg) through its L2: it gets blocks of up to 8 mg x 6 dg.  Four neighbouring dg are 4 KB of every row, all channels of
+// the L2 where rows are a multiple of that long; the 16 mg x 2 dg of before drew on a quarter of them.  An XCD gets every eighth unit: the blocks
+// of a slot turn on by what that passes, or blocks of unlike size would always be the same XCDs'.
+struct WeightedPlace { bool any; int mg, dg, slot; };
 __host__ __device__ __forceinline__ int weighted_units(const TreeArgs& a, int NT, int* mblocks, int* dblocks) {
   *mblocks = ((a.MT + NT - 1) / NT + 7) / 8;
-  *dblocks = ((a.DB + 3) / 4 + 3) / 4;
-  return a.B * a.S * *mblocks * *dblocks;
+  *dblocks = ((a.DB + 3) / 4 + 5) / 6;
+  return a.slots * *mblocks * *dblocks;
 }
 __device__ __forceinline__ WeightedPlace weighted_place(const TreeArgs& a, int NT, int i) {
   const int mgroups = (a.MT + NT - 1) / NT, dgroups = (a.DB + 3) / 4;
@@ -612,9 +663,9 @@ __device__ __forceinline__ WeightedPlace weighted_place(const TreeArgs& a, int N
   int unit, inner;
   WeightedPlace p;
   p.any = unit_of_workgroup(i, mper * dper, units, colocate_units(units), unit, inner);
-  const int block = unit % (mblocks * dblocks);
-  p.s = unit / (mblocks * dblocks) % a.S;
-  p.b = unit / (mblocks * dblocks) / a.S;
+  const int blocks = mblocks * dblocks;
+  p.slot = unit / blocks;
+  const int block = (unit + p.slot * blocks / 8) % blocks;
   p.mg = block / dblocks * mper + inner / dper;
   p.dg = block % dblocks * dper + inner % dper;
   p.any = p.any && p.mg < mgroups && p.dg < dgroups;
@@ -639,9 +690,18 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
   const WeightedPlace at = weighted_place(a, NT, blockIdx.x);
   if (!at.any) return;
-  const int mg = at.mg, dg = at.dg, block = dg * 4 + wave, s = at.s, b = at.b;
+  const int mg = at.mg, dg = at.dg, block = dg * 4 + wave;
+  const bool whole = a.slots == a.B;                       // a sequence each
+  int b = at.slot, s = 0, per = INT_MAX / TREE_STEP;
+  if (!whole) {
+    const int entry = __builtin_amdgcn_readfirstlane(a.plan[1 + at.slot]);
+    if (entry < 0) return;                                 // (a slot that no sequence needs)
+    b = entry / TREE_MAX_SPLITS;
+    s = entry % TREE_MAX_SPLITS;
+    per = __builtin_amdgcn_readfirstlane(a.plan[0]);
+  }
   const int len = __builtin_amdgcn_readfirstlane(seq_len_of(a.seq_lens, b, a.T)), L = len + a.N;
-  const Share share = split_share(a, L, s, CH);
+  const Share share = split_share(L, s, per, CH);
   if (share.first >= share.end) return;
   const int c0 = share.first;
 
@@ -710,7 +770,7 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
     if (sub == 0) fin[row] = top;
     __syncthreads();
     // (one split: its sum makes the weights; more: the first column blocks' workgroups note reference and sum for the merge)
-    if (a.S == 1 || dg == 0) {
+    if (whole || dg == 0) {
       float l = 0.f;
       if (sub < SUB) {
 #pragma unroll 4
@@ -724,12 +784,12 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
       l = 0.f;
 #pragma unroll
       for (int i = 0; i < SUB; ++i) l += red[i][row];
-      if (a.S > 1 && sub == 0 && mg * NT + row / 16 < a.MT) {
-        const size_t to = (((size_t)b * a.S + s) * a.MT + mg * NT + row / 16) * 16 + row % 16;
+      if (!whole && sub == 0 && mg * NT + row / 16 < a.MT) {
+        const size_t to = ((size_t)at.slot * a.MT + mg * NT + row / 16) * 16 + row % 16;
         a.sref[to] = top;
         a.sl[to] = l;
       }
-      if (a.S == 1 && sub == 0) wrow[row] = l != 0.f ? 1.f / l : 0.f;
+      if (whole && sub == 0) wrow[row] = l != 0.f ? 1.f / l : 0.f;
     }
   }
   f32x4 acc[VEC][NT];
@@ -831,12 +891,12 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
   // a lane has query row n16 of each tile and the columns 4 VEC g + VEC r + c of the block, which the projection reads as operands
   if (block >= a.DB) return;
   uint64_t anc = 0;
-  if (odd && a.S == 1) anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
+  if (odd && whole) anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     if (mg * NT + nt >= a.MT) continue;
-    const size_t row = ((size_t)b * a.S + s) * a.MT + mg * NT + nt;
-    if (a.S == 1) {
+    const size_t row = (size_t)at.slot * a.MT + mg * NT + nt;
+    if (whole) {
       float w = wrow[nt * 16 + n16];
       if (odd && __shfl((anc & odd) != 0 ? 1 : 0, ((mg * NT + nt) * 16 + n16) % a.N)) w = __builtin_nanf("");
       u32x4* out = (u32x4*)a.Cop + (row * a.DB + block) * VEC * 64 + lane;
@@ -868,14 +928,14 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
   constexpr int VEC = Elem<DT>::VEC;
   const int lane = threadIdx.x & 63, n16 = lane & 15, r = threadIdx.x >> 6, tile = blockIdx.x, b = blockIdx.z;
   __shared__ float weight[TREE_MAX_SPLITS][16];
-  const int ns = split_share(a, seq_len_of(a.seq_lens, b, a.T) + a.N, 0, 4 * VEC).splits;
+  const int entry = a.plan[1 + a.slots + b], slot0 = entry / (2 * TREE_MAX_SPLITS), ns = entry % (2 * TREE_MAX_SPLITS);
   if (r == 0) {
     bool nan = false;                                      // (a node that sees a drafted key that is not finite)
     if (const uint64_t odd = odd_keys(a, b, lane)) {
       const uint64_t anc = ancestors(a.parents + (size_t)b * a.N, a.N, lane);
       nan = __shfl((anc & odd) != 0 ? 1 : 0, (tile * 16 + n16) % a.N);
     }
-    const size_t at = ((size_t)b * a.S * a.MT + tile) * 16 + n16, pitch = (size_t)a.MT * 16;
+    const size_t at = ((size_t)slot0 * a.MT + tile) * 16 + n16, pitch = (size_t)a.MT * 16;
     float top = NEG_INF, sum = 0.f;
 #pragma unroll 4
     for (int s = 0; s < ns; ++s) top = fmaxf(top, a.sref[at + s * pitch]);
@@ -889,7 +949,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
   lds_barrier();
   const int end = min(a.DB, (int)(blockIdx.y + 1) * per);
   for (int blk = blockIdx.y * per; blk < end; ++blk) {
-    const f32x4* C = (const f32x4*)a.C + (((size_t)b * a.S * a.MT + tile) * a.DB + blk) * VEC * 64 + r * (VEC / 4) * 64 + lane;
+    const f32x4* C = (const f32x4*)a.C + (((size_t)slot0 * a.MT + tile) * a.DB + blk) * VEC * 64 + r * (VEC / 4) * 64 + lane;
     const size_t pitch = (size_t)a.MT * a.DB * VEC * 64;
     float v[VEC] = {};
 #pragma unroll 4
@@ -1097,14 +1157,21 @@ void launch_tree_project_t(const TreeArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// How the weighted sum is cut: NT query tiles of 16 rows to a wave, S splits of the context.  The fewest tiles of the sizes that
-// there are in the fewest groups of eight at most; splits until there is a workgroup for every compute unit, a step of rows each at least.
-void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* splits) {
+// How the weighted sum is cut: NT query tiles of 16 rows to a wave, and slots, each a range of a sequence's rows.  The fewest tiles of the sizes that
+// there are in the fewest groups of eight at most; more slots than sequences where there are two for each before the workgroups are as many as the
+// compute units (one and a half: 16 x 21 nodes x 1504 x 20 x 64 gains 12 us in the sum and loses as much in the merge), in whole rounds over the XCDs, and
+// of `per_min` steps at least.
+void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* slots, int* per_min) {
   const int mt = (H * N + 15) / 16, groups = (mt + 7) / 8, each = (mt + groups - 1) / groups, cw = 16 * vec_elems(dtype);
   *nt = each > 6 ? 8 : each > 4 ? 6 : each;
-  const long wgs = (long)B * ((mt + *nt - 1) / *nt) * ((d + 4 * cw - 1) / (4 * cw));
-  const int steps = (T + N + TREE_STEP - 1) / TREE_STEP;
-  *splits = (int)std::max(1l, std::min<long>({std::max(1l, 256 / wgs), (steps + 3) / 4, TREE_MAX_SPLITS}));
+  const int mgroups = (mt + *nt - 1) / *nt, dgroups = (d + 4 * cw - 1) / (4 * cw), blocks = (mgroups + 7) / 8 * ((dgroups + 5) / 6);
+  const int steps = (T + N + TREE_STEP - 1) / TREE_STEP, least = dtype == DT_F32 ? 2 : 4;
+  *per_min = std::max(least, (steps + TREE_MAX_SPLITS - 1) / TREE_MAX_SPLITS);
+  const long room = 256 / ((long)mgroups * dgroups), whole = blocks % 8 == 0 ? 1 : blocks % 4 == 0 ? 2 : blocks % 2 == 0 ? 4 : 8;
+  *slots = B;
+  if (room < 2 * (long)B) return;
+  const long most = std::min(room, (long)B * std::min((steps + least - 1) / least, TREE_MAX_SPLITS));
+  *slots = (int)std::max<long>(B, most >= whole ? most / whole * whole : most);
 }
 
 // Row splits of W_KV in the projection: until there is a workgroup for every compute unit, a turn for each wave at least.

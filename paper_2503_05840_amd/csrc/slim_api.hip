@@ -815,16 +815,16 @@ namespace {
 // Bounds that keep grids and 32-bit offsets inside their ranges
 constexpr int TREE_MAX_BATCH = 32768, TREE_MAX_ROWS = 1 << 20, TREE_MAX_WIDTH = 1 << 20, TREE_MAX_CONTEXT = (TREE_MAX_BLOCKS - 1) * TREE_BLOCK_ROWS, TREE_MAX_VOCABULARY = 1 << 24;
 
-struct TreePlan { size_t off_P, off_ref, off_lsum, off_C, off_Cop, off_sref, off_sl, off_odd, off_part, total; };
+struct TreePlan { size_t off_P, off_ref, off_lsum, off_C, off_Cop, off_sref, off_sl, off_plan, off_odd, off_part, total; };
 
-// Every term grows with T (tree_cut's splits do).
+// Every term grows with T (tree_cut's slots do).
 TreePlan tree_layout(TreeArgs& a, int dtype) {
   const int vec = vec_elems(dtype), ch = 4 * vec, cw = 16 * vec;
   a.MT = (a.H * a.N + 15) / 16;
   a.NB = (a.T + a.N + TREE_BLOCK_ROWS - 1) / TREE_BLOCK_ROWS;
   a.CT = a.NB * (TREE_BLOCK_ROWS / ch);
   a.DB = (a.d + cw - 1) / cw;
-  tree_cut(dtype, a.B, a.N, a.H, a.T, a.d, &a.NT, &a.S);
+  tree_cut(dtype, a.B, a.N, a.H, a.T, a.d, &a.NT, &a.slots, &a.per_min);
   a.csw = tree_row_splits(dtype, a.B, a.N, a.H, a.d);
   TreePlan p;
   size_t o = 0;
@@ -833,10 +833,11 @@ TreePlan tree_layout(TreeArgs& a, int dtype) {
   p.off_P = take((size_t)a.B * a.MT * a.CT * 1024);
   p.off_ref = take(sizeof(float) * rows * a.NB);
   p.off_lsum = take(sizeof(float) * rows * a.NB);
-  p.off_C = take(a.S > 1 ? sizeof(float) * rows * a.S * a.DB * cw : 0);
+  p.off_C = take(a.slots > a.B ? sizeof(float) * (size_t)a.slots * a.MT * 16 * a.DB * cw : 0);
   p.off_Cop = take(sizeof(float) * rows * a.DB * cw);
-  p.off_sref = take(sizeof(float) * rows * a.S);
-  p.off_sl = take(sizeof(float) * rows * a.S);
+  p.off_sref = take(sizeof(float) * (size_t)a.slots * a.MT * 16);
+  p.off_sl = take(sizeof(float) * (size_t)a.slots * a.MT * 16);
+  p.off_plan = take(sizeof(int32_t) * (1 + (size_t)a.slots + a.B));
   p.off_odd = take(sizeof(uint64_t) * 2 * (size_t)a.B * a.H);
   p.off_part = take(a.csw > 1 ? sizeof(float) * a.csw * (size_t)a.B * a.N * a.d : 0);
   p.total = o;
@@ -898,13 +899,14 @@ extern "C" int slim_tree_decode(const void* q, const void* Kcache, const void* W
   a.P = ws + p.off_P;
   a.ref = (float*)(ws + p.off_ref); a.lsum = (float*)(ws + p.off_lsum);
   a.C = (float*)(ws + p.off_C); a.Cop = ws + p.off_Cop; a.sref = (float*)(ws + p.off_sref); a.sl = (float*)(ws + p.off_sl);
+  a.plan = (int32_t*)(ws + p.off_plan);
   a.odd = (uint64_t*)(ws + p.off_odd);
   a.part = (float*)(ws + p.off_part);
   StageTimer tm(o, st);
   launch_tree_scores(dtype, a, st);
   tm.mark();
   launch_tree_weighted(dtype, a, st);
-  if (a.S > 1) launch_tree_merge(dtype, a, st);
+  if (a.slots > a.B) launch_tree_merge(dtype, a, st);
   tm.mark();
   launch_tree_project(dtype, a, st);
   tm.mark();

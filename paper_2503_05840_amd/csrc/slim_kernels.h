@@ -241,7 +241,8 @@ void launch_xweighted_full(const float* S, const void* K, long k_bstride, const 
 // ---- a tree of drafted tokens (kernels_tree.hip, kernels_verify.hip) -----------------------------------
 constexpr int TREE_MAX_NODES = 64;           // a node is a lane of a wave, a set of nodes 64 bits
 constexpr int TREE_BLOCK_ROWS = 256;         // cache rows that share a reference of the softmax numerators
-constexpr int TREE_MAX_SPLITS = 64;
+constexpr int TREE_MAX_SPLITS = 64;          // slots of a sequence
+constexpr int TREE_STEP_ROWS = 64;           // rows of a step of the weighted sum
 constexpr int TREE_MAX_BLOCKS = 16384;       // row blocks of a sequence
 
 struct TreeArgs {
@@ -253,16 +254,18 @@ struct TreeArgs {
   int B, N, H, d, d_k, T, banded;
   float qscale;                              // log2(e) / sqrt(d_k)
   // work in between.  Query row m = h N + i; a tile is 16 of them, a fragment 64 x 16 bytes: a matrix operand
-  int MT, CT, NB, DB, S, csw, NT;            // query tiles, fragments of a tile, row blocks, column blocks, context splits, row splits of W, tiles of a wave
+  int MT, CT, NB, DB, csw, NT;               // query tiles, fragments of a tile, row blocks, column blocks, row splits of W, tiles of a wave
+  int slots, per_min;                        // B, or more that the sequences' rows share, and a slot's fewest steps
+  int32_t* plan;                             // steps of a slot; [slots] sequence * TREE_MAX_SPLITS + split, or -1; [B] first slot * 2 TREE_MAX_SPLITS + splits
   void* P;                                   // [B][MT][CT] fragments: numerators
   float *ref, *lsum;                         // [B][NB][MT * 16]: reference and sum of a block's numerators
-  float* C;                                  // [B][S][MT][DB] blocks of 16 rows x 16 VEC columns: weighted sums, S > 1
+  float* C;                                  // [slots][MT][DB] blocks of 16 rows x 16 VEC columns: weighted sums, slots > B
   void* Cop;                                 // [B][MT][DB] the same divided by the softmax sums, as operands of the projection
-  float *sref, *sl;                          // [B][S][MT * 16]
+  float *sref, *sl;                          // [slots][MT * 16]
   uint64_t* odd;                             // [B][2][H]: drafted keys that are not finite in a head's columns (bit j: node j)
   float* part;                               // [csw][B][N][d], csw > 1
 };
-void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* splits);
+void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* slots, int* per_min);
 int tree_row_splits(int dtype, int B, int N, int H, int d);
 void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st);
 void launch_tree_weighted(int dtype, const TreeArgs& a, hipStream_t st);
