@@ -26,7 +26,11 @@ template <> struct Elem<DT_F32> {
 constexpr int TREE_BLOCK = TREE_BLOCK_ROWS;      // rows that share a reference of the numerators
 constexpr float REF_STEP = 32.f;                 // references are multiples of this (log2 domain)
 
-__device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+// Two of them, the first in the lower half (one instruction; a pair of single ones is three)
+__device__ __forceinline__ unsigned bf16_pair(float x, float y) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{x, y}, bf16x2));
+}
 __device__ __forceinline__ float bf16_value(unsigned bits) { return __uint_as_float(bits << 16); }
 
 template <int DT>
@@ -59,9 +63,8 @@ __device__ __forceinline__ void store_operand(const float (&v)[VEC], u32x4* out)
   if constexpr (DT == DT_BF16) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const unsigned h1 = bf16_bits(v[2 * j]), h2 = bf16_bits(v[2 * j + 1]);
-      hi[j] = h1 | h2 << 16;
-      lo[j] = (unsigned)bf16_bits(v[2 * j] - bf16_value(h1)) | (unsigned)bf16_bits(v[2 * j + 1] - bf16_value(h2)) << 16;
+      hi[j] = bf16_pair(v[2 * j], v[2 * j + 1]);
+      lo[j] = bf16_pair(v[2 * j] - bf16_value(hi[j] & 0xffffu), v[2 * j + 1] - __uint_as_float(hi[j] & 0xffff0000u));
     }
     out[0] = hi;
     out[64] = lo;
@@ -200,9 +203,8 @@ __device__ __forceinline__ void rotate_piece(u32x4 x, const f32x4* cs, u32x4& hi
       const float x1 = bf16_value(x[i] & 0xffffu), x2 = __uint_as_float(x[i] & 0xffff0000u);
       const float c = cs[i >> 1][2 * (i & 1)], s = cs[i >> 1][2 * (i & 1) + 1];
       const float y1 = x1 * c + x2 * s, y2 = x2 * c - x1 * s;
-      const unsigned h1 = bf16_bits(y1), h2 = bf16_bits(y2);
-      hi[i] = h1 | h2 << 16;
-      lo[i] = (unsigned)bf16_bits(y1 - bf16_value(h1)) | (unsigned)bf16_bits(y2 - bf16_value(h2)) << 16;
+      hi[i] = bf16_pair(y1, y2);
+      lo[i] = bf16_pair(y1 - bf16_value(hi[i] & 0xffffu), y2 - __uint_as_float(hi[i] & 0xffff0000u));
     }
   } else {
 #pragma unroll
@@ -217,13 +219,13 @@ __device__ __forceinline__ void rotate_piece(u32x4 x, const f32x4* cs, u32x4& hi
 
 template <int DT>
 __device__ __forceinline__ bool not_finite(u32x4 x) {
-  bool bad = false;
+  int bad = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if constexpr (DT == DT_BF16) bad |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
-    else bad |= (x[i] & 0x7f800000u) == 0x7f800000u;
+    if constexpr (DT == DT_BF16) bad |= (x[i] & 0x7f80u) == 0x7f80u;
+    bad |= (x[i] & 0x7f800000u) == 0x7f800000u;
   }
-  return bad;
+  return bad != 0;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -572,19 +574,18 @@ __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, 
 #pragma unroll
       for (int w = 1; w < WV; ++w) top = fmaxf(top, red[par][0][w][at]);
       const float ref = REF_STEP * ceilf(top * (1.f / REF_STEP));
-      // (an unused slot: 2^-inf; nothing visible, or nothing but NaN: numerators of 0 or NaN)
-      const float sub = !see[mt] ? INFINITY : top == NEG_INF ? 0.f : ref;
+      const float sub = top == NEG_INF ? 0.f : ref;        // (nothing visible, or nothing but NaN: numerators of 0 or NaN)
       u32x4 (&v)[PF] = pend[mt];
       float l = 0.f;
 #pragma unroll
       for (int ts = 0; ts < TS; ++ts) {
         float p[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = exp2_of(fmaf(acc[ts][mt][r], a.qscale, -sub));
+        for (int r = 0; r < 4; ++r) p[r] = see[mt] ? exp2_of(fmaf(acc[ts][mt][r], a.qscale, -sub)) : 0.f;
         if constexpr (DT == DT_BF16) {
           // (the weighted sum takes bf16 numerators; their sum is of the same values)
-          v[0][2 * ts] = (unsigned)bf16_bits(p[0]) | (unsigned)bf16_bits(p[1]) << 16;
-          v[0][2 * ts + 1] = (unsigned)bf16_bits(p[2]) | (unsigned)bf16_bits(p[3]) << 16;
+          v[0][2 * ts] = bf16_pair(p[0], p[1]);
+          v[0][2 * ts + 1] = bf16_pair(p[2], p[3]);
 #pragma unroll
           for (int i = 0; i < 2; ++i) l += bf16_value(v[0][2 * ts + i] & 0xffffu) + __uint_as_float(v[0][2 * ts + i] & 0xffff0000u);
         } else {
@@ -1056,7 +1057,7 @@ __global__ __launch_bounds__(256, 1) void tree_project_kernel(TreeArgs a) {
           *(f32x4*)(a.part + ((size_t)cs * a.B * a.N + node) * a.d + at) = v;
         } else if constexpr (DT == DT_BF16) {
           *(uint2*)((uint16_t*)a.out + node * a.d + at) =
-              uint2{(unsigned)bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16, (unsigned)bf16_bits(v[2]) | (unsigned)bf16_bits(v[3]) << 16};
+              uint2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
         } else {
           *(f32x4*)((float*)a.out + node * a.d + at) = v;
         }
@@ -1074,7 +1075,7 @@ __global__ __launch_bounds__(256) void tree_sum_kernel(const float* part, int cs
   f32x4 v = ((const f32x4*)part)[i];
   for (int c = 1; c < csw; ++c) v += ((const f32x4*)part)[c * n4 + i];
   if constexpr (DT == DT_BF16)
-    ((uint2*)out)[i] = uint2{(unsigned)bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16, (unsigned)bf16_bits(v[2]) | (unsigned)bf16_bits(v[3]) << 16};
+    ((uint2*)out)[i] = uint2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
   else
     ((f32x4*)out)[i] = v;
 }

@@ -142,3 +142,29 @@ def test_a_chain_gives_what_single_steps_give(N):
         want = one.cpu().numpy()[0]
         # both within the oracle's bound; sums of 700 terms in another order
         assert np.abs(got[0, i] - want).max() <= 2 * 700 * 2.0 ** -24 * 8
+
+
+MANY_BLOCKS = [  # (B, N, H, d_k, T, dtype, lens, base, banded): enough workgroups of scores for those that walk over row blocks or heads, splits of ragged batches
+    (4, 3, 16, 64, 2300, "f32", [2300, 700, 1, 1999], None, False), (2, 5, 16, 104, 4400, "bf16", None, None, False),
+    (4, 3, 64, 8, 1100, "bf16", [1100, 0, 255, 1024], 10000.0, False), (3, 16, 72, 16, 1250, "bf16", [513, 1250, 767], 10000.0, True),
+    (5, 2, 64, 4, 1000, "f32", [3, 1000, 511, 512, 800], 500.0, False), (9, 6, 8, 32, 3000, "bf16", [40, 3000, 0, 700, 64, 2222, 1, 333, 2900], None, False),
+    (70, 1, 2, 8, 900, "f32", [(37 * i) % 901 for i in range(70)], None, False),
+]
+
+
+@pytest.mark.parametrize("i", range(len(MANY_BLOCKS)))
+def test_many_row_blocks_against_the_oracle(i):
+    B, N, H, d_k, T, dtype, lens, base, banded = MANY_BLOCKS[i]
+    say(f"[case] tree, many blocks: B={B} N={N} H={H} d_k={d_k} T={T} {dtype} base={base} banded={banded}")
+    c = TreeCase(B, N, H, d_k, T, dtype, lens=lens, base=base, banded=banded, seed=300 + i)
+    say(f"       {c.check():.3f} of the bound")
+
+
+@pytest.mark.parametrize("B,N,H,d_k,T,dtype,base", [(1, 5, 16, 64, 40, "bf16", None), (4, 5, 16, 64, 2300, "f32", None), (4, 5, 64, 8, 1100, "bf16", 10000.0)])
+def test_a_context_that_is_not_finite_leaves_unused_slots_zero(B, N, H, d_k, T, dtype, base):
+    say(f"[case] tree, NaN in the context: B={B} N={N} H={H} d_k={d_k} T={T} {dtype}")
+    c = TreeCase(B, N, H, d_k, T, dtype, parents=[[-1, 0, 7, 0, 2]] * B, base=base, seed=23)
+    c.K[:, 5] = np.nan
+    c.K[0, T - 1] = np.inf
+    got = c.run()
+    assert (got[:, [2, 4]] == 0).all() and not np.isfinite(got[:, [0, 1, 3]]).any()
