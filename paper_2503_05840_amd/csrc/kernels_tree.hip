@@ -85,6 +85,8 @@ __device__ __forceinline__ void mma_in_place(const u32x4& a, const u32x4& b, f32
   else acc = mma<DT>(a, b, acc);
 }
 __device__ __forceinline__ void operands_ready() { asm volatile("s_nop 1"); }
+// (the same for an operand that has just been written: an asm statement keeps its place among others of its kind only)
+__device__ __forceinline__ void operands_ready(u32x4& x) { asm volatile("s_nop 1" : "+v"(x)); }
 __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
 // VEC rows x VEC columns per lane -> VEC operands (one per column), each VEC rows of that column
@@ -134,7 +136,7 @@ __device__ __forceinline__ uint64_t ancestors(const int32_t* parents, int N, int
 }
 
 // How the sequences share the slots of the weighted sum: the fewest steps of 64 rows a slot that leave enough of them (ragged batches: 8 sequences of 600
-// to 5000 rows in 16 slots take 27 steps, where as many slots for each take 40).  By one wave, which has up to four sequences a lane.
+// to 5000 rows in 16 slots take 30 steps, where as many slots for each take 40).  By one wave, which has up to four sequences a lane.
 __device__ void plan_splits(const TreeArgs& a, int lane) {
   int steps[4];
 #pragma unroll
@@ -874,10 +876,12 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
       }
       transpose<DT>(k[0], kt[0]);
 #pragma unroll
+      for (int c = 0; c < VEC; ++c) operands_ready(kt[0][c]);
+#pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         u32x4 pf = ((const u32x4*)a.P)[(((size_t)b * a.MT + min(mg * NT + nt, a.MT - 1)) * a.CT + chunk) * 64 + lane];
         pf = lowered<DT>(pf, lower_by(a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + min(mg * NT + nt, a.MT - 1) * 16 + n16], fin[nt * 16 + n16]));
-        operands_ready();
+        operands_ready(pf);
 #pragma unroll
         for (int c = 0; c < VEC; ++c) mma_in_place<DT>(kt[0][c], pf, acc[c][nt]);
       }
@@ -1101,10 +1105,11 @@ void launch_tree_scores_r(const TreeArgs& a, hipStream_t st) {
   if (blocks <= 512) return launch_tree_scores_s<DT, ROPE, 1>(a, st);     // few workgroups: more waves of fewer rows
   // The walk where its four steps of a row are all used, there is no rotation to wait for, and a round of workgroups holds every head: 8 x 64
   // nodes x 4096 x 32 x 128 175 -> 105 us, 4 ragged x 32 x 8000 86 -> 62, 1 x 2 x 16384 40 -> 31; but heads of 64 columns 34 -> 38 (16 x 21 x
-  // 1504 x 20), rotary ones 72 -> 100 (8 x 16 x 5000 x 24 x 96), 384 heads in a batch 112 -> 119 (24 x 5 x 6000 x 16 x 128).
+  // 1504 x 20), rotary ones 72 -> 100 (8 x 16 x 5000 x 24 x 96), 384 heads in a batch 112 -> 119 (24 x 5 x 6000 x 16 x 128).  Rotary keys: two score
+  // tiles a wave and twice the waves 72 -> 70; with cos and sin asked for together with the keys 88.
   constexpr int W = 16 * Elem<DT>::VEC;
   const int tiles = tree_head_tiles(a.N);
-  if (ROPE || a.d_k > W || a.d_k <= W * 3 / 4 || tiles > 4 || a.H * a.B > 256) return launch_tree_scores_s<DT, ROPE, 4>(a, st);
+  if (ROPE || a.d_k > W || a.d_k <= W * 3 / 4 || tiles > 4 || a.H * a.B > 256) return launch_tree_scores_s<DT, ROPE, ROPE ? 2 : 4>(a, st);
   const int z = std::min(a.NB, 256 / (a.H * a.B)), per = (a.NB + z - 1) / z;
   const dim3 grid(a.H, (a.NB + per - 1) / per, a.B);
   switch (tiles) {
@@ -1160,8 +1165,7 @@ void launch_tree_project_t(const TreeArgs& a, hipStream_t st) {
 
 // How the weighted sum is cut: NT query tiles of 16 rows to a wave, and slots, each a range of a sequence's rows.  The fewest tiles of the sizes that
 // there are in the fewest groups of eight at most; more slots than sequences where there are two for each before the workgroups are as many as the
-// compute units (one and a half: 16 x 21 nodes x 1504 x 20 x 64 gains 12 us in the sum and loses as much in the merge), in whole rounds over the XCDs, and
-// of `per_min` steps at least.
+// compute units (the merge that they need takes 5-16 us, which fewer would hardly gain), in whole rounds over the XCDs, and of `per_min` steps at least.
 void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* slots, int* per_min) {
   const int mt = (H * N + 15) / 16, groups = (mt + 7) / 8, each = (mt + groups - 1) / groups, cw = 16 * vec_elems(dtype);
   *nt = each > 6 ? 8 : each > 4 ? 6 : each;
