@@ -126,3 +126,17 @@ def test_commit_without_lengths_and_with_entries_that_are_no_slots():
     torch.cuda.synchronize()
     before[T + 4] = before[T + 5]
     assert np.array_equal(K.cpu().numpy()[0], before) and int(new[0]) == T + N
+
+
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("V,dtype", [(300001, "f32"), (1100003, "bf16")])
+def test_vocabularies_summed_in_parts_of_parts(V, dtype, draft):
+    """Tokens at the vocabulary's very ends, between them, and past a stretch without any weight."""
+    say(f"[case] verify: V={V} {dtype} draft={draft}")
+    rng = np.random.default_rng(V)
+    p, q = _probabilities(rng, 3, 2, V, dtype, draft)
+    p[1, :, 1000:V - 5] = 0.0
+    parents, tokens = np.tile(np.array([-1, 0], dtype=np.int32), (3, 1)), rng.integers(0, 3, (3, 2)).astype(np.int32)
+    for u0 in (0.0, 0.31, 0.77, np.float32(1) - np.float32(2 ** -24)):
+        u = np.array([[u0, 0.999]] * 3, dtype=np.float32)
+        _same(_call(tokens, parents, p, q if draft else None, u, dtype), tokens, parents, p, q if draft else None, u)
