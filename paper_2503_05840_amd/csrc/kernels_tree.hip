@@ -1099,17 +1099,28 @@ void launch_tree_scores_s(const TreeArgs& a, hipStream_t st) {
   if (a.N <= 17) hipLaunchKernelGGL((tree_scores_kernel<DT, ROPE, TS, 2>), grid, block, 0, st, a);      // (a head's rows touch two tiles at most)
   else hipLaunchKernelGGL((tree_scores_kernel<DT, ROPE, TS, 5>), grid, block, 0, st, a);
 }
+// Two score tiles a wave and twice the waves where a wave of four keeps more than two query tiles' sums, 200 registers: 16 x 21 nodes x 1504 x 20 x 64
+// 104.9 -> 99.0 us for the call, 4 x 40 x 8000 x 12 x 72 110.5 -> 105.8; of two query tiles 319.6 -> 336.3 (24 x 5 x 6000 x 16 x 128), 157.5 -> 161.3 (8 x 16 x
+// 3000 x 32 x 80).  And for rotary keys, with two tiles 72 -> 70 (8 x 16 x 5000 x 24 x 96; cos and sin asked for together with the keys 88).
+template <int DT, bool ROPE>
+void launch_tree_scores_w(const TreeArgs& a, hipStream_t st) {
+  if constexpr (ROPE) {
+    launch_tree_scores_s<DT, ROPE, 2>(a, st);
+  } else {
+    if (a.N > 17) launch_tree_scores_s<DT, ROPE, 2>(a, st);
+    else launch_tree_scores_s<DT, ROPE, 4>(a, st);
+  }
+}
 template <int DT, bool ROPE>
 void launch_tree_scores_r(const TreeArgs& a, hipStream_t st) {
   const long blocks = (long)a.H * a.NB * a.B;
   if (blocks <= 512) return launch_tree_scores_s<DT, ROPE, 1>(a, st);     // few workgroups: more waves of fewer rows
   // The walk where its four steps of a row are all used, there is no rotation to wait for, and a round of workgroups holds every head: 8 x 64
   // nodes x 4096 x 32 x 128 175 -> 105 us, 4 ragged x 32 x 8000 86 -> 62, 1 x 2 x 16384 40 -> 31; but heads of 64 columns 34 -> 38 (16 x 21 x
-  // 1504 x 20), rotary ones 72 -> 100 (8 x 16 x 5000 x 24 x 96), 384 heads in a batch 112 -> 119 (24 x 5 x 6000 x 16 x 128).  Rotary keys: two score
-  // tiles a wave and twice the waves 72 -> 70; with cos and sin asked for together with the keys 88.
+  // 1504 x 20), rotary ones 72 -> 100 (8 x 16 x 5000 x 24 x 96), 384 heads in a batch 112 -> 119 (24 x 5 x 6000 x 16 x 128).
   constexpr int W = 16 * Elem<DT>::VEC;
   const int tiles = tree_head_tiles(a.N);
-  if (ROPE || a.d_k > W || a.d_k <= W * 3 / 4 || tiles > 4 || a.H * a.B > 256) return launch_tree_scores_s<DT, ROPE, ROPE ? 2 : 4>(a, st);
+  if (ROPE || a.d_k > W || a.d_k <= W * 3 / 4 || tiles > 4 || a.H * a.B > 256) return launch_tree_scores_w<DT, ROPE>(a, st);
   const int z = std::min(a.NB, 256 / (a.H * a.B)), per = (a.NB + z - 1) / z;
   const dim3 grid(a.H, (a.NB + per - 1) / per, a.B);
   switch (tiles) {
