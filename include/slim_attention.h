@@ -320,6 +320,7 @@ int vanilla_attention_block(const void* x, const void* W_Q, const void* W_K, con
  * q and out have the cache's type (slim_decode's are fp32): N rows a sequence are inputs and outputs of matrix products.  Scores,
  * softmax sums and weighted sums are fp32; the softmax numerators are rounded to dtype where they enter the weighted sum.
  * A drafted key that is not finite makes NaN of the nodes that see it and changes nothing for the others.
+ * The same batch gives the same bits; one of other lengths may cut a sequence's rows otherwise and sum them in another order.
  * opts->stage_ms: scores, weighted sum, projection.  Scratch: slim_workspace_bytes_tree (0 on invalid arguments), else library-owned. */
 size_t slim_workspace_bytes_tree(int B, int N, int H, int T, int d, int dtype);
 int slim_tree_decode(const void* q, const void* Kcache, const void* W_KV, const int32_t* parents, void* out,

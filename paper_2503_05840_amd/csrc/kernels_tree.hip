@@ -236,7 +236,8 @@ __device__ __forceinline__ bool not_finite(u32x4 x) {
 // to MAXT tiles of 16, whose other rows are other heads': zero in the query operand and written by their own workgroups.  As references the
 // numerators 2^(s - ref) take the block's maximum rounded up to a multiple of 32: a bf16 or fp32 numerator is as exact at 2^-32 as at 1,
 // and blocks whose maxima differ by less than that have the same reference, so that the weighted sum hardly ever needs a factor.  They
-// leave as operands of that sum (lane l of a 1 KB fragment: query row l % 16, cache rows slot_row(l / 16, j)).
+// leave as operands of that sum (lane l of a 1 KB fragment: query row l % 16, cache rows slot_row(l / 16, j)).  Bound by the chain of a short workgroup:
+// lengths, keys, maxima, numerators.  16 x 21 nodes x 500..1504 x 20 x 64 28 us, 8 x 16 x 600..5000 x 24 x 96 rotary 68, 1 x 1 x 777 x 32 x 128 8.
 // ------------------------------------------------------------------------------------------------
 template <int DT, bool ROPE, int TS, int MAXT>
 __global__ __launch_bounds__(1024 / TS) void tree_scores_kernel(TreeArgs a) {
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(1024 / TS) void tree_scores_kernel(TreeArgs a) {
 // head's queries resident as operands (heads of up to four steps: 128 columns in bf16, 64 in fp32) and the next block's keys in flight
 // while this one's are scored.  One barrier a block, for the maxima; the sums of a block are put together behind the next one's, and its
 // numerators stored behind the wait for the next one's keys, which would else be a wait for them as well.  Blocks of context alone need
-// no mask.
+// no mask.  8 x 64 nodes x 4096 x 32 x 128: 96 us, of which K (270 MB) would take 55 at a copy's rate; 1 x 26 x 16384 42.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int MAXT>
 __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, int per) {
@@ -638,7 +639,8 @@ __device__ __forceinline__ u32x4 lowered(u32x4 p, float e) {
 // Weighted sum: C^T = K^T P^T over a split of the context, for all heads together: every query row sums whole rows of K.  A wave owns
 // 16 VEC columns of K (128 in bf16) and NT tiles of 16 query rows; a workgroup's four waves, one per SIMD, are four neighbouring column blocks
 // of the same query rows.  K goes from memory to the wave's registers and is transposed there (no other wave of the workgroup needs it), RK
-// steps of 64 rows ahead; the numerators are the same for the four waves and go through LDS, a step ahead, one barrier a step.
+// steps of 64 rows ahead; the numerators are the same for the four waves and go through LDS, a step ahead, one barrier a step.  Bound by the matrix cores and
+// what has to be issued beside them: 8 x 64 nodes x 4096 x 32 x 128 498 us, 1.10 PFLOP/s (a library product of 8192^3: 1.08), 54 % of their cycles.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int NT> struct Weighted {
   static constexpr int VEC = Elem<DT>::VEC, CH = 4 * VEC, SC = TREE_STEP / CH;    // chunks of a step
@@ -974,7 +976,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
 // ------------------------------------------------------------------------------------------------
 // Projection: out[i, h] = C[h N + i] W_KV[:, h].  A workgroup of four waves, one per SIMD, takes one head (or 16 VEC columns of one), NM of the query
 // tiles that hold rows of it (of any sequence) and a range of rows of W_KV, which the waves share out 4 VEC at a time; what they load lies
-// RD turns ahead in registers, and their sums meet in LDS.
+// RD turns ahead in registers, and their sums meet in LDS.  1 x 1 node x 32 x 128: W_KV (33.5 MB) in 13 us, 2.5 TB/s, half of it the start and the end;
+// 8 x 64 73 us, C read once for every head that has rows in a tile.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int NM>
 __global__ __launch_bounds__(256, 1) void tree_project_kernel(TreeArgs a) {

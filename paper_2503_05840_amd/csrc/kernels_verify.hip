@@ -247,7 +247,8 @@ __device__ int draw(const R& r, double u, double* part) {
 // One workgroup per sequence.  After k rejections at a node the residual distribution is max(p - a_k q, 0) / F(a_k) with F(a) = sum max(p - a q, 0),
 // a_0 = 0, F(a_0) = 1 and a_{k+1} = a_k + F(a_k): one scalar stands for the chain of residual vectors, and only F of the last one needs
 // a pass over the vocabulary.  Every product and sum in 64 bits.  A node is a lane of every wave, which has asked for the node's p and q
-// before the walk begins, so that the walk itself reads registers.
+// before the walk begins, so that the walk itself reads registers.  Bound by one compute unit's passes over a row: 8 x 26 nodes x 128000 chosen, one pass of
+// 512 KB, 15 us; 32 x 16 x 50257 bf16 24; 1 x 8 x 32000 8.
 // ------------------------------------------------------------------------------------------------
 template <int DT, bool DRAFT>
 __global__ __launch_bounds__(VW * 64) void tree_verify_kernel(VerifyArgs a) {
@@ -358,7 +359,8 @@ __global__ __launch_bounds__(VW * 64) void tree_verify_kernel(VerifyArgs a) {
 // ------------------------------------------------------------------------------------------------
 // One workgroup per sequence.  A thread moves 16-byte column pieces of the path's rows, in the path's order: row j goes to len + j < len + path[j], so
 // no row is overwritten before it has been read, and no thread reads what another writes.  The new length may take the old one's place:
-// it is written when every thread has read that.
+// it is written when every thread has read that.  Eight rows are asked for before the first is stored (each is read from a later place than any of them is
+// written to): 64 sequences of 16 rows x 1280 in 7 us, one of two rows x 4096 in 2.
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void tree_commit_kernel(u32x4* K, long bstride, const int32_t* path, const int32_t* n_path, const int32_t* seq_lens,
                                                            int32_t* new_lens, int N, int T, int pieces, int head_pieces, int banded) {
