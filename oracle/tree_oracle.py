@@ -30,20 +30,20 @@ def rotate(x: np.ndarray, H: int, pos: np.ndarray, base: float) -> np.ndarray:
     return np.stack([z.real, z.imag], axis=-1).reshape(n, d)
 
 
-def tree_attention(q, K, W_KV, parents, length: int, H: int, base=None):
-    """q (N, d), K (length + N, d) raw keys, W_KV (d, d), parents (N,).  Returns (out (N, d), spread, size, swing), the last three
+def tree_attention(q, K, W_KV, parents, length: int, H: int, base=None, nodes=None):
+    """q (N, d), K (length + N, d) raw keys, W_KV (d, d), parents (N,).  `nodes`: the nodes that are computed (None: all); the others' rows are 0.  Returns (out (N, d), spread, size, swing), the last three
     for error bounds: spread = sum_t P |V_t - out|, size = (P |K|) |W_KV| per element of the result, swing = the largest
     sum_j |q_j k_tj| / sqrt(d_k) of a node and head over its rows."""
     q, K, W = (np.asarray(x, dtype=np.float64) for x in (q, K, W_KV))
     N, d = q.shape
     d_k = d // H
     out, spread, size, swing = np.zeros((N, d)), np.zeros((N, d)), np.zeros((N, d)), np.zeros((N, H))
-    for i in range(N):
-        nodes = chain(parents, i)
-        if nodes is None:
+    for i in range(N) if nodes is None else nodes:
+        seen = chain(parents, i)
+        if seen is None:
             continue
-        rows = list(range(length)) + [length + j for j in nodes]
-        pos = list(range(length)) + [length + len(chain(parents, j)) - 1 for j in nodes]
+        rows = list(range(length)) + [length + j for j in seen]
+        pos = list(range(length)) + [length + len(chain(parents, j)) - 1 for j in seen]
         Ki = K[rows]
         key = Ki if base is None else rotate(Ki, H, np.array(pos), base)
         V = Ki @ W

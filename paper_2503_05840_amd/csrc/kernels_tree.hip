@@ -434,7 +434,11 @@ __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, 
   const int blk0 = blockIdx.y * per, blk1 = min(blk0 + per, (L + TREE_BLOCK - 1) / TREE_BLOCK);
   plan_once(a, lane, wave);
   if (blk0 >= blk1) return;
-  __shared__ float red[2][2][WV][MAXT * 16];               // [block parity][maximum, sum]
+  // [block parity][maximum, sum], and the odd keys of a block, each wave's in its own place.  Two barriers without one between them leave no wave more than
+  // a block ahead of another (wave 0 alone finishes blocks for all), so a place is read for the last time before the barrier behind which it may be
+  // written again, two blocks on: maxima and odd keys are written before their block's barrier, read between that and the next and written again
+  // behind the next; sums are written behind their block's barrier, read between the next and the one after and written again behind that.
+  __shared__ float red[2][2][WV][MAXT * 16];
   __shared__ uint64_t odd[2][WV];
   const int rp = a.banded ? a.d_k : a.d, nk = (a.d_k + KW - 1) / KW;
   const T* K = (const T*)a.K + (size_t)b * a.k_bstride + piece_at(h * a.d_k, a.d_k, a.banded);
@@ -472,21 +476,19 @@ __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, 
     const uint64_t own = __shfl((unsigned)anc, i & 63) | (uint64_t)__shfl((unsigned)(anc >> 32), i & 63) << 32;
     see[mt] = mine ? own : 0;
   }
-  // the sums, references and odd keys of a block whose waves are all past it
+  // the sums of a block whose waves are all past it
   auto finish = [&](int blk, int par) {
     for (int at = threadIdx.x; at < ntiles * 16; at += WV * 64) {
       const int m = tile0 * 16 + at;
       if (m < m0 || m >= m1) continue;
-      float l = red[par][1][0][at], top = red[par][0][0][at];
+      float l = red[par][1][0][at];
 #pragma unroll
-      for (int w = 1; w < WV; ++w) {
-        l += red[par][1][w][at];
-        top = fmaxf(top, red[par][0][w][at]);
-      }
-      const size_t to = ((size_t)b * a.NB + blk) * a.MT * 16 + m;
-      a.lsum[to] = l;
-      a.ref[to] = top == NEG_INF ? NEG_INF : REF_STEP * ceilf(top * (1.f / REF_STEP));
+      for (int w = 1; w < WV; ++w) l += red[par][1][w][at];
+      a.lsum[((size_t)b * a.NB + blk) * a.MT * 16 + m] = l;
     }
+  };
+  // the odd keys of a block, between its barrier and the next
+  auto note_odd = [&](int blk, int par) {
     const int at = blk - len / TREE_BLOCK;
     if (threadIdx.x == 0 && at >= 0) {
       uint64_t any = 0;
@@ -570,14 +572,16 @@ __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, 
     }
     lds_barrier();
     if (blk > blk0) finish(blk - 1, 1 - par);
+    note_odd(blk, par);
 #pragma unroll
     for (int mt = 0; mt < MAXT; ++mt) {
-      const int at = mt * 16 + n16;
+      const int at = mt * 16 + n16, m = (tile0 + mt) * 16 + n16;
       float top = red[par][0][0][at];
 #pragma unroll
       for (int w = 1; w < WV; ++w) top = fmaxf(top, red[par][0][w][at]);
       const float ref = REF_STEP * ceilf(top * (1.f / REF_STEP));
       const float sub = top == NEG_INF ? 0.f : ref;        // (nothing visible, or nothing but NaN: numerators of 0 or NaN)
+      if (wave == 0 && g == 0 && m >= m0 && m < m1) a.ref[((size_t)b * a.NB + blk) * a.MT * 16 + m] = ref;
       u32x4 (&v)[PF] = pend[mt];
       float l = 0.f;
 #pragma unroll

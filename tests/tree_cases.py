@@ -63,16 +63,16 @@ class TreeCase:
         torch.cuda.synchronize()
         return out.float().cpu().numpy()
 
-    def expected(self):
-        """(result, bound), both (B, N, d).  The bound, to first order and then a tenth more for the products of errors:
+    def expected(self, sequences=None, nodes=None):
+        """(result, bound), both (B, N, d), zeros but for the given sequences and nodes (None: all).  The bound, to first order and then a tenth more for the products of errors:
         a numerator is off by half a step of the type (and the softmax sum is of the rounded ones), by the error of its score and by two steps of
         fp32 for its exponential: spread times that; sums over T rows and d columns in fp32, and C as the type's hi + lo: size times
         that; the result's own rounding."""
         out, bound = np.zeros((self.B, self.N, self.d)), np.zeros((self.B, self.N, self.d))
         f32, half = HALF["f32"], HALF[self.dtype]
-        for b in range(self.B):
+        for b in range(self.B) if sequences is None else sequences:
             n = int(self.lens[b])
-            o, spread, size, swing = orc.tree_attention(self.q[b], self.K[b, :n + self.N], self.W, self.parents[b], n, self.H, self.base)
+            o, spread, size, swing = orc.tree_attention(self.q[b], self.K[b, :n + self.N], self.W, self.parents[b], n, self.H, self.base, nodes)
             score = swing * (self.d_k + 4) * f32
             if self.base is not None:
                 # angles' cos and sin as fp32, the rotation in fp32, and in bf16 the rotated key as hi + lo
@@ -88,5 +88,15 @@ class TreeCase:
         want, bound = self.expected()
         assert np.isfinite(got).all()
         worst = np.abs(got - want) / bound
+        assert worst.max() <= 1.0, f"{worst.max():.3f} of the bound at {np.unravel_index(worst.argmax(), worst.shape)}"
+        return float(worst.max())
+
+    def check_some(self, sequences, nodes, got=None):
+        """`check` of a few nodes of a few sequences; the other results have to be finite."""
+        got = self.run() if got is None else got
+        want, bound = self.expected(sequences, nodes)
+        assert np.isfinite(got).all()
+        at = np.ix_(sequences, nodes)
+        worst = np.abs(got[at] - want[at]) / bound[at]
         assert worst.max() <= 1.0, f"{worst.max():.3f} of the bound at {np.unravel_index(worst.argmax(), worst.shape)}"
         return float(worst.max())
