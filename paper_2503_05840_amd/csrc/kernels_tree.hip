@@ -799,6 +799,7 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
         a.sl[to] = l;
       }
       if (whole && sub == 0) wrow[row] = l != 0.f ? 1.f / l : 0.f;
+      lds_barrier();                                       // (wrow is read by all; without steps before the odd keys' there is no other barrier in between)
     }
   }
   f32x4 acc[VEC][NT];
