@@ -309,6 +309,7 @@ int vanilla_attention_block(const void* x, const void* W_Q, const void* W_K, con
  * the keys are stored raw and rotated for the scores, q is taken as given, as in slim_decode.
  * Both layouts of opts->k_layout (t_stride % 32 == 0 for the banded one), any H and d_k of whole 16-byte vectors.
  * opts->variant and opts->wait_budget_us mean nothing to these calls: none of their kernels waits for another workgroup.
+ * On a workspace that decode steps use too, what slim_status says of the latest of those stays.
  * They allocate nothing when given a workspace, and may be captured. */
 
 /* eq. 7 option 2 for the N nodes of each of B trees:

@@ -830,6 +830,7 @@ TreePlan tree_layout(TreeArgs& a, int dtype) {
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += up(bytes); return at; };
   const size_t rows = (size_t)a.B * a.MT * 16;
+  take(sizeof(int) * CTRL_INTS);             // (a workspace's control block: what slim_status reads of a decode step on the same workspace stays)
   p.off_P = take((size_t)a.B * a.MT * a.CT * 1024);
   p.off_ref = take(sizeof(float) * rows * a.NB);
   p.off_lsum = take(sizeof(float) * rows * a.NB);
