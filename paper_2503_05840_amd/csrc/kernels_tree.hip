@@ -1205,6 +1205,19 @@ int tree_row_splits(int dtype, int B, int N, int H, int d) {
   return (int)std::max(1l, std::min<long>({(256 + wgs - 1) / wgs, db, 16}));
 }
 
+// A sequence has `cuts` slots at most (tree_cut's `most`), and room * MT <= 256 MT / (mgroups dgroups), where MT / mgroups <= min(MT, 8).
+size_t tree_most_split_tiles(int dtype, int B, int N, int H, int T, int d) {
+  const int mt = (H * N + 15) / 16, cw = 16 * vec_elems(dtype), dgroups = (d + 4 * cw - 1) / (4 * cw), steps = (T + N + TREE_STEP - 1) / TREE_STEP;
+  const int least = dtype == DT_F32 ? 2 : 4, cuts = std::min((steps + least - 1) / least, TREE_MAX_SPLITS);
+  return cuts > 1 ? std::min<size_t>((size_t)B * cuts * mt, 256 * std::min(mt, 8) / dgroups) : 0;
+}
+
+// With csw > 1 there are fewer than 256 workgroups, so csw <= 256 / wgs + 1 <= 512 / wgs, and wgs >= H cblocks B N / 64 (four tiles of 16 rows a workgroup at most).
+size_t tree_most_split_rows(int dtype, int B, int N, int H, int d) {
+  const int cw = 16 * vec_elems(dtype), cblocks = (d / H + cw - 1) / cw, db = (d + cw - 1) / cw;
+  return db > 1 ? std::min<size_t>((size_t)std::min(db, 16) * B * N, 512 * 64 / ((long)H * cblocks)) : 0;
+}
+
 void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st) {
   if (dtype == DT_BF16) launch_tree_scores_t<DT_BF16>(a, st);
   else launch_tree_scores_t<DT_F32>(a, st);

@@ -817,7 +817,8 @@ constexpr int TREE_MAX_BATCH = 32768, TREE_MAX_ROWS = 1 << 20, TREE_MAX_WIDTH = 
 
 struct TreePlan { size_t off_P, off_ref, off_lsum, off_C, off_Cop, off_sref, off_sl, off_plan, off_odd, off_part, total; };
 
-// Every term grows with T (tree_cut's slots do).
+// Every term grows with T, B and N, so that a workspace sized for the largest serves every smaller one.  Slots and row splits do not by themselves (a batch
+// that fills the chip has none): what they take is reserved by bounds that do, up to 67 and 17 MB, tree_most_split_tiles and tree_most_split_rows.
 TreePlan tree_layout(TreeArgs& a, int dtype) {
   const int vec = vec_elems(dtype), ch = 4 * vec, cw = 16 * vec;
   a.MT = (a.H * a.N + 15) / 16;
@@ -834,13 +835,16 @@ TreePlan tree_layout(TreeArgs& a, int dtype) {
   p.off_P = take((size_t)a.B * a.MT * a.CT * 1024);
   p.off_ref = take(sizeof(float) * rows * a.NB);
   p.off_lsum = take(sizeof(float) * rows * a.NB);
-  p.off_C = take(a.slots > a.B ? sizeof(float) * (size_t)a.slots * a.MT * 16 * a.DB * cw : 0);
+  const size_t split_tiles = std::max(tree_most_split_tiles(dtype, a.B, a.N, a.H, a.T, a.d), a.slots > a.B ? (size_t)a.slots * a.MT : 0);
+  const size_t slot_rows = std::max(rows, split_tiles * 16), slots = std::max((size_t)a.B, (size_t)std::min(256l, (long)a.B * TREE_MAX_SPLITS));
+  p.off_C = take(sizeof(float) * split_tiles * 16 * a.DB * cw);
   p.off_Cop = take(sizeof(float) * rows * a.DB * cw);
-  p.off_sref = take(sizeof(float) * (size_t)a.slots * a.MT * 16);
-  p.off_sl = take(sizeof(float) * (size_t)a.slots * a.MT * 16);
-  p.off_plan = take(sizeof(int32_t) * (1 + (size_t)a.slots + a.B));
+  p.off_sref = take(sizeof(float) * slot_rows);
+  p.off_sl = take(sizeof(float) * slot_rows);
+  p.off_plan = take(sizeof(int32_t) * (1 + slots + a.B));
   p.off_odd = take(sizeof(uint64_t) * 2 * (size_t)a.B * a.H);
-  p.off_part = take(a.csw > 1 ? sizeof(float) * a.csw * (size_t)a.B * a.N * a.d : 0);
+  const size_t split_rows = std::max(tree_most_split_rows(dtype, a.B, a.N, a.H, a.d), a.csw > 1 ? (size_t)a.csw * a.B * a.N : 0);
+  p.off_part = take(sizeof(float) * split_rows * a.d);
   p.total = o;
   return p;
 }

@@ -267,6 +267,9 @@ struct TreeArgs {
 };
 void tree_cut(int dtype, int B, int N, int H, int T, int d, int* nt, int* slots, int* per_min);
 int tree_row_splits(int dtype, int B, int N, int H, int d);
+// Bounds of slots * MT where there are more slots than sequences, and of csw * B * N where there is more than one row split, that grow with every size
+size_t tree_most_split_tiles(int dtype, int B, int N, int H, int T, int d);
+size_t tree_most_split_rows(int dtype, int B, int N, int H, int d);
 void launch_tree_scores(int dtype, const TreeArgs& a, hipStream_t st);
 void launch_tree_weighted(int dtype, const TreeArgs& a, hipStream_t st);
 void launch_tree_merge(int dtype, const TreeArgs& a, hipStream_t st);
