@@ -347,9 +347,11 @@ int slim_tree_decode(const void* q, const void* Kcache, const void* W_KV, const 
 int slim_tree_verify(const int32_t* tokens, const int32_t* parents, const void* p, const void* draft, const float* u,
                      int32_t* path, int32_t* n_path, int32_t* next_token, int B, int N, int V, const slim_opts* opts);
 
-/* Row len_b + path[b][j] of the cache to row len_b + j, j < n_path[b], and new_lens[b] = len_b + n_path[b] (which may be
- * opts->seq_lens itself; then it is the next step's).  path is strictly increasing, as slim_tree_verify writes it; entries that are
- * no slot, or not past their place, move nothing.  path and n_path: device int32 [B][N], [B]. */
+/* Row len_b + path[b][j] of the cache to row len_b + j, j < n_path[b], and new_lens[b] = len_b + n_path[b].  A call moves one layer's rows
+ * and takes the lengths of before: new_lens may be opts->seq_lens itself (then it is the next step's) in the last layer's call only.  The layers before
+ * it write theirs, the same figures, elsewhere, or the next layer would move its rows from len_b + n_path[b] on.
+ * path is strictly increasing, as slim_tree_verify writes it; entries that are no slot, or not past their place, move nothing.
+ * path and n_path: device int32 [B][N], [B]. */
 int slim_tree_commit(void* Kcache, const int32_t* path, const int32_t* n_path, int32_t* new_lens, int B, int N, int H, int T, int d,
                      const slim_opts* opts);
 

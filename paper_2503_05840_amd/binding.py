@@ -431,7 +431,8 @@ def slim_tree_verify(tokens, parents, p, draft, u, path, n_path, next_token, B, 
 
 def slim_tree_commit(Kcache, path, n_path, new_lens, B, N, H, T, d, dtype="bf16", seq_lens=None, seq_lens_host=None, t_stride=0,
                      stage_ms=None, k_layout=K_ROWMAJOR):
-    """The accepted path's keys to their places in the cache; new_lens (B,) int32 may be seq_lens itself."""
+    """The accepted path's keys to their places in one layer's cache; new_lens (B,) int32 may be seq_lens itself in the last layer's call only (every layer's
+    call takes the lengths of before)."""
     import torch
     i32 = torch.int32
     _lens_ok(seq_lens, B, "seq_lens")
