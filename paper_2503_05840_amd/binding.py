@@ -387,10 +387,14 @@ def _element(dtype):
     return torch.bfloat16 if dtype == "bf16" else torch.float32
 
 
-def _lens_ok(t, B, name):
+def _lens_ok(seq_lens, seq_lens_host, B):
+    """Both are read for B sequences."""
     import torch
+    t = seq_lens
     if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_cuda or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous int32 device tensor of {B}")
+        raise ValueError(f"seq_lens must be a contiguous int32 device tensor of {B}")
+    if seq_lens_host is not None and np.shape(seq_lens_host) != (B,):
+        raise ValueError(f"seq_lens_host must hold {B} lengths")
 
 
 def _rows_of_tree(Kcache, B, N, T, d, t_stride, dtype):
@@ -403,9 +407,11 @@ def slim_tree_decode(q, Kcache, W_KV, parents, out, B, N, H, T, d, dtype="bf16",
     """Attention of B trees of N drafted tokens over their K-caches: q, out (B, N, d), Kcache (B, t_stride or T + N, d), parents (B, N) int32."""
     import torch
     el = _element(dtype)
-    _lens_ok(seq_lens, B, "seq_lens")
+    _lens_ok(seq_lens, seq_lens_host, B)
     if rope_table is not None and (rope_table.dtype != torch.float32 or rope_table.numel() < (T + N) * (d // H)):
         raise ValueError("rope_table must be float32 and hold T + N positions")
+    if workspace is not None:
+        _dev_ptr(workspace)
     ptrs = (_tree_ptr(q, (B, N, d), el), _rows_of_tree(Kcache, B, N, T, d, t_stride, dtype), _tree_ptr(W_KV, (d, d), el),
             _tree_ptr(parents, (B, N), torch.int32), _tree_ptr(out, (B, N, d), el))
     o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, workspace, VARIANT_AUTO, stage_ms, rope_table, 0, k_layout)
@@ -435,7 +441,7 @@ def slim_tree_commit(Kcache, path, n_path, new_lens, B, N, H, T, d, dtype="bf16"
     call takes the lengths of before)."""
     import torch
     i32 = torch.int32
-    _lens_ok(seq_lens, B, "seq_lens")
+    _lens_ok(seq_lens, seq_lens_host, B)
     ptrs = (_rows_of_tree(Kcache, B, N, T, d, t_stride, dtype), _tree_ptr(path, (B, N), i32), _tree_ptr(n_path, (B,), i32),
             _tree_ptr(new_lens, (B,), i32))
     o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, None, VARIANT_AUTO, stage_ms, None, 0, k_layout)
