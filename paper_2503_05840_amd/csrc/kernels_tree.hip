@@ -84,9 +84,14 @@ __device__ __forceinline__ void mma_in_place(const u32x4& a, const u32x4& b, f32
   if constexpr (DT == DT_BF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
   else acc = mma<DT>(a, b, acc);
 }
-__device__ __forceinline__ void operands_ready() { asm volatile("s_nop 1"); }
-// (the same for an operand that has just been written: an asm statement keeps its place among others of its kind only)
+// (An operand that has just been written is named: an asm statement keeps its place among others of its kind only.)
 __device__ __forceinline__ void operands_ready(u32x4& x) { asm volatile("s_nop 1" : "+v"(x)); }
+// (and for the accumulators of a tile's products: where registers are short the compiler parks one elsewhere and brings it back right before its product)
+template <int VEC, int NT>
+__device__ __forceinline__ void operands_ready(f32x4 (&acc)[VEC][NT], int nt) {
+  if constexpr (VEC == 8)
+    asm volatile("s_nop 1" : "+a"(acc[0][nt]), "+a"(acc[1][nt]), "+a"(acc[2][nt]), "+a"(acc[3][nt]), "+a"(acc[4][nt]), "+a"(acc[5][nt]), "+a"(acc[6][nt]), "+a"(acc[7][nt]));
+}
 __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
 // VEC rows x VEC columns per lane -> VEC operands (one per column), each VEC rows of that column
@@ -842,7 +847,7 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
       if constexpr (at == TILES - AHEAD) lds_barrier();
       if constexpr (at + AHEAD < TILES) pf[(at + AHEAD) % PQ] = ring[st & 1][fragment(at + AHEAD) * 64 + lane];
       else pf[(at + AHEAD) % PQ] = ring[st + 1 & 1][fragment(at + AHEAD - TILES) * 64 + lane];
-      operands_ready();
+      operands_ready(acc, nt);
       __builtin_amdgcn_sched_barrier(0);
     }
     mma_in_place<DT>(kt[c & 1][cc], pf[at % PQ], acc[cc][nt]);
@@ -889,6 +894,7 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
         u32x4 pf = ((const u32x4*)a.P)[(((size_t)b * a.MT + min(mg * NT + nt, a.MT - 1)) * a.CT + chunk) * 64 + lane];
         pf = lowered<DT>(pf, lower_by(a.ref[((size_t)b * a.NB + chunk / CPB) * a.MT * 16 + min(mg * NT + nt, a.MT - 1) * 16 + n16], fin[nt * 16 + n16]));
         operands_ready(pf);
+        operands_ready(acc, nt);
 #pragma unroll
         for (int c = 0; c < VEC; ++c) mma_in_place<DT>(kt[0][c], pf, acc[c][nt]);
       }
