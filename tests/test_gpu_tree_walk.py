@@ -34,3 +34,17 @@ def test_walk_over_row_blocks(i, far):
         scale = np.array([1.0, 0.02, 0.3])[np.arange(c.rows) // 256 % 3]
         c.K = synth.round_through(c.K * scale[None, :, None], dtype)
     say(f"       {c.check_some(sequences, nodes):.3f} of the bound")
+
+
+@pytest.mark.parametrize("dtype,d_k", [("bf16", 8), ("f32", 4)])
+@pytest.mark.parametrize("N", [3, 6, 9, 12, 17, 24])
+@pytest.mark.parametrize("far", [False, True])
+def test_a_slot_a_sequence_over_many_steps(N, dtype, d_k, far):
+    """More sequences than half the compute units: none is cut, whatever its length.  One to eight query tiles a wave, up to 15 steps of 64 rows."""
+    B, H, T = 130, 5, 900
+    say(f"[case] tree, a slot a sequence: B={B} N={N} H={H} d_k={d_k} T={T} {dtype} far={far}")
+    c = TreeCase(B, N, H, d_k, T, dtype, lens=[(901 - 53 * i) % 901 for i in range(B)], seed=600 + N, q_scale=40.0 if far else 1.5)
+    if far:
+        scale = np.array([0.02, 1.0, 0.3, 1.0])[np.arange(c.rows) // 256 % 4]
+        c.K = synth.round_through(c.K * scale[None, :, None], dtype)
+    say(f"       {c.check_some([0, 1, 2, 16, 17, 77, 129], [0, N // 2, N - 1]):.3f} of the bound")
