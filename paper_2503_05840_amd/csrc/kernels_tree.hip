@@ -946,6 +946,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
   constexpr int VEC = Elem<DT>::VEC;
   const int lane = threadIdx.x & 63, n16 = lane & 15, r = threadIdx.x >> 6, tile = blockIdx.x, b = blockIdx.z;
   __shared__ float weight[TREE_MAX_SPLITS][16];
+  __shared__ bool nothing[16];                             // an unused slot's row: its sums may be anything
   const int entry = a.plan[1 + a.slots + b], slot0 = entry / (2 * TREE_MAX_SPLITS), ns = entry % (2 * TREE_MAX_SPLITS);
   if (r == 0) {
     bool nan = false;                                      // (a node that sees a drafted key that is not finite)
@@ -963,6 +964,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
       const float w = sum == 0.f ? 0.f : (top == NEG_INF ? 1.f : exp2_of(a.sref[at + s * pitch] - top)) / sum;
       weight[s][n16] = nan ? __builtin_nanf("") : w;
     }
+    if (lane < 16) nothing[n16] = sum == 0.f && !nan;
   }
   lds_barrier();
   const int end = min(a.DB, (int)(blockIdx.y + 1) * per);
@@ -977,9 +979,11 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
       for (int hf = 0; hf < VEC / 4; ++hf) {
         const f32x4 x = C[s * pitch + hf * 64];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[hf * 4 + j] += w == 0.f ? 0.f : x[j] * w;      // (0: a row without weight, whose sum may be anything)
+        for (int j = 0; j < 4; ++j) v[hf * 4 + j] += x[j] * w;      // (a weight may vanish, but not a value that is not finite)
       }
     }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v[j] = nothing[n16] ? 0.f : v[j];
     store_operand<DT>(v, (u32x4*)a.Cop + (((size_t)b * a.MT + tile) * a.DB + blk) * VEC * 64 + r * (VEC / 4) * 64 + lane);
   }
 }
