@@ -310,6 +310,8 @@ int vanilla_attention_block(const void* x, const void* W_Q, const void* W_K, con
  * the keys are stored raw and rotated for the scores, q is taken as given, as in slim_decode.
  * Both layouts of opts->k_layout (t_stride % 32 == 0 for the banded one), any H and d_k of whole 16-byte vectors.
  * opts->variant and opts->wait_budget_us mean nothing to these calls: none of their kernels waits for another workgroup.
+ * They fill the chip, though, and the library does not order them: beside a bf16 fast-path call on another stream they can use up that call's
+ * waits (see slim_status), so the caller orders the two.
  * On a workspace that decode steps use too, what slim_status says of the latest of those stays.
  * They allocate nothing when given a workspace, and may be captured. */
 
@@ -321,6 +323,8 @@ int vanilla_attention_block(const void* x, const void* W_Q, const void* W_K, con
  *   out     : device dtype [B][N][d]   concat of heads, written; zeros for unused slots
  * q and out have the cache's type (slim_decode's are fp32): N rows a sequence are inputs and outputs of matrix products.  Scores,
  * softmax sums and weighted sums are fp32; the softmax numerators are rounded to dtype where they enter the weighted sum.
+ * (With a bf16 cache the result is off by 2.3e-3 of its norm, against 1.7e-3 of an fp32 computation that is rounded once.)  For trees of one node
+ * slim_decode is the call: it keeps q in fp32 and takes two thirds of the time (1 x 777 rows x 32 x 128: 22 us against 37).
  * A drafted key that is not finite makes NaN of the nodes that see it and changes nothing for the others.
  * The same batch gives the same bits; one of other lengths may cut a sequence's rows otherwise and sum them in another order.
  * opts->stage_ms: scores, weighted sum, projection.  Scratch: slim_workspace_bytes_tree (0 on invalid arguments), else library-owned. */

@@ -427,7 +427,8 @@ __global__ __launch_bounds__(1024 / TS) void tree_scores_kernel(TreeArgs a) {
 // head's queries resident as operands (heads of up to four steps: 128 columns in bf16, 64 in fp32) and the next block's keys in flight
 // while this one's are scored.  One barrier a block, for the maxima; the sums of a block are put together behind the next one's, and its
 // numerators stored behind the wait for the next one's keys, which would else be a wait for them as well.  Blocks of context alone need
-// no mask.  8 x 64 nodes x 4096 x 32 x 128: 96 us, of which K (270 MB) would take 55 at a copy's rate; 1 x 26 x 16384 42.
+// no mask.  8 x 64 nodes x 4096 x 32 x 128: 97 us, of which K (270 MB) would take 55 at a copy's rate; 1 x 26 x 16384 43.  (A workgroup's range is cut by T, not
+// by the sequence's length: one short sequence of a large T is walked by few workgroups.)
 // ------------------------------------------------------------------------------------------------
 template <int DT, int MAXT>
 __global__ __launch_bounds__(512, 1) void tree_scores_stream_kernel(TreeArgs a, int per) {
@@ -649,7 +650,9 @@ __device__ __forceinline__ u32x4 lowered(u32x4 p, float e) {
 // 16 VEC columns of K (128 in bf16) and NT tiles of 16 query rows; a workgroup's four waves, one per SIMD, are four neighbouring column blocks
 // of the same query rows.  K goes from memory to the wave's registers and is transposed there (no other wave of the workgroup needs it), RK
 // steps of 64 rows ahead; the numerators are the same for the four waves and go through LDS, a step ahead, one barrier a step.  Bound by the matrix cores and
-// what has to be issued beside them: 8 x 64 nodes x 4096 x 32 x 128 498 us, 1.10 PFLOP/s (a library product of 8192^3: 1.08), 54 % of their cycles.
+// what has to be issued beside them: 8 x 64 nodes x 4096 x 32 x 128 508 us (479 to
+// 563), 1.10 PFLOP/s (a library product of 8192^3: 1.08 to 1.16 from run to run), 54 % of their cycles.  With eight tiles in bf16 the epilogue, not the loop, keeps 92 bytes
+// a lane in scratch.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int NT> struct Weighted {
   static constexpr int VEC = Elem<DT>::VEC, CH = 4 * VEC, SC = TREE_STEP / CH;    // chunks of a step
@@ -860,7 +863,7 @@ __global__ __launch_bounds__(256, 1) void tree_weighted_kernel(TreeArgs a) {
     }
 #pragma unroll
     for (int r = 0; r < rows; ++r)
-      if (cc == (slots < VEC ? slots + r * (VEC - slots) / rows : VEC - 1)) next[j0 * VEC / 4 + r] = load_row(j0 * VEC / 4 + r);
+      if (cc == (slots < VEC ? slots + r * (VEC - slots) / (rows ? rows : 1) : VEC - 1)) next[j0 * VEC / 4 + r] = load_row(j0 * VEC / 4 + r);
     // fragments parked beside this tile
     constexpr int i0 = PF * at / (TILES - AHEAD), i1 = at < TILES - AHEAD ? PF * (at + 1) / (TILES - AHEAD) : i0;
 #pragma unroll
@@ -992,7 +995,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int per) {
 // Projection: out[i, h] = C[h N + i] W_KV[:, h].  A workgroup of four waves, one per SIMD, takes one head (or 16 VEC columns of one), NM of the query
 // tiles that hold rows of it (of any sequence) and a range of rows of W_KV, which the waves share out 4 VEC at a time; what they load lies
 // RD turns ahead in registers, and their sums meet in LDS.  1 x 1 node x 32 x 128: W_KV (33.5 MB) in 13 us, 2.5 TB/s, half of it the start and the end;
-// 8 x 64 73 us, C read once for every head that has rows in a tile.
+// 8 x 64 71 us, C read once for every head that has rows in a tile.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int NM>
 __global__ __launch_bounds__(256, 1) void tree_project_kernel(TreeArgs a) {
@@ -1118,7 +1121,7 @@ void launch_tree_scores_s(const TreeArgs& a, hipStream_t st) {
   else hipLaunchKernelGGL((tree_scores_kernel<DT, ROPE, TS, 5>), grid, block, 0, st, a);
 }
 // Two score tiles a wave and twice the waves where a wave of four keeps more than two query tiles' sums, 200 registers: 16 x 21 nodes x 1504 x 20 x 64
-// 104.9 -> 99.0 us for the call, 4 x 40 x 8000 x 12 x 72 110.5 -> 105.8; of two query tiles 319.6 -> 336.3 (24 x 5 x 6000 x 16 x 128), 157.5 -> 161.3 (8 x 16 x
+// 104.9 -> 99.0 us for the call, 4 x 40 x 8000 x 12 x 72 113.9 -> 107.8; of two query tiles 319.6 -> 336.3 (24 x 5 x 6000 x 16 x 128), 157.5 -> 161.3 (8 x 16 x
 // 3000 x 32 x 80).  And for rotary keys, with two tiles 72 -> 70 (8 x 16 x 5000 x 24 x 96; cos and sin asked for together with the keys 88).
 template <int DT, bool ROPE>
 void launch_tree_scores_w(const TreeArgs& a, hipStream_t st) {
