@@ -182,7 +182,7 @@ def _quantised(x, bits):
     amax = g.abs().amax(-1)
     sound = torch.isfinite(g).all(-1)
     f, e = torch.frexp(torch.where(sound, amax, torch.ones_like(amax)))         # amax = f 2^e, 0.5 <= f < 1
-    s = (e - 1 + (f > 0.875).int() - emax).clamp(min=-127)
+    s = (e - 1 + (f > 0.875).int() - emax).clamp(min=-127, max=127 - emax)
     s = torch.where(amax == 0, torch.full_like(s, -127), s)
     a, b = _pow2(-s, torch.float32)
     y = g.abs() * a[..., None] * b[..., None]
@@ -416,7 +416,8 @@ def _nearest(x, bits):
     e = torch.floor(torch.log2(amax.clamp(min=1e-300)))
     e = torch.where(2.0 ** e > amax, e - 1, torch.where(2.0 ** (e + 1) <= amax, e + 1, e))
     e = torch.where(amax > 1.75 * 2.0 ** e, e + 1, e)
-    unit = 2.0 ** (e - (2 if bits == 4 else 8)).clamp(min=-127)
+    top = 2 if bits == 4 else 8
+    unit = 2.0 ** (e - top).clamp(min=-127, max=127 - top)
     y = (g.abs() / unit).clamp(max=float(grid[-1]))
     hi = torch.searchsorted(grid, y.contiguous()).clamp(max=len(grid) - 1)
     lo = (hi - 1).clamp(min=0)
