@@ -359,6 +359,68 @@ int slim_tree_verify(const int32_t* tokens, const int32_t* parents, const void* 
 int slim_tree_commit(void* Kcache, const int32_t* path, const int32_t* n_path, int32_t* new_lens, int B, int N, int H, int T, int d,
                      const slim_opts* opts);
 
+/* ---- K-caches in 4 or 8 bits ------------------------------------------------------------------- */
+
+/* A K-cache whose rows are quantised as they are written: half or a quarter of a bf16 cache's bytes for the step that reads all of it.
+ *   format : groups of 32 columns of a row share a power of two 2^s, an element is an e2m1 (SLIM_Q4: 0, 0.5, 1, 1.5, 2, 3, 4, 6) or e4m3 (SLIM_Q8: up
+ *            to 448) value times it.  s is the exponent of the group's largest magnitude, one more where its significand is over 1.75, less
+ *            2 (Q4) or 8 (Q8), from -127 to 125 or 119; elements are rounded to the nearest value, ties to the even code, magnitudes over the
+ *            largest value to that.  A group with a NaN or an infinity is NaN as a whole.
+ *   codes  : device [B][t_stride][d * bits / 8] bytes; of a 4-bit row byte j holds column 2 j in its low half
+ *   scales : device [B][d / 32][t_stride] bytes, s + 127, 255 for NaN: the scales of consecutive rows are neighbours
+ * d % 32 == 0.  t_stride counts rows kept a sequence, a multiple of 64 (SLIM_ERR_LAYOUT otherwise); opts->t_stride 0 => T up to the next one.  Rows behind a
+ * sequence's length may hold anything.  opts->k_layout is SLIM_ERR_ARG but for SLIM_K_ROWMAJOR; opts->variant and opts->wait_budget_us mean nothing
+ * to these calls: none of their kernels waits for another workgroup.  (They fill the chip, and the library does not order them: see the drafted trees above.)
+ * They allocate nothing when given a workspace, and may be captured; calls that may overlap need a workspace each. */
+#define SLIM_Q4 4
+#define SLIM_Q8 8
+
+/* New rows into the caches.
+ *   rows    : device dtype, n_rows rows of d elements, `pitch` elements apart (0 => d; a multiple of 16 bytes): the sequences' new rows one after the other
+ *   cu_rows : device int32 [B + 1], nullable: sequence b brings rows [cu_rows[b], cu_rows[b + 1]); null: n_rows / B each (n_rows % B == 0)
+ *   opts->seq_lens : device int32 [B], rows that sequence b holds before the call, nullable => none; the new ones go behind them
+ * Rows that would come to lie at or behind T, and packed rows of no sequence, are not written.  No scratch.  opts->rope_table: SLIM_ERR_ARG (keys are
+ * stored raw).  opts->stage_ms: one figure. */
+int slim_quant_append(const void* rows, const int32_t* cu_rows, void* codes, void* scales, int B, int n_rows, int T, int d, int bits,
+                      int64_t pitch, const slim_opts* opts);
+
+/* The way back, with the same arguments: rows [seq_lens[b], ...) of the caches to packed rows, the values they stand for (exact in both types but for magnitudes
+ * under 2^-126).  Packed rows of no sequence stay as they are; those that would come from at or behind T are zeros. */
+int slim_quant_read(const void* codes, const void* scales, const int32_t* cu_rows, void* rows, int B, int n_rows, int T, int d, int bits,
+                    int64_t pitch, const slim_opts* opts);
+
+/* eq. 7 option 2 for B sequences, one new token each, over such a cache: slim_decode on the values that the codes stand for.
+ *   q    : device dtype [B][d]      projected, un-scaled queries
+ *   W_KV : device dtype [d][d]
+ *   out  : device dtype [B][d]      concat of heads, written
+ * Lengths from 0 (its result is zeros) to T; d_k a multiple of 8 up to 512, H <= 1024.  q and out have the weights' type, as in slim_tree_decode.  Scores, softmax sums
+ * and weighted sums are fp32; with bf16 weights the softmax numerators are rounded to bf16 where they enter the weighted sum.  opts->rope_table ([T][d_k/2][2]):
+ * as in slim_decode.  A row of the context that is not finite makes NaN of the results of its sequence.  The same batch gives the same bits.
+ * opts->stage_ms: scores, weighted sum, projection.  Scratch: slim_workspace_bytes_quant (0 on invalid arguments), else library-owned. */
+size_t slim_workspace_bytes_quant(int B, int H, int T, int d, int bits, int dtype);
+int slim_quant_decode(const void* q, const void* codes, const void* scales, const void* W_KV, void* out, int B, int H, int T, int d, int bits,
+                      const slim_opts* opts);
+
+/* ---- attention over whole prompts ------------------------------------------------------------------ */
+
+/* The step before the first generated token, for sequences packed one after the other (the paper's prompt phase: keys and values are at hand there, so
+ * it is eq. 2 as it stands; only K is kept for the steps that follow):
+ *   out_i,h = sum_j softmax_j(q_i,h k_j,g / sqrt(d_k)) v_j,g,   g = h / (H / H_kv)
+ *   q : device dtype, rows_q rows of H * d_k elements, q_pitch elements apart (0 => dense; a multiple of 16 bytes)
+ *   k, v : device dtype, rows_k rows of H_kv * d_k elements, k_pitch and v_pitch elements apart (q, k and v may be columns of one buffer)
+ *   cu_q, cu_k : device int32 [B + 1], increasing: sequence b has query rows [cu_q[b], cu_q[b + 1]) and key rows [cu_k[b], cu_k[b + 1]);
+ *            cu_k null => cu_q (rows_k == rows_q)
+ *   causal : non-zero: query i of n_q sees keys j <= i + n_k - n_q, so that the last query sees all (a prompt in pieces: the queries are the last rows);
+ *            0: every query sees every key of its sequence (encoders, cross-attention)
+ *   out : device dtype [rows_q][H * d_k], dense; zeros for a query that sees no key; rows of no sequence stay as they are
+ * H % H_kv == 0; d_k whole 16-byte vectors up to 256.  Offsets are clamped to the rows there are.  Rotary positions are the caller's (opts->rope_table,
+ * seq_lens, t_stride and k_layout: SLIM_ERR_ARG).  Scores and sums are fp32; bf16 numerators are rounded where they enter the product with v.  Keys and values that
+ * a query does not see have no effect on it, whatever they hold.  The same call gives the same bits.  opts->stage_ms: one figure.
+ * Scratch (few queries over many keys only): slim_workspace_bytes_prompt (0 on invalid arguments), else library-owned. */
+size_t slim_workspace_bytes_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dtype);
+int slim_prompt_attention(const void* q, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_k, void* out, int B, int rows_q,
+                          int rows_k, int H, int H_kv, int d_k, int causal, int64_t q_pitch, int64_t k_pitch, int64_t v_pitch, const slim_opts* opts);
+
 #ifdef __cplusplus
 }
 #endif

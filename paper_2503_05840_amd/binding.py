@@ -20,13 +20,16 @@ SLIM_F32, SLIM_BF16 = 0, 1
 VARIANT_AUTO, VARIANT_GENERIC, VARIANT_FUSED_SPLIT, VARIANT_FUSED = 0, 1, 2, 3
 VARIANT_VIA_MEMORY, VARIANT_APART = 0x100, 0x200      # for tests, added to a variant
 K_ROWMAJOR, K_BANDED = 0, 1       # slim_opts.k_layout
+QUANT_GROUP, QUANT_ROWS = 32, 64  # columns that share a scale; rows kept a sequence are a multiple
 DTYPES = {"f32": SLIM_F32, "bf16": SLIM_BF16}
 
 EXPORTS = ("slim_strerror", "slim_prepare_wkv", "slim_prepare_wkv_nonsquare", "slim_pack_weights", "slim_rope_table", "slim_workspace_bytes",
            "slim_workspace_bytes_xcache", "slim_workspace_bytes_block", "slim_attention_block", "vanilla_attention_block",
            "slim_variant_for", "slim_decode", "vanilla_kv_decode", "slim_decode_xcache", "slim_init", "slim_status",
            "slim_read_probe", "slim_decode_static", "slim_static_scratch_bytes", "slim_band_kcache",
-           "slim_workspace_bytes_tree", "slim_tree_decode", "slim_tree_verify", "slim_tree_commit")
+           "slim_workspace_bytes_tree", "slim_tree_decode", "slim_tree_verify", "slim_tree_commit",
+           "slim_quant_append", "slim_quant_read", "slim_workspace_bytes_quant", "slim_quant_decode", "slim_workspace_bytes_prompt",
+           "slim_prompt_attention")
 VARIANT_NAMES = {1: "generic", 2: "fused_split", 3: "fused"}
 
 
@@ -118,6 +121,18 @@ def load():
     lib.slim_tree_verify.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, op]
     lib.slim_tree_commit.restype = ci
     lib.slim_tree_commit.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, op]
+    i64 = ctypes.c_int64
+    for name in ("slim_quant_append", "slim_quant_read"):
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, i64, op]
+    lib.slim_workspace_bytes_quant.restype = ctypes.c_size_t
+    lib.slim_workspace_bytes_quant.argtypes = [ci, ci, ci, ci, ci, ci]
+    lib.slim_quant_decode.restype = ci
+    lib.slim_quant_decode.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, op]
+    lib.slim_workspace_bytes_prompt.restype = ctypes.c_size_t
+    lib.slim_workspace_bytes_prompt.argtypes = [ci, ci, ci, ci, ci, ci, ci]
+    lib.slim_prompt_attention.restype = ci
+    lib.slim_prompt_attention.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, i64, i64, i64, op]
     lib.slim_read_probe.restype = ci
     lib.slim_read_probe.argtypes = [vp, ctypes.c_size_t, vp]
     _lib = lib
@@ -205,6 +220,14 @@ def slim_workspace_bytes_block(B, H, T, d, dtype: str) -> int:
 
 def slim_workspace_bytes_tree(B, N, H, T, d, dtype: str) -> int:
     return int(load().slim_workspace_bytes_tree(B, N, H, T, d, DTYPES[dtype]))
+
+
+def slim_workspace_bytes_quant(B, H, T, d, bits: int, dtype: str) -> int:
+    return int(load().slim_workspace_bytes_quant(B, H, T, d, bits, DTYPES[dtype]))
+
+
+def slim_workspace_bytes_prompt(B, rows_q, rows_k, H, H_kv, d_k, dtype: str) -> int:
+    return int(load().slim_workspace_bytes_prompt(B, rows_q, rows_k, H, H_kv, d_k, DTYPES[dtype]))
 
 
 def auto_variant_name(B, H, T, d, dtype: str) -> str:
@@ -449,3 +472,107 @@ def slim_tree_commit(Kcache, path, n_path, new_lens, B, N, H, T, d, dtype="bf16"
     if rc != SLIM_OK:
         raise SlimError(rc, "slim_tree_commit")
     return new_lens
+
+
+# ---- K-caches in 4 or 8 bits, and prompts ----------------------------------------------------
+def _rows_ptr(t, rows, width, dtype, what):
+    """The address (null where there are no rows) and pitch in elements of a device tensor of `rows` rows of `width` elements, which may be columns of a wider one."""
+    if t.dim() != 2 or tuple(t.shape) != (rows, width) or t.dtype != _element(dtype) or not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor ({rows}, {width}) {dtype}, got {tuple(t.shape)} {t.dtype}")
+    if rows == 0:
+        return None, width
+    if (width > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < width):
+        raise ValueError(f"{what}: rows must be contiguous and apart")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else width)
+
+
+def _one_device(*tensors):
+    """Kernels run on the current device, on its current stream."""
+    import torch
+    on = {t.device.index for t in tensors if t is not None and t.is_cuda}
+    if on and on != {torch.cuda.current_device()}:
+        raise ValueError("tensors must be on the current device")
+
+
+def _offsets_ptr(cu, B, what):
+    import torch
+    return None if cu is None else _tree_ptr(cu, (B + 1,), torch.int32)
+
+
+def _quant_ptrs(codes, scales, B, T, d, bits, t_stride):
+    import torch
+    stride = int(t_stride or 0) or (T + QUANT_ROWS - 1) // QUANT_ROWS * QUANT_ROWS
+    return (_tree_ptr(codes, (B, stride, d * bits // 8), torch.uint8), _tree_ptr(scales, (B, d // QUANT_GROUP, stride), torch.uint8))
+
+
+def slim_quant_cache(B, T, d, bits, t_stride=0):
+    """New codes and scales for a cache of T rows a sequence on the current device: (codes, scales), zeros."""
+    import torch
+    stride = int(t_stride or 0) or (T + QUANT_ROWS - 1) // QUANT_ROWS * QUANT_ROWS
+    return (torch.zeros((B, stride, d * bits // 8), dtype=torch.uint8, device="cuda"),
+            torch.zeros((B, d // QUANT_GROUP, stride), dtype=torch.uint8, device="cuda"))
+
+
+def slim_quant_append(rows, codes, scales, B, T, d, bits, cu_rows=None, dtype="bf16", seq_lens=None, seq_lens_host=None, t_stride=0, stage_ms=None):
+    """Packed new rows (n, d), quantised behind the seq_lens[b] rows that each cache holds; cu_rows (B + 1,) int32, None: n / B rows each."""
+    _lens_ok(seq_lens, seq_lens_host, B)
+    _one_device(rows, codes, scales, cu_rows, seq_lens)
+    n = rows.shape[0]
+    at, pitch = _rows_ptr(rows, n, d, dtype, "rows")
+    ptrs = (at, _offsets_ptr(cu_rows, B, "cu_rows"), *_quant_ptrs(codes, scales, B, T, d, bits, t_stride))
+    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, None, VARIANT_AUTO, stage_ms)
+    rc = load().slim_quant_append(*ptrs, B, n, T, d, bits, pitch, ctypes.byref(o))
+    if rc != SLIM_OK:
+        raise SlimError(rc, "slim_quant_append")
+    return codes, scales
+
+
+def slim_quant_read(codes, scales, rows, B, T, d, bits, cu_rows=None, dtype="bf16", seq_lens=None, seq_lens_host=None, t_stride=0, stage_ms=None):
+    """The way back: the caches' rows from seq_lens[b] on (None: the first ones) to packed rows (n, d)."""
+    _lens_ok(seq_lens, seq_lens_host, B)
+    _one_device(rows, codes, scales, cu_rows, seq_lens)
+    n = rows.shape[0]
+    at, pitch = _rows_ptr(rows, n, d, dtype, "rows")
+    ptrs = (*_quant_ptrs(codes, scales, B, T, d, bits, t_stride), _offsets_ptr(cu_rows, B, "cu_rows"), at)
+    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, None, VARIANT_AUTO, stage_ms)
+    rc = load().slim_quant_read(*ptrs, B, n, T, d, bits, pitch, ctypes.byref(o))
+    if rc != SLIM_OK:
+        raise SlimError(rc, "slim_quant_read")
+    return rows
+
+
+def slim_quant_decode(q, codes, scales, W_KV, out, B, H, T, d, bits, dtype="bf16", seq_lens=None, seq_lens_host=None, t_stride=0, workspace=None,
+                      stage_ms=None, rope_table=None):
+    """The decode step over a cache in 4 or 8 bits: q, out (B, d), W_KV (d, d), all of `dtype`."""
+    import torch
+    el = _element(dtype)
+    _lens_ok(seq_lens, seq_lens_host, B)
+    _one_device(q, codes, scales, W_KV, out, seq_lens, workspace, rope_table)
+    if rope_table is not None and (rope_table.dtype != torch.float32 or rope_table.numel() < T * (d // H)):
+        raise ValueError("rope_table must be float32 and hold T positions")
+    if workspace is not None:
+        _dev_ptr(workspace)
+    ptrs = (_tree_ptr(q, (B, d), el), *_quant_ptrs(codes, scales, B, T, d, bits, t_stride), _tree_ptr(W_KV, (d, d), el), _tree_ptr(out, (B, d), el))
+    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, workspace, VARIANT_AUTO, stage_ms, rope_table)
+    rc = load().slim_quant_decode(*ptrs, B, H, T, d, bits, ctypes.byref(o))
+    if rc != SLIM_OK:
+        raise SlimError(rc, "slim_quant_decode")
+    return out
+
+
+def slim_prompt_attention(q, k, v, cu_q, out, B, H, H_kv, d_k, cu_k=None, causal=True, dtype="bf16", workspace=None, stage_ms=None):
+    """Attention over packed prompts: q (rows_q, H d_k), k and v (rows_k, H_kv d_k), possibly columns of one buffer; out (rows_q, H d_k); cu_q, cu_k (B + 1,)."""
+    rows_q, rows_k = q.shape[0], k.shape[0]
+    _one_device(q, k, v, out, cu_q, cu_k, workspace)
+    (qp, q_pitch), (kp, k_pitch), (vp, v_pitch) = (_rows_ptr(t, r, w * d_k, dtype, n)
+                                                   for t, r, w, n in ((q, rows_q, H, "q"), (k, rows_k, H_kv, "k"), (v, rows_k, H_kv, "v")))
+    if workspace is not None:
+        _dev_ptr(workspace)
+    if cu_q is None:
+        raise ValueError("cu_q: the offsets of the sequences are needed")
+    ptrs = (qp, kp, vp, _offsets_ptr(cu_q, B, "cu_q"), _offsets_ptr(cu_k, B, "cu_k"), _tree_ptr(out, (rows_q, H * d_k), _element(dtype)))
+    o, keep = _opts(dtype, None, None, 0, workspace, VARIANT_AUTO, stage_ms)
+    rc = load().slim_prompt_attention(*ptrs, B, rows_q, rows_k, H, H_kv, d_k, int(causal), q_pitch, k_pitch, v_pitch, ctypes.byref(o))
+    if rc != SLIM_OK:
+        raise SlimError(rc, "slim_prompt_attention")
+    return out

@@ -1,0 +1,293 @@
+// Attention over whole prompts in bf16: causal or full, grouped heads, packed sequences.
+#include "prompt_common.h"
+
+namespace slim {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int PQ = 128, PK = 64;               // queries of a workgroup (32 a wave), keys of a tile
+
+// 16-byte pieces of a row in LDS: a power of two, so that they can be swapped among themselves by the row's number.  Keys are read with lanes on consecutive
+// rows, 16 bytes each; values with four rows x 32 bytes for every 16 lanes.  Either way the rows of one access shall lie in different banks.
+template <int DKP> struct Pitch { static constexpr int pieces = DKP <= 32 ? 4 : DKP <= 64 ? 8 : DKP <= 128 ? 16 : 32; };
+template <int PC> __device__ __forceinline__ int k_swap(int row) { return PC >= 16 ? row & 15 : PC == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
+template <int PC> __device__ __forceinline__ int v_swap(int row) { return PC >= 16 ? (row & 3) << 2 : PC == 8 ? (row & 2) << 1 : 0; }
+
+// One pass over the keys with a running reference and sum a query.  Products are 32x32x16: S^T = K Q^T, whose result has a query's scores in two lanes, so that
+// maxima and sums are the lane's own but for one exchange; its registers, rounded to bf16, are the operand of O^T += V^T P^T as they are, V's
+// operand being read in the same order of keys (transposed reads of four rows).
+template <int DKP>
+__global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
+  constexpr int PC = Pitch<DKP>::pieces, NS = DKP / 16, NV = DKP / 32;
+  __shared__ __align__(16) char tiles[2][2][PK * PC * 16];       // [buffer][keys, values]
+  PromptTile t;
+  if (!prompt_tile(a, PQ, t)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, half = lane >> 5;
+  const int hk = t.h / (a.H / a.H_kv);
+  const int i = min(t.i0 + wave * 32 + n, t.n_q - 1);          // this lane's query (past the last: the last, not stored)
+  const int off = t.n_k - t.n_q;
+  const int sees = a.causal ? i + off : t.n_k - 1;               // its last key
+  const int wave_first = a.causal ? min(t.i0 + wave * 32, t.n_q - 1) + off : t.n_k - 1;
+  const int wave_last = a.causal ? min(t.i0 + wave * 32 + 31, t.n_q - 1) + off : t.n_k - 1;
+  const int end = a.causal ? min(t.i0 + PQ, t.n_q) + off : t.n_k;     // keys that the workgroup needs
+  const int all = end > 0 ? (end + PK - 1) / PK : 0, per = (all + a.nsplit - 1) / a.nsplit;
+  const int tile0 = t.split * per, tile1 = min(tile0 + per, all);
+  const bool clear = a.d_k < PC * 8;
+
+  const uint16_t* K = (const uint16_t*)a.k + t.k0 * a.k_pitch + (long)hk * a.d_k;
+  const uint16_t* V = (const uint16_t*)a.v + t.k0 * a.v_pitch + (long)hk * a.d_k;
+  if (clear) {                                                     // pieces past d_k: zeros that nothing is loaded over
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    for (int x = tid; x < 4 * PK * PC; x += 256) ((u32x4*)tiles)[x] = zero;
+    __syncthreads();
+  }
+  const int pieces = a.d_k / 8;
+  auto load = [&](int tile, int buf) {
+    const int key0 = tile * PK;
+#pragma unroll
+    for (int x = 0; x < PK * PC / 256; ++x) {
+      const int at = (x * 4 + wave) * 64 + lane, row = at / PC, place = at % PC;
+      const long key = min(key0 + row, t.n_k - 1);                 // (rows past the last are masked)
+      const int ck = place ^ k_swap<PC>(row), cv = place ^ v_swap<PC>(row);
+      if (!clear || ck < pieces) load_to_lds(K + key * a.k_pitch + ck * 8, lds_address(tiles[buf][0]) + (x * 4 + wave) * 1024);
+      if (!clear || cv < pieces) load_to_lds(V + key * a.v_pitch + cv * 8, lds_address(tiles[buf][1]) + (x * 4 + wave) * 1024);
+    }
+  };
+
+  bf16x8 q[NS];
+  {
+    const uint16_t* src = (const uint16_t*)a.q + (t.q0 + i) * a.q_pitch + (long)t.h * a.d_k;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int c = s * 16 + half * 8;
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (c < a.d_k) x = *(const u32x4*)(src + c);
+      q[s] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  f32x16 o[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[v][r] = 0.f;
+  float ref = NEG_INF, sum = 0.f;
+
+  if (tile0 < tile1) load(tile0, 0);
+  for (int tile = tile0; tile < tile1; ++tile) {
+    const int buf = (tile - tile0) & 1, key0 = tile * PK;
+    tiles_barrier();
+    if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
+    if (key0 > wave_last) continue;
+    const char* kt = tiles[buf][0];
+    const char* vt = tiles[buf][1];
+    f32x16 s[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
+      const int row = x * 32 + n;
+#pragma unroll
+      for (int k = 0; k < NS; ++k) {
+        const bf16x8 A = *(const bf16x8*)(kt + (row * PC + ((2 * k + half) ^ k_swap<PC>(row))) * 16);
+        s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, q[k], s[x], 0, 0, 0);
+      }
+    }
+    const bool masked = key0 + PK - 1 > wave_first;
+    unsigned long long bad = 0;                                  // rows of values that are not finite, where some queries do not see all rows
+    if (masked) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key0 + x * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > sees) s[x][r] = NEG_INF;
+      u16x2 top = {0, 0};
+#pragma unroll
+      for (int c = 0; c < PC; ++c) {
+        const u32x4 v = *(const u32x4*)(vt + (lane * PC + (c ^ (lane & (PC - 1)))) * 16);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[y] & 0x7fff7fffu));
+      }
+      bad = __ballot(top[0] >= 0x7f80 || top[1] >= 0x7f80);
+    }
+    float m = NEG_INF;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) m = fmaxf(m, s[x][r]);
+    m = max_of_halves(m) * a.scale;
+    // The reference moves only when a score leaves it 2^8 behind: numerators up to that are as exact, and the sums have room for them.
+    if (__any(m > ref + 8.f)) {
+      const float to = fmaxf(ref, m);
+      const float f = to == NEG_INF ? 1.f : exp2f(ref - to);
+      ref = to;
+      sum *= f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[v][r] *= f;
+    }
+    const float base = ref == NEG_INF ? 0.f : ref;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -base));
+        sum += s[x][r];
+      }
+    const int tr_row = 4 * half + ((lane & 15) >> 2), tr_col = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;      // (bytes)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      bf16x8 p;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[r] = (__bf16)s[k >> 1][(k & 1) * 8 + r];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        u32x4 A;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int row = k * 16 + g * 8 + tr_row, byte = v * 64 + tr_col;
+          const char* at = vt + (row * PC + ((byte >> 4) ^ v_swap<PC>(row))) * 16 + (byte & 15);
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+          A[2 * g] = x[0];
+          A[2 * g + 1] = x[1];
+        }
+        if (bad) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (bad >> (k * 16 + (e >> 2) * 8 + 4 * half + (e & 3)) & 1) A[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
+        }
+        o[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, A), p, o[v], 0, 0, 0);
+      }
+    }
+    // A row with a value that is not finite goes to the queries that see it one by one.
+    while (bad) {
+      const int row = __ffsll((long long)bad) - 1;
+      bad &= bad - 1;
+      const int reg = (row >> 5) * 16 + ((row & 31) >> 3) * 4 + (row & 3);
+      float p = 0.f;
+#pragma unroll
+      for (int x = 0; x < 32; ++x) p = x == reg ? s[x >> 4][x & 15] : p;
+      p = __shfl(p, n + 32 * ((row >> 2) & 1));
+      if (key0 + row <= sees) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int c = v * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+            const uint16_t x = *(const uint16_t*)(vt + (row * PC + ((c >> 3) ^ v_swap<PC>(row))) * 16 + (c & 7) * 2);
+            o[v][r] = fmaf(p, __uint_as_float((unsigned)x << 16), o[v][r]);
+          }
+      }
+    }
+  }
+  sum = sum_of_halves(sum);
+  if (t.i0 + wave * 32 + n >= t.n_q) return;
+  const long row = (t.q0 + i) * a.H + t.h;
+  if (a.nsplit > 1) {
+    if (half == 0) {
+      float* ml = a.ml + ((long)t.split * a.rows_q * a.H + row) * 2;
+      ml[0] = ref;
+      ml[1] = sum;
+    }
+    float* dst = a.O + ((long)t.split * a.rows_q * a.H + row) * a.d_k;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int c = v * 32 + 8 * r + 4 * half;
+        if (c < a.d_k) *(f32x4*)(dst + c) = f32x4{o[v][4 * r], o[v][4 * r + 1], o[v][4 * r + 2], o[v][4 * r + 3]};
+      }
+    return;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;                // (no key: zeros)
+  uint16_t* dst = (uint16_t*)a.out + row * a.d_k;
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      const int c = v * 32 + 8 * r + 4 * half;
+      bf16x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (__bf16)(o[v][4 * r + e] * inv);
+      if (c < a.d_k) *(bf16x4*)(dst + c) = x;
+    }
+}
+
+// The splits of the keys joined: four columns a thread.  Rows of no sequence stay as they are.
+template <bool F32>
+__global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
+  const long x = (long)blockIdx.x * 256 + threadIdx.x, per = a.d_k / 4;
+  const long row = x / per, n = (long)a.rows_q * a.H;          // row: query * H + head
+  if (row >= n) return;
+  const int c = (int)(x % per) * 4, i = (int)(row / a.H);
+  int lo = 0, hi = a.B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.cu_q[mid] <= i) lo = mid; else hi = mid;
+  }
+  if (i < a.cu_q[lo] || i >= a.cu_q[lo + 1]) return;
+  float m = NEG_INF;
+  for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, a.ml[(s * n + row) * 2]);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  for (int s = 0; s < a.nsplit; ++s) {
+    const float r = a.ml[(s * n + row) * 2], l = a.ml[(s * n + row) * 2 + 1];
+    if (r == NEG_INF && l == 0.f) continue;                      // no key there
+    const float f = r == NEG_INF ? 1.f : exp2f(r - m);           // (keys that are not a number leave no reference)
+    const f32x4 y = *(const f32x4*)(a.O + (s * n + row) * a.d_k + c);
+    sum = fmaf(l, f, sum);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = fmaf(y[k], f, v[k]);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if constexpr (F32) {
+    *(f32x4*)((float*)a.out + row * a.d_k + c) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+  } else {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = (__bf16)(v[k] * inv);
+    *(bf16x4*)((uint16_t*)a.out + row * a.d_k + c) = y;
+  }
+}
+
+template <int DKP>
+void prompt_of(const PromptArgs& a, hipStream_t st) { prompt_kernel<DKP><<<prompt_grid(a, PQ), 256, 0, st>>>(a); }
+
+}  // namespace
+
+// Parts of the keys, where the queries alone do not fill the chip: a part has 256 keys at least.
+int prompt_splits(int dtype, int B, int rows_q, int rows_k, int H, int d_k) {
+  const int rows = dtype == DT_F32 ? PROMPT_F32_ROWS : PQ;
+  const long tiles = (long)B * ((rows_q / B + rows - 1) / rows) * H;      // (as if the sequences were equally long)
+  if (tiles < 1 || tiles >= 256) return 1;
+  const long want = 512 / tiles, keys = rows_k / B / 256;
+  long n = want < keys ? want : keys;
+  n = n > 32 ? 32 : n;
+  (void)d_k;
+  return n < 1 ? 1 : (int)n;
+}
+
+void launch_prompt(int dtype, const PromptArgs& a, hipStream_t st) {
+  if (dtype == DT_F32) launch_prompt_f32(a, st);
+  else if (a.d_k <= 32) prompt_of<32>(a, st);
+  else if (a.d_k <= 64) prompt_of<64>(a, st);
+  else if (a.d_k <= 96) prompt_of<96>(a, st);
+  else if (a.d_k <= 128) prompt_of<128>(a, st);
+  else if (a.d_k <= 192) prompt_of<192>(a, st);
+  else prompt_of<256>(a, st);
+}
+
+void launch_prompt_merge(int dtype, const PromptArgs& a, hipStream_t st) {
+  const long n = (long)a.rows_q * a.H * (a.d_k / 4);
+  const unsigned grid = (unsigned)((n + 255) / 256);
+  if (dtype == DT_F32) prompt_merge_kernel<true><<<grid, 256, 0, st>>>(a);
+  else prompt_merge_kernel<false><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace slim

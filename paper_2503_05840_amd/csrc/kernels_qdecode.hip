@@ -1,0 +1,669 @@
+// The decode step of slim attention over a K-cache in 4 or 8 bits (its format: kernels_quant.hip): scores, weighted sum of K, merge + projection through W_KV.
+// Three launches; none of their workgroups waits for another.  What a code stands for is exact in bf16, so that K enters both products without a rounding.
+#include "device_common.h"
+#include "slim_kernels.h"
+
+namespace slim {
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float scale_of(unsigned dw, int k) { return __uint_as_float(((dw >> (8 * k)) & 0xffu) << 23); }
+
+// Eight codes of a row: columns 2 k and 2 k + 1 as floats, or as a pair of bf16 (exact)
+template <int BITS> struct Codes8;
+template <> struct Codes8<4> {
+  unsigned w;
+  __device__ __forceinline__ void load(const unsigned char* p) { w = *(const unsigned*)p; }
+  template <int K> __device__ __forceinline__ f32x2 f32(float s) const { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, K); }
+  template <int K> __device__ __forceinline__ unsigned bf16(float s) const {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, K));
+  }
+};
+template <> struct Codes8<8> {
+  u32x2 w;
+  __device__ __forceinline__ void load(const unsigned char* p) { w = *(const u32x2*)p; }
+  template <int K> __device__ __forceinline__ f32x2 f32(float s) const { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[K >> 1], s, (K & 1) != 0); }
+  template <int K> __device__ __forceinline__ unsigned bf16(float s) const {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[K >> 1], s, (K & 1) != 0));
+  }
+};
+
+// ---- scores -------------------------------------------------------------------------------------------
+
+template <int STEP>
+__device__ __forceinline__ float from_partner(float v) {
+  if constexpr (STEP == 1) return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true));
+  else if constexpr (STEP == 2) return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true));
+  else if constexpr (STEP == 4) return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));     // 7 - lane
+  else if constexpr (STEP == 8) return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true));     // 15 - lane
+  else return __shfl_xor(v, STEP);
+}
+// Lane i of a head's P lanes gets the sum over these lanes of their v[i]: halves are exchanged from the widest step on.  (The mirrors that steps of
+// 4 and 8 use flip the lower bits too; whom they join still differs in the step's own bit, and in every round from everyone joined before.)
+template <int P>
+__device__ __forceinline__ float sums_to_lanes(float (&v)[P], int lane) {
+  if constexpr (P > 1) {
+    constexpr int S = P / 2;
+    float u[S];
+    const bool upper = (lane & S) != 0;
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      const float mine = upper ? v[k + S] : v[k], other = upper ? v[k] : v[k + S];
+      u[k] = mine + from_partner<S>(other);
+    }
+    return sums_to_lanes<S>(u, lane);
+  } else {
+    return v[0];
+  }
+}
+template <int P>
+__device__ __forceinline__ float max_over_lanes(float v) {
+  if constexpr (P > 1) { v = fmaxf(v, from_partner<P / 2>(v)); return max_over_lanes<P / 2>(v); }
+  else return v;
+}
+template <int P>
+__device__ __forceinline__ float sum_over_lanes(float v) {
+  if constexpr (P > 1) { v = v + from_partner<P / 2>(v); return sum_over_lanes<P / 2>(v); }
+  else return v;
+}
+
+// A wave takes 64 rows x 64 / P heads; a head is P lanes of eight columns (those past d_k are idle).  Rows go P at a time, lane i of a head ends with the
+// 64 / P consecutive rows from i * 64 / P on, and the scale bytes of all 64 rows are one run of a lane's group.  From the scores come softmax numerators relative
+// to a power of two per head and block: a whole exponent, so that a later change of reference is exact in every type.
+// HBM-bound (0.53 or 1.03 bytes an element); about 20 instructions a row and lane, 45 with rotated keys.
+template <bool F32, int BITS, int P, bool ROPE>
+__global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  {
+    const long wgs = (long)gridDim.x * gridDim.y * gridDim.z, wg = blockIdx.x + (long)gridDim.x * (blockIdx.y + (long)gridDim.y * blockIdx.z);
+    for (long i = wg * 256 + tid; i < a.ncounters; i += wgs * 256) a.counters[i] = 0;
+  }
+  const int b = blockIdx.z, t0 = blockIdx.x * QUANT_ROWS;
+  const int len = seq_len_of(a.seq_lens, b, a.T);
+  if (t0 >= len) return;
+  constexpr int HW = 64 / P, RP = 64 / P;
+  const int h = (blockIdx.y * 4 + wave) * HW + lane / P, i = lane % P;
+  const bool on = h < a.H && i * 8 < a.d_k;
+  const int col = on ? h * a.d_k + i * 8 : 0;
+  float qf[8];
+  unsigned qb[4];
+  if constexpr (F32) {
+    const f32x4* src = (const f32x4*)((const float*)a.q + (long)b * a.d + col);
+    const f32x4 lo = src[0], hi = src[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { qf[j] = lo[j]; qf[4 + j] = hi[j]; }
+  } else {
+    const u32x4 v = *(const u32x4*)((const uint16_t*)a.q + (long)b * a.d + col);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { qb[j] = v[j]; qf[2 * j] = __uint_as_float(v[j] << 16); qf[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u); }
+  }
+  const unsigned char* codes = a.codes + ((long)b * a.stride + t0) * (a.d * BITS / 8) + col * BITS / 8;
+  const u32x4* sp = (const u32x4*)(a.scales + ((long)b * (a.d / 32) + col / 32) * a.stride + t0);
+  u32x4 sc[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sc[k] = sp[k];
+  const long row_bytes = a.d * BITS / 8;
+  float s[RP];
+  Codes8<BITS> w[2][P];
+  auto fetch = [&](int j, auto buf) {
+#pragma unroll
+    for (int r = 0; r < P; ++r) w[buf.value][r].load(codes + (long)(r * RP + j) * row_bytes);
+  };
+  auto step = [&](int j, auto J) {
+    constexpr int cur = decltype(J)::value & 1;
+    float v[P];
+#pragma unroll
+    for (int r = 0; r < P; ++r) {
+      const int row = r * RP + decltype(J)::value;
+      const float f = scale_of(sc[row >> 4][(row >> 2) & 3], row & 3);
+      const Codes8<BITS>& c = w[cur][r];
+      float x = 0.f;
+      if constexpr (ROPE) {
+        // (rows behind the sequence, whose score is masked, have no position in the table)
+        const f32x4* cs = (const f32x4*)(a.rope + ((long)min(t0 + row, len - 1) * (a.d_k / 2) + (on ? i * 4 : 0)) * 2);
+        const f32x4 t[2] = {cs[0], cs[1]};
+        auto pair = [&](auto K) {
+          constexpr int k = decltype(K)::value;
+          const f32x2 y = c.template f32<k>(f);
+          const float co = t[k >> 1][2 * (k & 1)], si = t[k >> 1][2 * (k & 1) + 1];
+          x = fmaf(qf[2 * k], fmaf(y[0], co, y[1] * si), x);
+          x = fmaf(qf[2 * k + 1], fmaf(y[1], co, -(y[0] * si)), x);
+        };
+        pair(std::integral_constant<int, 0>{}); pair(std::integral_constant<int, 1>{});
+        pair(std::integral_constant<int, 2>{}); pair(std::integral_constant<int, 3>{});
+      } else if constexpr (F32) {
+        auto pair = [&](auto K) {
+          constexpr int k = decltype(K)::value;
+          const f32x2 y = c.template f32<k>(f);
+          x = fmaf(qf[2 * k], y[0], x);
+          x = fmaf(qf[2 * k + 1], y[1], x);
+        };
+        pair(std::integral_constant<int, 0>{}); pair(std::integral_constant<int, 1>{});
+        pair(std::integral_constant<int, 2>{}); pair(std::integral_constant<int, 3>{});
+      } else {
+        auto pair = [&](auto K) {
+          constexpr int k = decltype(K)::value;
+          x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, c.template bf16<k>(f)), __builtin_bit_cast(bf16x2, qb[k]), x, false);
+        };
+        pair(std::integral_constant<int, 0>{}); pair(std::integral_constant<int, 1>{});
+        pair(std::integral_constant<int, 2>{}); pair(std::integral_constant<int, 3>{});
+      }
+      v[r] = on ? x : 0.f;
+    }
+    s[decltype(J)::value] = sums_to_lanes<P>(v, lane);
+  };
+  fetch(0, std::integral_constant<int, 0>{});
+  auto both = [&](int j, auto J) {
+    if constexpr (decltype(J)::value + 1 < RP) fetch(decltype(J)::value + 1, std::integral_constant<int, (decltype(J)::value + 1) & 1>{});
+    step(j, J);
+  };
+  full_steps<0, RP>(0, both);
+  // numerators
+  float m = NEG_INF;
+#pragma unroll
+  for (int j = 0; j < RP; ++j) {
+    s[j] = t0 + i * RP + j < len ? s[j] * a.qscale : NEG_INF;
+    m = fmaxf(m, s[j]);
+  }
+  m = max_over_lanes<P>(m);
+  const float ref = m == NEG_INF ? 0.f : ceilf(m);
+  float l = 0.f;
+  const long o = ((long)b * a.H + h) * a.Tp + t0 + i * RP;
+  float p[RP];
+#pragma unroll
+  for (int j = 0; j < RP; ++j) {
+    p[j] = exp2f(s[j] - ref);
+    if constexpr (!F32) p[j] = (float)(__bf16)p[j];       // rounded where it enters the product with K, and the sum is of what enters
+    l += p[j];
+  }
+  l = sum_over_lanes<P>(l);
+  if (h >= a.H) return;
+  if constexpr (F32) {
+#pragma unroll
+    for (int j = 0; j < RP; ++j) ((float*)a.P)[o + j] = p[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < RP; ++j) ((__bf16*)a.P)[o + j] = (__bf16)p[j];
+  }
+  if (i == 0) {
+    const long at = ((long)b * a.H + h) * a.NB + blockIdx.x;
+    a.ref[at] = ref;
+    a.sum[at] = l;
+  }
+}
+
+// ---- weighted sum of K ----------------------------------------------------------------------------------
+
+// A split's blocks of one sequence: [blk0, blk1), none where the sequence is shorter
+__device__ __forceinline__ bool split_blocks(const QDecodeArgs& a, int len, int split, int& blk0, int& blk1) {
+  const int nb = (len + QUANT_ROWS - 1) / QUANT_ROWS;
+  blk0 = split * a.per;
+  blk1 = min(blk0 + a.per, nb);
+  return blk0 < blk1;
+}
+
+// References of up to 32 heads for a split: the largest of its blocks, to LDS; the first column block notes them and the sums for the merge.
+// Eight threads a head.
+__device__ __forceinline__ void split_references(const QDecodeArgs& a, int b, int split, int blk0, int blk1, int h0, int nh, bool note, float* mref) {
+  const int tid = threadIdx.x, j = tid >> 3, k = tid & 7, h = h0 + j;
+  float m = NEG_INF, l = 0.f;
+  if (j < nh && h < a.H) {
+    const long at = ((long)b * a.H + h) * a.NB;
+    for (int blk = blk0 + k; blk < blk1; blk += 8) m = fmaxf(m, a.ref[at + blk]);
+  }
+  m = max_over_lanes<8>(m);
+  if (j < nh && h < a.H && note) {
+    const long at = ((long)b * a.H + h) * a.NB;
+    for (int blk = blk0 + k; blk < blk1; blk += 8) l += a.sum[at + blk] * exp2f(a.ref[at + blk] - m);
+  }
+  l = sum_over_lanes<8>(l);
+  if (k == 0 && j < nh) {
+    mref[j] = m;
+    if (note && h < a.H) {
+      const long at = ((long)b * a.nsplit + split) * a.H + h;
+      a.sref[at] = m;
+      a.ssum[at] = l;
+    }
+  }
+  __syncthreads();
+}
+
+template <int BITS> struct Codes16;              // 16 columns of a row
+template <> struct Codes16<4> { typedef u32x2 type; };
+template <> struct Codes16<8> { typedef u32x4 type; };
+template <int BITS, int K>
+__device__ __forceinline__ unsigned bf16_pair(const typename Codes16<BITS>::type& w, float s) {
+  if constexpr (BITS == 4) return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[K >> 2], s, K & 3));
+  else return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[K >> 1], s, (K & 1) != 0));
+}
+
+constexpr int QW_COLS = 256;                     // columns of a workgroup: 16 lanes x 16
+
+// C[h][c] = sum_t p[h][t] K[t][c] on 16x16x32 matrix instructions: rows are heads, the contraction is over 32 cache rows, a lane holds eight rows x 16 columns and
+// makes one column of operands after the other.  The four waves take every fourth 32 rows of the split and join through LDS in a fixed order.
+// Bound by HBM for the codes where a sequence is long.
+template <int BITS, int NT>
+__global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
+  typedef typename Codes16<BITS>::type W16;
+  __shared__ float mref[32];
+  __shared__ f32x4 join[4][NT * 4][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int ngroups = (a.H + 16 * NT - 1) / (16 * NT);
+  const int b = blockIdx.z / ngroups, h0 = blockIdx.z % ngroups * 16 * NT, split = blockIdx.y;
+  const int len = seq_len_of(a.seq_lens, b, a.T);
+  int blk0, blk1;
+  if (!split_blocks(a, len, split, blk0, blk1)) return;
+  split_references(a, b, split, blk0, blk1, h0, 16 * NT, blockIdx.x == 0, mref);
+  const int n = lane & 15, kg = lane >> 4;
+  const int c = blockIdx.x * QW_COLS + n * 16;
+  const int cc = min(c, a.d - 16);               // (columns past the row's end: anything, not stored)
+  float m[NT];
+  const uint16_t* P[NT];
+  const float* R[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int h = min(h0 + t * 16 + n, a.H - 1);  // (heads past the last: anything, not stored)
+    m[t] = mref[h - h0];
+    P[t] = (const uint16_t*)a.P + ((long)b * a.H + h) * a.Tp + kg * 8;
+    R[t] = a.ref + ((long)b * a.H + h) * a.NB;
+  }
+  const long row_bytes = a.d * BITS / 8;
+  const unsigned char* codes = a.codes + ((long)b * a.stride + kg * 8) * row_bytes + (long)cc * BITS / 8;
+  const unsigned char* scales = a.scales + ((long)b * (a.d / 32) + cc / 32) * a.stride + kg * 8;
+  f32x4 acc[NT][16];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int step1 = min(blk1 * 2, (len + 31) / 32);
+  struct Rows { W16 w[8]; u32x2 s; u32x4 p[NT]; float r[NT]; };
+  auto fetch = [&](int k, Rows& x) {
+    const long r0 = (long)k * 32;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.w[i] = *(const W16*)(codes + (r0 + i) * row_bytes);
+    x.s = *(const u32x2*)(scales + r0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) { x.p[t] = *(const u32x4*)(P[t] + r0); x.r[t] = R[t][k >> 1]; }
+  };
+  auto compute = [&](int k, Rows& x) {
+    if (k * 32 + 32 > len) {
+      // Rows behind the sequence may hold anything, and their numerators of zero would not make zero of a NaN.
+      const int left = len - k * 32 - kg * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= left) {
+          x.w[i] = W16{};
+          x.s[i >> 2] &= ~(0xffu << (8 * (i & 3)));
+        }
+    }
+    bf16x8 A[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      // relative to the split's reference: so many binades less
+      const unsigned sh = (unsigned)fminf(fmaxf(m[t] - x.r[t], 0.f), 255.f) << 7;
+      const u16x2 by = {(unsigned short)sh, (unsigned short)sh};
+      u32x4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned w = x.p[t][j];              // (a bit cast of the element itself takes the vector's first, whatever j is)
+        v[j] = __builtin_bit_cast(unsigned, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, w), by));
+      }
+      A[t] = __builtin_bit_cast(bf16x8, v);
+    }
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = scale_of(x.s[i >> 2], i & 3);
+    auto pair = [&](int, auto K) {
+      constexpr int kk = decltype(K)::value;
+      unsigned y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = bf16_pair<BITS, kk>(x.w[i], s[i]);
+      u32x4 lo, hi;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        lo[i] = __builtin_amdgcn_perm(y[2 * i + 1], y[2 * i], 0x05040100u);
+        hi[i] = __builtin_amdgcn_perm(y[2 * i + 1], y[2 * i], 0x07060302u);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        acc[t][2 * kk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[t], __builtin_bit_cast(bf16x8, lo), acc[t][2 * kk], 0, 0, 0);
+        acc[t][2 * kk + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[t], __builtin_bit_cast(bf16x8, hi), acc[t][2 * kk + 1], 0, 0, 0);
+      }
+    };
+    full_steps<0, 8>(0, pair);
+  };
+  Rows x0, x1;
+  int k = blk0 * 2 + wave;
+  if (k < step1) fetch(k, x0);
+  for (; k < step1; k += 8) {
+    if (k + 4 < step1) fetch(k + 4, x1);
+    compute(k, x0);
+    if (k + 4 >= step1) break;
+    if (k + 8 < step1) fetch(k + 8, x0);
+    compute(k + 4, x1);
+  }
+  // Wave w ends with operands 4 w .. 4 w + 3 of every tile: in three rounds each wave hands the quarter of another one over.
+  auto quarter = [&](int qd, auto f) {
+    if (qd == 0) f(std::integral_constant<int, 0>{});
+    else if (qd == 1) f(std::integral_constant<int, 1>{});
+    else if (qd == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 3>{});
+  };
+#pragma unroll 1
+  for (int r = 1; r < 4; ++r) {
+    quarter((wave + r) & 3, [&](auto Q) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) join[wave][t * 4 + j][lane] = acc[t][decltype(Q)::value * 4 + j];
+    });
+    __syncthreads();
+    quarter(wave, [&](auto Q) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[t][decltype(Q)::value * 4 + j] += join[(wave - r) & 3][t * 4 + j][lane];
+    });
+    __syncthreads();
+  }
+  if (c >= a.d) return;
+  quarter(wave, [&](auto Q) {
+    constexpr int q0 = decltype(Q)::value * 4;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int h = h0 + t * 16 + kg * 4 + i;
+        if (h >= a.H) continue;
+        *(f32x4*)(a.C + (((long)b * a.nsplit + split) * a.H + h) * a.d + c + q0) = f32x4{acc[t][q0][i], acc[t][q0 + 1][i], acc[t][q0 + 2][i], acc[t][q0 + 3][i]};
+      }
+  });
+}
+
+// The same in fp32 on the vector ALU: a thread has eight columns and eight heads, numerators are uniform.  For caches of layers that are kept in full precision.
+template <int BITS>
+__global__ __launch_bounds__(256) void qweighted_f32_kernel(QDecodeArgs a) {
+  __shared__ float mref[32];
+  __shared__ float join[3][64][65];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int ngroups = (a.H + 7) / 8;
+  const int b = blockIdx.z / ngroups, h0 = blockIdx.z % ngroups * 8, split = blockIdx.y;
+  const int len = seq_len_of(a.seq_lens, b, a.T);
+  int blk0, blk1;
+  if (!split_blocks(a, len, split, blk0, blk1)) return;
+  split_references(a, b, split, blk0, blk1, h0, 8, blockIdx.x == 0, mref);
+  const int c = blockIdx.x * 512 + lane * 8, cc = min(c, a.d - 8);
+  const long row_bytes = a.d * BITS / 8;
+  const unsigned char* codes = a.codes + (long)b * a.stride * row_bytes + (long)cc * BITS / 8;
+  const unsigned char* scales = a.scales + ((long)b * (a.d / 32) + cc / 32) * a.stride;
+  float acc[8][8];
+#pragma unroll
+  for (int h = 0; h < 8; ++h)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[h][j] = 0.f;
+  const float* P[8];
+  float f[8];
+#pragma unroll
+  for (int h = 0; h < 8; ++h) P[h] = (const float*)a.P + ((long)b * a.H + min(h0 + h, a.H - 1)) * a.Tp;
+  for (int blk = blk0; blk < blk1; ++blk) {
+#pragma unroll
+    for (int h = 0; h < 8; ++h) {
+      const int hh = min(h0 + h, a.H - 1);
+      f[h] = exp2f(a.ref[((long)b * a.H + hh) * a.NB + blk] - mref[hh - h0]);
+    }
+    const int t1 = min((blk + 1) * QUANT_ROWS, len);
+    for (int t = blk * QUANT_ROWS + wave; t < t1; t += 4) {       // (the waves: every fourth row)
+      Codes8<BITS> w;
+      w.load(codes + t * row_bytes);
+      const float s = __uint_as_float((unsigned)scales[t] << 23);
+      const f32x2 y0 = w.template f32<0>(s), y1 = w.template f32<1>(s), y2 = w.template f32<2>(s), y3 = w.template f32<3>(s);
+      const float y[8] = {y0[0], y0[1], y1[0], y1[1], y2[0], y2[1], y3[0], y3[1]};
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        const float p = P[h][t] * f[h];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[h][j] = fmaf(p, y[j], acc[h][j]);
+      }
+    }
+  }
+  for (int w = 1; w < 4; ++w) {
+    if (wave == w)
+#pragma unroll
+      for (int h = 0; h < 8; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) join[w - 1][h * 8 + j][lane] = acc[h][j];
+  }
+  __syncthreads();
+  if (wave != 0 || c >= a.d) return;
+#pragma unroll
+  for (int h = 0; h < 8; ++h) {
+    if (h0 + h >= a.H) continue;
+    float* o = a.C + (((long)b * a.nsplit + split) * a.H + h0 + h) * a.d + c;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = acc[h][j] + join[0][h * 8 + j][lane] + join[1][h * 8 + j][lane] + join[2][h * 8 + j][lane];
+  }
+}
+
+// ---- merge of the splits and projection -------------------------------------------------------------------
+
+constexpr int QP_BATCH = 16, QP_COLS = 128, QP_MAX_SPLITS = 64, QP_MAX_ROWS = 256;
+
+// Weights of a batch tile's splits for head h: 2^(reference - largest) / sum; zero for splits that a sequence does not have, and for sequences without rows
+__device__ __forceinline__ void split_weights(const QDecodeArgs& a, int b0, int h, float (&wt)[QP_BATCH][QP_MAX_SPLITS + 1]) {
+  // 16 threads a sequence
+  const int j = threadIdx.x >> 4, k = threadIdx.x & 15, b = b0 + j;
+  const int len = b < a.B ? seq_len_of(a.seq_lens, b, a.T) : 0;
+  const int nb = (len + QUANT_ROWS - 1) / QUANT_ROWS, used = (nb + a.per - 1) / a.per;
+  float m = NEG_INF, l = 0.f;
+  for (int s = k; s < used; s += 16) m = fmaxf(m, a.sref[((long)b * a.nsplit + s) * a.H + h]);
+  m = max_over_lanes<16>(m);
+  for (int s = k; s < used; s += 16) {
+    const long at = ((long)b * a.nsplit + s) * a.H + h;
+    l += a.ssum[at] * exp2f(a.sref[at] - m);
+  }
+  l = sum_over_lanes<16>(l);
+  for (int s = k; s < a.nsplit; s += 16) wt[j][s] = s < used ? exp2f(a.sref[((long)b * a.nsplit + s) * a.H + h] - m) / l : 0.f;
+  if (k == 0) wt[j][QP_MAX_SPLITS] = __int_as_float(used);
+}
+
+// out[b][h d_k + j] = sum_c C[b][h][c] W[c][h d_k + j].  A workgroup takes a head, up to 128 of its columns, 16 sequences and a row split of W: it merges the
+// splits' partial sums into LDS (as bf16 hi + lo, which keeps 16 bits of them; W is bf16), multiplies on 16x16x32 matrix instructions, and whoever of a
+// head's row splits comes last adds their results in the order of their numbers.  HBM-bound on W for small batches.
+template <bool F32>
+__global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
+  __shared__ float wt[QP_BATCH][QP_MAX_SPLITS + 1];
+  __shared__ __align__(16) char operand[F32 ? QP_BATCH * QP_MAX_ROWS * 4 : 2 * QP_BATCH * (QP_MAX_ROWS + 8) * 2];
+  __shared__ f32x4 join[4][8][64];
+  __shared__ int last;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int ct = (a.d_k + QP_COLS - 1) / QP_COLS;
+  const int h = blockIdx.x / ct, j0 = blockIdx.x % ct * QP_COLS, rs = blockIdx.y, b0 = blockIdx.z * QP_BATCH;
+  const int cr0 = rs * a.crows, rows = min(a.crows, a.d - cr0);
+  split_weights(a, b0, h, wt);
+  __syncthreads();
+  // merge: four columns a thread, 16 threads a sequence
+  {
+    const int j = tid >> 4, b = b0 + j, used = __float_as_int(wt[j][QP_MAX_SPLITS]);
+    const int padded = F32 ? rows : (rows + 31) / 32 * 32;
+    for (int r = (tid & 15) * 4; r < padded; r += 64) {
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      if (r < rows)
+        for (int s = 0; s < used; ++s) {
+          const f32x4 x = *(const f32x4*)(a.C + (((long)b * a.nsplit + s) * a.H + h) * a.d + cr0 + r);
+          const float f = wt[j][s];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = fmaf(f, x[k], v[k]);
+        }
+      if constexpr (F32) {
+        *(f32x4*)(operand + (j * QP_MAX_ROWS + r) * 4) = v;
+      } else {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { hi[k] = (__bf16)v[k]; lo[k] = (__bf16)(v[k] - (float)hi[k]); }
+        *(bf16x4*)(operand + (j * (QP_MAX_ROWS + 8) + r) * 2) = hi;
+        *(bf16x4*)(operand + ((QP_BATCH + j) * (QP_MAX_ROWS + 8) + r) * 2) = lo;
+      }
+    }
+  }
+  __syncthreads();
+  const int nj = min(QP_COLS, a.d_k - j0);
+  float mine[8];                                 // this thread's results: sequence tid / 16, columns 8 (tid % 16) ...
+  if constexpr (!F32) {
+    const int n = lane & 15, kg = lane >> 4;
+    const bool in = n * 8 < nj;
+    const uint16_t* W = (const uint16_t*)a.W + (long)h * a.d_k + j0 + (in ? n * 8 : 0);
+    f32x4 acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int r = wave * 32; r < rows; r += 128) {
+      u32x4 kt[8], t[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) kt[i] = *(const u32x4*)(W + (long)min(cr0 + r + kg * 8 + i, a.d - 1) * a.d);     // (d is a multiple of 32: no row is past the end)
+      transpose8x8(kt, t);
+      const bf16x8 hi = *(const bf16x8*)(operand + (n * (QP_MAX_ROWS + 8) + r + kg * 8) * 2);
+      const bf16x8 lo = *(const bf16x8*)(operand + ((QP_BATCH + n) * (QP_MAX_ROWS + 8) + r + kg * 8) * 2);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, __builtin_bit_cast(bf16x8, t[j]), acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, __builtin_bit_cast(bf16x8, t[j]), acc[j], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) join[wave][j][lane] = acc[j];
+    __syncthreads();
+    // row m of a product is lane group m / 4, element m % 4
+    const int m = tid >> 4, from = (m >> 2) * 16 + (tid & 15);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mine[j] = (join[0][j][from][m & 3] + join[1][j][from][m & 3]) + (join[2][j][from][m & 3] + join[3][j][from][m & 3]);
+  } else {
+    const float* C = (const float*)operand + (tid >> 4) * QP_MAX_ROWS;
+    const int c = (tid & 15) * 8;
+    const float* W = (const float*)a.W + (long)cr0 * a.d + (long)h * a.d_k + j0 + (c < nj ? c : 0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mine[j] = 0.f;
+    for (int r = 0; r < rows; ++r) {
+      const f32x4 lo = *(const f32x4*)(W + (long)r * a.d), hi = *(const f32x4*)(W + (long)r * a.d + 4);
+      const float x = C[r];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { mine[k] = fmaf(x, lo[k], mine[k]); mine[4 + k] = fmaf(x, hi[k], mine[4 + k]); }
+    }
+  }
+  const int b = b0 + (tid >> 4), c = (tid & 15) * 8;
+  const bool mine_there = b < a.B && c < nj;
+  const long o = (long)b * a.d + (long)h * a.d_k + j0 + c;
+  if (a.csw > 1) {
+    if (mine_there) {
+      f32x4* p = (f32x4*)(a.part + (long)rs * a.B * a.d + o);
+      p[0] = f32x4{mine[0], mine[1], mine[2], mine[3]};
+      p[1] = f32x4{mine[4], mine[5], mine[6], mine[7]};
+    }
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) last = atomicAdd(a.counters + blockIdx.z * gridDim.x + blockIdx.x, 1) == a.csw - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    if (mine_there) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mine[j] = 0.f;
+      for (int s = 0; s < a.csw; ++s) {
+        const f32x4* p = (const f32x4*)(a.part + (long)s * a.B * a.d + o);
+        const f32x4 lo = p[0], hi = p[1];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { mine[k] += lo[k]; mine[4 + k] += hi[k]; }
+      }
+    }
+  }
+  if (!mine_there) return;
+  if constexpr (F32) {
+    f32x4* p = (f32x4*)((float*)a.out + o);
+    p[0] = f32x4{mine[0], mine[1], mine[2], mine[3]};
+    p[1] = f32x4{mine[4], mine[5], mine[6], mine[7]};
+  } else {
+    bf16x8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (__bf16)mine[j];
+    *(bf16x8*)((uint16_t*)a.out + o) = v;
+  }
+}
+
+template <bool F32, int BITS, int P>
+void scores_of(const QDecodeArgs& a, hipStream_t st) {
+  const int hw = 4 * 64 / P;
+  const dim3 grid(a.NB, (a.H + hw - 1) / hw, a.B);
+  if (a.rope) qscores_kernel<F32, BITS, P, true><<<grid, 256, 0, st>>>(a);
+  else qscores_kernel<F32, BITS, P, false><<<grid, 256, 0, st>>>(a);
+}
+template <bool F32, int BITS>
+void scores_by_width(const QDecodeArgs& a, hipStream_t st) {
+  if (a.d_k <= 32) scores_of<F32, BITS, 4>(a, st);
+  else if (a.d_k <= 64) scores_of<F32, BITS, 8>(a, st);
+  else if (a.d_k <= 128) scores_of<F32, BITS, 16>(a, st);
+  else if (a.d_k <= 256) scores_of<F32, BITS, 32>(a, st);
+  else scores_of<F32, BITS, 64>(a, st);
+}
+
+}  // namespace
+
+int qdecode_counters(int B, int H, int d) { return H * ((d / H + QP_COLS - 1) / QP_COLS) * ((B + QP_BATCH - 1) / QP_BATCH); }
+
+// How the work is cut: splits of the weighted sum so that about 512 workgroups (two a compute unit) share it, each of 256 rows at least (a step of 32 rows for
+// every wave, twice), and row splits of W likewise.  (The splits themselves go up and down with T.)
+void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* most_splits, int* csw, int* crows) {
+  const int nb = (T + QUANT_ROWS - 1) / QUANT_ROWS;
+  const long units = dtype == DT_F32 ? (long)B * ((d + 511) / 512) * ((H + 7) / 8) : (long)B * ((d + QW_COLS - 1) / QW_COLS) * ((H + 31) / 32);
+  long want = (512 + units - 1) / units;
+  want = want > QP_MAX_SPLITS ? QP_MAX_SPLITS : want;
+  int p = (int)((nb + want - 1) / want);
+  *per = p < 4 ? 4 : p;
+  *nsplit = (nb + *per - 1) / *per;
+  *most_splits = (int)((nb + 3) / 4 < want ? (nb + 3) / 4 : want);
+  const int d_k = d / H, ct = (d_k + QP_COLS - 1) / QP_COLS;
+  const long tiles = (long)H * ct * ((B + QP_BATCH - 1) / QP_BATCH);
+  const int least = (d + QP_MAX_ROWS - 1) / QP_MAX_ROWS, most = d / 32;
+  long c = (512 + tiles - 1) / tiles;
+  if (c < least) c = least;
+  if (c > most) c = most;
+  *crows = (int)(((d + c - 1) / c + 31) / 32 * 32);
+  *csw = (d + *crows - 1) / *crows;
+}
+
+void launch_qdecode_scores(int dtype, const QDecodeArgs& a, hipStream_t st) {
+  if (dtype == DT_F32) {
+    if (a.bits == 4) scores_by_width<true, 4>(a, st); else scores_by_width<true, 8>(a, st);
+  } else {
+    if (a.bits == 4) scores_by_width<false, 4>(a, st); else scores_by_width<false, 8>(a, st);
+  }
+}
+
+void launch_qdecode_weighted(int dtype, const QDecodeArgs& a, hipStream_t st) {
+  if (dtype == DT_F32) {
+    const dim3 grid((a.d + 511) / 512, a.nsplit, a.B * ((a.H + 7) / 8));
+    if (a.bits == 4) qweighted_f32_kernel<4><<<grid, 256, 0, st>>>(a);
+    else qweighted_f32_kernel<8><<<grid, 256, 0, st>>>(a);
+    return;
+  }
+  const int cols = (a.d + QW_COLS - 1) / QW_COLS;
+  if (a.H <= 16) {
+    const dim3 grid(cols, a.nsplit, a.B);
+    if (a.bits == 4) qweighted_kernel<4, 1><<<grid, 256, 0, st>>>(a);
+    else qweighted_kernel<8, 1><<<grid, 256, 0, st>>>(a);
+  } else {
+    const dim3 grid(cols, a.nsplit, a.B * ((a.H + 31) / 32));
+    if (a.bits == 4) qweighted_kernel<4, 2><<<grid, 256, 0, st>>>(a);
+    else qweighted_kernel<8, 2><<<grid, 256, 0, st>>>(a);
+  }
+}
+
+void launch_qdecode_project(int dtype, const QDecodeArgs& a, hipStream_t st) {
+  const int ct = (a.d_k + QP_COLS - 1) / QP_COLS;
+  const dim3 grid(a.H * ct, a.csw, (a.B + QP_BATCH - 1) / QP_BATCH);
+  if (dtype == DT_F32) qproject_kernel<true><<<grid, 256, 0, st>>>(a);
+  else qproject_kernel<false><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace slim

@@ -1,0 +1,69 @@
+// What the kernels of prompt attention share (kernels_prompt.hip, kernels_prompt_f32.hip): which rows a workgroup has, rows from memory into LDS, the merge's inputs.
+#pragma once
+#include "device_common.h"
+#include "slim_kernels.h"
+
+namespace slim {
+
+// 16 bytes a lane from memory to LDS: lane l's go to lds + 16 l.  The caller waits (vmcnt) before it, or another wave behind a barrier, reads them.
+// (As asm: the compiler would wait for all of them before the first LDS read that follows, of another buffer too.)
+__device__ __forceinline__ void load_to_lds(const void* p, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(__builtin_amdgcn_readfirstlane((int)lds)) : "memory");
+}
+__device__ __forceinline__ unsigned lds_address(const void* p) {
+  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// The tiles that this wave asked for are there, then everybody's; and everybody is done with the buffer that is filled next.
+__device__ __forceinline__ void tiles_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+struct PromptTile {
+  long q0, k0;            // first rows of the sequence
+  int n_q, n_k, i0;       // its rows, and the tile's first query
+  int h, split;
+};
+
+__device__ __forceinline__ int clamped(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
+
+// Workgroup -> head, tile of `rows` queries, split of the keys.  Sequence b's tiles have places from cu_q[b] / rows + b on: never more tiles than places up to the
+// next one's, so that no workgroup needs a sum over the batch; places behind a sequence's last tile are empty.  Workgroups are dealt to the 8 XCDs round
+// robin: each XCD gets a run of consecutive heads, whose keys and values then stay in its L2.  The longest rows of a causal sequence come first.
+__device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int rows, PromptTile& t) {
+  const int places = a.rows_q / rows + a.B, units = a.H * places * a.nsplit;
+  const int per = (units + 7) / 8, unit = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+  if (((int)blockIdx.x >> 3) >= per || unit >= units) return false;
+  t.split = unit % a.nsplit;
+  t.h = unit / a.nsplit / places;
+  const int place = places - 1 - unit / a.nsplit % places;
+  int lo = 0, hi = a.B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (clamped(a.cu_q[mid], a.rows_q) / rows + mid <= place) lo = mid; else hi = mid;
+  }
+  const int q0 = clamped(a.cu_q[lo], a.rows_q), q1 = clamped(a.cu_q[lo + 1], a.rows_q);
+  const int k0 = clamped(a.cu_k[lo], a.rows_k), k1 = clamped(a.cu_k[lo + 1], a.rows_k);
+  t.q0 = q0; t.n_q = q1 - q0;
+  t.k0 = k0; t.n_k = max(k1 - k0, 0);
+  const int j = place - (q0 / rows + lo);
+  t.i0 = j * rows;
+  return j >= 0 && t.i0 < t.n_q;
+}
+inline unsigned prompt_grid(const PromptArgs& a, int rows) {
+  return 8u * (unsigned)(((long)a.H * (a.rows_q / rows + a.B) * a.nsplit + 7) / 8);
+}
+
+// max / sum over the lanes l and l ^ 32
+__device__ __forceinline__ float max_of_halves(float v) {
+  const unsigned u = __float_as_uint(v);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+  const unsigned u = __float_as_uint(v);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+void launch_prompt_f32(const PromptArgs& a, hipStream_t st);
+constexpr int PROMPT_F32_ROWS = 64;          // queries of a workgroup
+
+}  // namespace slim

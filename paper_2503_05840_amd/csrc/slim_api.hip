@@ -953,3 +953,204 @@ extern "C" int slim_tree_commit(void* Kcache, const int32_t* path, const int32_t
   tm.finish();
   return launch_status();
 }
+
+// ---- K-caches in 4 or 8 bits ------------------------------------------------------------------------
+namespace {
+
+// Bounds that keep grids, LDS tables and 32-bit offsets inside their ranges
+constexpr int QUANT_MAX_BATCH = 32768, QUANT_MAX_WIDTH = 1 << 20, QUANT_MAX_HEADS = 1024, QUANT_MAX_HEAD_WIDTH = 512, QUANT_MAX_CONTEXT = 1 << 24;
+
+// What the calls on such a cache check alike: its format, rows and width.
+int check_quant(int B, int T, int d, int bits, const slim_opts* o, int* dtype, long* t_stride) {
+  if (bits != SLIM_Q4 && bits != SLIM_Q8) return SLIM_ERR_ARG;
+  if (o && o->k_layout != SLIM_K_ROWMAJOR) return SLIM_ERR_ARG;
+  if (B < 1 || B > QUANT_MAX_BATCH || T < 1 || T > QUANT_MAX_CONTEXT || d < 1 || d > QUANT_MAX_WIDTH || d % 32 != 0) return SLIM_ERR_SHAPE;
+  *dtype = o ? o->dtype : SLIM_F32;
+  if (*dtype != SLIM_F32 && *dtype != SLIM_BF16) return SLIM_ERR_DTYPE;
+  *t_stride = (o && o->t_stride) ? (long)o->t_stride : ((long)T + QUANT_ROWS - 1) / QUANT_ROWS * QUANT_ROWS;
+  if (*t_stride < T) return SLIM_ERR_SHAPE;
+  if (*t_stride % QUANT_ROWS != 0) return SLIM_ERR_LAYOUT;
+  if (o && o->seq_lens && misaligned4(o->seq_lens)) return SLIM_ERR_ALIGN;
+  return SLIM_OK;
+}
+
+int quant_rows(bool write, const void* src, const int32_t* cu_rows, void* codes, void* scales, void* dst, int B, int n_rows, int T, int d, int bits,
+               int64_t pitch, const slim_opts* o) {
+  if ((n_rows > 0 && !(write ? src : dst)) || !codes || !scales || pitch < 0) return SLIM_ERR_ARG;
+  if (o && o->rope_table) return SLIM_ERR_ARG;        // keys are stored raw
+  int dtype; long t_stride;
+  if (int rc = check_quant(B, T, d, bits, o, &dtype, &t_stride)) return rc;
+  if (pitch == 0) pitch = d;
+  if (n_rows < 0 || pitch < d || pitch % vec_elems(dtype) != 0) return SLIM_ERR_SHAPE;
+  if (!cu_rows && n_rows % B != 0) return SLIM_ERR_SHAPE;
+  if (misaligned(src) || misaligned(dst) || misaligned(codes) || misaligned(scales) || misaligned4(cu_rows)) return SLIM_ERR_ALIGN;
+  if (o && o->seq_lens_host)
+    for (int b = 0; b < B; ++b)
+      if (o->seq_lens_host[b] < 0 || o->seq_lens_host[b] > T) return SLIM_ERR_SEQLEN;
+  hipStream_t st = o ? (hipStream_t)o->stream : nullptr;
+  StageTimer tm(o, st);
+  if (n_rows > 0) {
+    QuantArgs a{src, dst, cu_rows, o ? o->seq_lens : nullptr, (unsigned char*)codes, (unsigned char*)scales, pitch, t_stride, B, n_rows, T, d};
+    if (write) launch_quant_append(dtype, bits, a, st);
+    else launch_quant_read(dtype, bits, a, st);
+  }
+  tm.mark();
+  tm.finish();
+  return launch_status();
+}
+
+struct QDecodePlan { size_t off_P, off_ref, off_sum, off_C, off_sref, off_ssum, off_part, off_counters, total; };
+
+// Every term grows with T: the splits of a context are bounded by those of a longer one.
+QDecodePlan qdecode_layout(QDecodeArgs& a, int dtype) {
+  a.NB = (a.T + QUANT_ROWS - 1) / QUANT_ROWS;
+  a.Tp = a.NB * QUANT_ROWS;
+  int most;
+  qdecode_cut(dtype, a.B, a.H, a.T, a.d, &a.per, &a.nsplit, &most, &a.csw, &a.crows);
+  QDecodePlan p;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o += up(bytes); return at; };
+  take(sizeof(int) * CTRL_INTS);             // (a workspace's control block: what slim_status reads of a decode step on the same workspace stays)
+  const size_t BH = (size_t)a.B * a.H;
+  a.ncounters = qdecode_counters(a.B, a.H, a.d);
+  p.off_counters = take(sizeof(int) * a.ncounters);
+  p.off_P = take((size_t)elem_bytes(dtype) * BH * a.Tp);
+  p.off_ref = take(sizeof(float) * BH * a.NB);
+  p.off_sum = take(sizeof(float) * BH * a.NB);
+  p.off_C = take(sizeof(float) * BH * most * a.d);
+  p.off_sref = take(sizeof(float) * BH * most);
+  p.off_ssum = take(sizeof(float) * BH * most);
+  p.off_part = take(a.csw > 1 ? sizeof(float) * (size_t)a.csw * a.B * a.d : 0);
+  p.total = o;
+  return p;
+}
+
+int check_qdecode(int H, int d) {
+  if (H < 1 || H > QUANT_MAX_HEADS || d % H != 0 || d / H % 8 != 0 || d / H > QUANT_MAX_HEAD_WIDTH) return SLIM_ERR_SHAPE;
+  return SLIM_OK;
+}
+
+}  // namespace
+
+extern "C" int slim_quant_append(const void* rows, const int32_t* cu_rows, void* codes, void* scales, int B, int n_rows, int T, int d, int bits,
+                                 int64_t pitch, const slim_opts* o) {
+  return quant_rows(true, rows, cu_rows, codes, scales, nullptr, B, n_rows, T, d, bits, pitch, o);
+}
+
+extern "C" int slim_quant_read(const void* codes, const void* scales, const int32_t* cu_rows, void* rows, int B, int n_rows, int T, int d, int bits,
+                               int64_t pitch, const slim_opts* o) {
+  return quant_rows(false, nullptr, cu_rows, (void*)codes, (void*)scales, rows, B, n_rows, T, d, bits, pitch, o);
+}
+
+extern "C" size_t slim_workspace_bytes_quant(int B, int H, int T, int d, int bits, int dtype) {
+  slim_opts o{};
+  o.dtype = dtype;
+  long ts;
+  if (check_quant(B, T, d, bits, &o, &dtype, &ts) || check_qdecode(H, d)) return 0;
+  QDecodeArgs a{};
+  a.B = B; a.H = H; a.T = T; a.d = d; a.d_k = d / H; a.bits = bits;
+  return qdecode_layout(a, dtype).total;
+}
+
+extern "C" int slim_quant_decode(const void* q, const void* codes, const void* scales, const void* W_KV, void* out, int B, int H, int T, int d, int bits,
+                                 const slim_opts* o) {
+  if (!q || !codes || !scales || !W_KV || !out) return SLIM_ERR_ARG;
+  int dtype; long t_stride;
+  if (int rc = check_quant(B, T, d, bits, o, &dtype, &t_stride)) return rc;
+  if (int rc = check_qdecode(H, d)) return rc;
+  if (misaligned(q) || misaligned(codes) || misaligned(scales) || misaligned(W_KV) || misaligned(out)) return SLIM_ERR_ALIGN;
+  const float* rope = o ? o->rope_table : nullptr;
+  if (rope && misaligned(rope)) return SLIM_ERR_ALIGN;
+  if (o && o->seq_lens_host)
+    for (int b = 0; b < B; ++b)
+      if (o->seq_lens_host[b] < 0 || o->seq_lens_host[b] > T) return SLIM_ERR_SEQLEN;
+  QDecodeArgs a{};
+  a.B = B; a.H = H; a.T = T; a.d = d; a.d_k = d / H; a.bits = bits;
+  const QDecodePlan p = qdecode_layout(a, dtype);
+  char* ws;
+  if (int rc = get_workspace(o, p.total, &ws)) return rc;
+  hipStream_t st = o ? (hipStream_t)o->stream : nullptr;
+  a.q = q; a.W = W_KV; a.codes = (const unsigned char*)codes; a.scales = (const unsigned char*)scales; a.out = out;
+  a.seq_lens = o ? o->seq_lens : nullptr;
+  a.rope = rope; a.stride = t_stride;
+  a.qscale = 1.4426950408889634f / sqrtf((float)a.d_k);
+  a.P = ws + p.off_P;
+  a.ref = (float*)(ws + p.off_ref); a.sum = (float*)(ws + p.off_sum);
+  a.C = (float*)(ws + p.off_C); a.sref = (float*)(ws + p.off_sref); a.ssum = (float*)(ws + p.off_ssum);
+  a.part = (float*)(ws + p.off_part); a.counters = (int*)(ws + p.off_counters);
+  StageTimer tm(o, st);
+  launch_qdecode_scores(dtype, a, st);
+  tm.mark();
+  launch_qdecode_weighted(dtype, a, st);
+  tm.mark();
+  launch_qdecode_project(dtype, a, st);
+  tm.mark();
+  tm.finish();
+  return launch_status();
+}
+
+// ---- attention over whole prompts ----------------------------------------------------------------------
+namespace {
+
+constexpr int PROMPT_MAX_BATCH = 32768, PROMPT_MAX_ROWS = 1 << 24, PROMPT_MAX_HEADS = 4096;
+
+int check_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dtype) {
+  if (B < 1 || B > PROMPT_MAX_BATCH || rows_q < 0 || rows_q > PROMPT_MAX_ROWS || rows_k < 0 || rows_k > PROMPT_MAX_ROWS) return SLIM_ERR_SHAPE;
+  if (H < 1 || H > PROMPT_MAX_HEADS || H_kv < 1 || H % H_kv != 0 || d_k < 1 || d_k > PROMPT_MAX_WIDTH) return SLIM_ERR_SHAPE;
+  if (dtype != SLIM_F32 && dtype != SLIM_BF16) return SLIM_ERR_DTYPE;
+  if (d_k % vec_elems(dtype) != 0) return SLIM_ERR_SHAPE;
+  return SLIM_OK;
+}
+
+size_t prompt_bytes(int nsplit, int rows_q, int H, int d_k) {
+  // (the control block: as above)
+  return up(sizeof(int) * CTRL_INTS) + (nsplit > 1 ? up(sizeof(float) * (size_t)nsplit * rows_q * H * d_k) + up(sizeof(float) * 2 * (size_t)nsplit * rows_q * H) : 0);
+}
+
+}  // namespace
+
+extern "C" size_t slim_workspace_bytes_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dtype) {
+  if (check_prompt(B, rows_q, rows_k, H, H_kv, d_k, dtype)) return 0;
+  return prompt_bytes(prompt_splits(dtype, B, rows_q, rows_k, H, d_k), rows_q, H, d_k);
+}
+
+extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_k, void* out, int B, int rows_q,
+                                     int rows_k, int H, int H_kv, int d_k, int causal, int64_t q_pitch, int64_t k_pitch, int64_t v_pitch, const slim_opts* o) {
+  if (!cu_q || q_pitch < 0 || k_pitch < 0 || v_pitch < 0) return SLIM_ERR_ARG;
+  if ((rows_q > 0 && (!q || !out)) || (rows_k > 0 && (!k || !v))) return SLIM_ERR_ARG;
+  // (there is no cache in this call: lengths are cu_q's and cu_k's, queries and keys carry their positions)
+  if (o && (o->seq_lens || o->seq_lens_host || o->rope_table || o->k_layout || o->t_stride)) return SLIM_ERR_ARG;
+  const int dtype = o ? o->dtype : SLIM_F32;
+  if (int rc = check_prompt(B, rows_q, rows_k, H, H_kv, d_k, dtype)) return rc;
+  if (!cu_k && rows_k != rows_q) return SLIM_ERR_SHAPE;
+  if (q_pitch == 0) q_pitch = (int64_t)H * d_k;
+  if (k_pitch == 0) k_pitch = (int64_t)H_kv * d_k;
+  if (v_pitch == 0) v_pitch = (int64_t)H_kv * d_k;
+  const int vec = vec_elems(dtype);
+  if (q_pitch < (int64_t)H * d_k || k_pitch < (int64_t)H_kv * d_k || v_pitch < (int64_t)H_kv * d_k || q_pitch % vec || k_pitch % vec || v_pitch % vec)
+    return SLIM_ERR_SHAPE;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned4(cu_q) || misaligned4(cu_k)) return SLIM_ERR_ALIGN;
+  const int nsplit = prompt_splits(dtype, B, rows_q, rows_k, H, d_k);
+  char* ws = nullptr;
+  if (nsplit > 1)
+    if (int rc = get_workspace(o, prompt_bytes(nsplit, rows_q, H, d_k), &ws)) return rc;
+  hipStream_t st = o ? (hipStream_t)o->stream : nullptr;
+  StageTimer tm(o, st);
+  if (rows_q > 0) {
+    PromptArgs a{};
+    a.q = q; a.k = k; a.v = v; a.out = out; a.cu_q = cu_q; a.cu_k = cu_k ? cu_k : cu_q;
+    a.q_pitch = q_pitch; a.k_pitch = k_pitch; a.v_pitch = v_pitch;
+    a.B = B; a.rows_q = rows_q; a.rows_k = rows_k; a.H = H; a.H_kv = H_kv; a.d_k = d_k; a.causal = causal != 0;
+    a.scale = 1.4426950408889634f / sqrtf((float)d_k);
+    a.nsplit = nsplit;
+    if (nsplit > 1) {
+      a.O = (float*)(ws + up(sizeof(int) * CTRL_INTS));
+      a.ml = (float*)((char*)a.O + up(sizeof(float) * (size_t)nsplit * rows_q * H * d_k));
+    }
+    launch_prompt(dtype, a, st);
+    if (nsplit > 1) launch_prompt_merge(dtype, a, st);
+  }
+  tm.mark();
+  tm.finish();
+  return launch_status();
+}

@@ -287,4 +287,61 @@ void launch_tree_verify(int dtype, const VerifyArgs& a, hipStream_t st);
 void launch_tree_commit(int dtype, void* K, long k_bstride, const int32_t* path, const int32_t* n_path, const int32_t* seq_lens, int32_t* new_lens,
                         int B, int N, int T, int d, int d_k, int banded, hipStream_t st);
 
+// ---- K-caches in 4 or 8 bits (kernels_quant.hip, kernels_qdecode.hip) -------------------------------------
+constexpr int QUANT_ROWS = 64;               // rows kept a sequence are a multiple of these; rows that share a reference of the softmax numerators
+
+struct QuantArgs {
+  const void* rows;                          // append: [n_rows] rows, `pitch` elements apart
+  void* out;                                 // read: the same
+  const int32_t *cu, *start;                 // [B + 1] offsets of the sequences' rows (nullable: n_rows / B each), [B] first cache row (nullable: 0)
+  unsigned char *codes, *scales;             // [B][stride][d bits / 8], [B][d / 32][stride]
+  long pitch, stride;
+  int B, n_rows, T, d;
+};
+void launch_quant_append(int dtype, int bits, const QuantArgs& a, hipStream_t st);
+void launch_quant_read(int dtype, int bits, const QuantArgs& a, hipStream_t st);
+
+struct QDecodeArgs {
+  const void *q, *W;                         // [B][d], [d][d]
+  const unsigned char *codes, *scales;
+  const int32_t* seq_lens;                   // nullable: T each
+  const float* rope;                         // [T][d_k / 2][2], nullable
+  void* out;                                 // [B][d]
+  long stride;                               // rows kept a sequence
+  int B, H, T, d, d_k, bits;
+  float qscale;                              // log2(e) / sqrt(d_k)
+  // work in between
+  int NB, Tp;                                // blocks of QUANT_ROWS rows of the longest sequence, NB * QUANT_ROWS
+  int per, nsplit;                           // blocks of a split of the weighted sum, splits of the longest sequence
+  int csw, crows;                            // row splits of W and their rows
+  void* P;                                   // [B][H][Tp] numerators, dtype
+  float *ref, *sum;                          // [B][H][NB]: whole exponent that a block's numerators are relative to, and their sum
+  float* C;                                  // [B][nsplit][H][d]
+  float *sref, *ssum;                        // [B][nsplit][H]
+  float* part;                               // [csw][B][d], csw > 1
+  int* counters; int ncounters;              // arrivals of the row splits
+};
+int qdecode_counters(int B, int H, int d);
+// blocks of a split, splits, their bound that grows with T, row splits of W and their rows
+void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* most, int* csw, int* crows);
+void launch_qdecode_scores(int dtype, const QDecodeArgs& a, hipStream_t st);
+void launch_qdecode_weighted(int dtype, const QDecodeArgs& a, hipStream_t st);
+void launch_qdecode_project(int dtype, const QDecodeArgs& a, hipStream_t st);
+
+// ---- attention over whole prompts (kernels_prompt.hip, kernels_prompt_f32.hip) -----------------------------
+struct PromptArgs {
+  const void *q, *k, *v;
+  void* out;                                 // [rows_q][H * d_k]
+  const int32_t *cu_q, *cu_k;                // [B + 1]
+  long q_pitch, k_pitch, v_pitch;            // elements between rows
+  int B, rows_q, rows_k, H, H_kv, d_k, causal;
+  float scale;                               // log2(e) / sqrt(d_k)
+  int nsplit;                                // parts of the keys, each a workgroup of its own; 1: results are written at once
+  float *O, *ml;                             // nsplit > 1: [nsplit][rows_q][H][d_k] unnormalised, [nsplit][rows_q][H][2] reference and sum
+};
+constexpr int PROMPT_MAX_WIDTH = 256;        // columns of a head
+int prompt_splits(int dtype, int B, int rows_q, int rows_k, int H, int d_k);
+void launch_prompt(int dtype, const PromptArgs& a, hipStream_t st);
+void launch_prompt_merge(int dtype, const PromptArgs& a, hipStream_t st);
+
 }  // namespace slim

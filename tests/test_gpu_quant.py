@@ -1,0 +1,231 @@
+"""Caches in 4 or 8 bits: rows written and read back against the format's list of values, and the decode step over them against fp64."""
+import numpy as np
+import pytest
+
+from oracle import prompt_oracle as orc
+from paper_2503_05840_amd import binding, synth
+from prompt_cases import QuantCase, ints, offsets, up
+
+pytestmark = pytest.mark.gpu
+
+
+def _rows(rng, n, d, dtype):
+    """Rows on many scales, with the values where a format can go wrong."""
+    x = rng.standard_normal((n, d)) * np.exp(rng.standard_normal((n, 1)) * 4)
+    if n > 6:
+        x[0] = 0.0
+        x[1, ::2] = -0.0
+        x[2] *= 1e-36                                            # near and under the smallest normal number
+        x[3, 5], x[3, 40 % d] = 3e38, -3.3e38                    # the largest numbers
+        x[4, :8] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.9]    # ties
+        x[4, 8:32] = 0.0
+        x[5, :32] = np.array([1.75, 1.7499, 1.7501, -0.875] * 8)
+        x[6, :3] = [448, 432, 440]
+    return synth.round_through(x, dtype)
+
+
+def _written(rows, start, new, codes, scales, T, bits):
+    """What the caches hold after an append, from the oracle."""
+    at = offsets(new)
+    for b in range(len(new)):
+        c, s = orc.quantise(rows[at[b]:at[b + 1]], bits)
+        n = max(min(T - start[b], new[b]), 0)
+        codes[b, start[b]:start[b] + n] = orc.pack(c, bits)[:n]
+        scales[b, :, start[b]:start[b] + n] = s.T[:, :n]
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,new,start", [(32, [9], [0]), (96, [1, 1, 1], [0, 70, 127]), (864, [70, 0, 3], [5, 0, 61]), (288, [2, 129], [64, 1])])
+def test_rows_written_and_read_back(bits, dtype, d, new, start):
+    import torch
+    rng = np.random.default_rng(d + bits)
+    B, T, stride, tail = len(new), 190, 256, 5
+    rows = _rows(rng, sum(new) + tail, d, dtype)
+    codes, scales = rng.integers(0, 256, (B, stride, d * bits // 8), dtype=np.uint8), rng.integers(0, 256, (B, d // 32, stride), dtype=np.uint8)
+    dc, ds = torch.from_numpy(codes.copy()).cuda(), torch.from_numpy(scales.copy()).cuda()
+    dev = up(rows, dtype)
+    kw = dict(cu_rows=ints(offsets(new)), dtype=dtype, seq_lens=ints(start), t_stride=stride)
+    binding.slim_quant_append(dev, dc, ds, B, T, d, bits, **kw)
+    _written(dev.double().cpu().numpy(), start, new, codes, scales, T, bits)
+    assert (dc.cpu().numpy() == codes).all() and (ds.cpu().numpy() == scales).all()
+    back = torch.full_like(dev, 77.0)
+    binding.slim_quant_read(dc, ds, back, B, T, d, bits, **kw)
+    got, at = back.double().cpu().numpy(), offsets(new)
+    for b in range(B):
+        want = orc.values(orc.unpack(codes[b], bits), scales[b].T, bits)[start[b]:start[b] + new[b]]
+        want = up(want, dtype).double().cpu().numpy()               # (magnitudes under 2^-126 are rounded)
+        assert np.array_equal(got[at[b]:at[b + 1]], want, equal_nan=True)
+    assert (got[at[-1]:] == 77.0).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_rows_that_are_not_finite_or_do_not_fit(bits):
+    import torch
+    rng = np.random.default_rng(3)
+    d, T = 128, 70
+    rows = synth.round_through(rng.standard_normal((6, d)), "bf16")
+    rows[1, 40], rows[2, 0], rows[3, 127] = np.nan, np.inf, -np.inf
+    codes, scales = binding.slim_quant_cache(2, T, d, bits)
+    before = (codes.clone(), scales.clone())
+    binding.slim_quant_append(up(rows, "bf16"), codes, scales, 2, T, d, bits, seq_lens=ints([0, 68]))       # three rows each: the last of sequence 1 has no place
+    c, s = codes.cpu().numpy(), scales.cpu().numpy()
+    want_c, want_s = (x.cpu().numpy() for x in before)
+    _written(rows, [0, 68], [3, 3], want_c, want_s, T, bits)
+    assert (c == want_c).all() and (s == want_s).all()
+    out = torch.full((6, d), 77.0, dtype=torch.bfloat16, device="cuda")
+    binding.slim_quant_read(codes, scales, out, 2, T, d, bits, seq_lens=ints([0, 68]))
+    o = out.float().cpu().numpy()
+    bad = np.isnan(o)
+    assert bad[1, 32:64].all() and bad[2, :32].all() and bad[3, 96:].all() and bad.sum() == 96 and (o[5] == 0).all()
+    # starts that are no row of the cache: nothing is written, zeros are read
+    held = codes.clone()
+    binding.slim_quant_append(up(rows, "bf16"), codes, scales, 2, T, d, bits, seq_lens=ints([-9, 1 << 30]))
+    binding.slim_quant_read(codes, scales, out, 2, T, d, bits, seq_lens=ints([-9, 1 << 30]))
+    assert torch.equal(held, codes) and (out == 0).all()
+
+
+def test_columns_of_a_wider_buffer_and_no_rows():
+    import torch
+    rng = np.random.default_rng(5)
+    d, n = 256, 37
+    wide = up(rng.standard_normal((n, 3 * d)), "bf16")
+    k = wide[:, d:2 * d]
+    a, b = binding.slim_quant_cache(1, n, d, 8), binding.slim_quant_cache(1, n, d, 8)
+    binding.slim_quant_append(k, *a, 1, n, d, 8)
+    binding.slim_quant_append(k.contiguous(), *b, 1, n, d, 8)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and a[0].any()
+    into = torch.full_like(wide, 77.0)
+    binding.slim_quant_read(*a, into[:, :d], 1, n, d, 8)
+    out = torch.empty((n, d), dtype=torch.bfloat16, device="cuda")
+    binding.slim_quant_read(*a, out, 1, n, d, 8)
+    assert torch.equal(into[:, :d], out) and (into[:, d:] == 77.0).all()
+    binding.slim_quant_append(k[:0], *a, 1, n, d, 8)
+    assert torch.equal(a[0], b[0])
+    with pytest.raises(ValueError):
+        binding.slim_quant_append(k[:1].expand(n, d), *a, 1, n, d, 8)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_rows_past_32_bit_offsets(bits):
+    import torch
+    d, T, B = 4096, 131072, 10                                   # 2.7 or 5.4 GB of codes
+    codes, scales = binding.slim_quant_cache(B, T, d, bits)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows = torch.randn((B, d), generator=g, device="cuda").bfloat16()
+    at = ints([T - 1 - b for b in range(B)])
+    binding.slim_quant_append(rows, codes, scales, B, T, d, bits, seq_lens=at)
+    out = torch.empty_like(rows)
+    binding.slim_quant_read(codes, scales, out, B, T, d, bits, seq_lens=at)
+    c, s = orc.quantise(rows.double().cpu().numpy(), bits)
+    assert np.array_equal(out.double().cpu().numpy(), orc.values(c, s, bits))
+    for b in (0, B - 1):
+        assert np.array_equal(codes[b, T - 1 - b].cpu().numpy(), orc.pack(c, bits)[b])
+    assert int(codes.ne(0).any(-1).sum()) == B
+
+
+DECODE = [  # B, H, d_k, T, lens
+    (1, 1, 32, 1, None), (1, 4, 64, 63, None), (2, 4, 64, 65, [1, 65]), (3, 20, 64, 300, [0, 300, 129]), (1, 12, 72, 200, None), (2, 4, 128, 520, [64, 511]),
+    (1, 40, 32, 100, None), (2, 24, 96, 130, [130, 33]), (17, 2, 48, 90, list(range(1, 18))), (1, 3, 160, 70, None), (1, 2, 272, 140, None), (1, 32, 128, 97, None)]
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,d_k,T,lens", DECODE)
+def test_decode_against_fp64(B, H, d_k, T, lens, dtype, bits):
+    QuantCase(B, H, d_k, T, bits, dtype, lens=lens, seed=T + bits).check()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,d_k,T", [(4, 64, 130), (4, 96, 65), (2, 128, 300), (2, 32, 40), (4, 200, 33)])
+def test_decode_with_rotary_keys(H, d_k, T, dtype, bits):
+    QuantCase(2, H, d_k, T, bits, dtype, lens=[T, T // 2], base=10000.0, seed=T).check()
+
+
+@pytest.mark.parametrize("dtype,B,H,d_k,T", [("bf16", 1, 8, 128, 20000), ("bf16", 3, 4, 64, 9000), ("f32", 2, 4, 64, 5000)])
+def test_decode_of_long_contexts(dtype, B, H, d_k, T):
+    lens = None if B == 1 else [T - 77 * b for b in range(B)]
+    for bits in (4, 8):
+        QuantCase(B, H, d_k, T, bits, dtype, lens=lens, seed=2).check()
+
+
+def test_decode_with_scores_far_apart():
+    """Numerators over many binades: blocks whose references differ by hundreds."""
+    c = QuantCase(2, 4, 64, 700, 4, lens=[700, 450], q_scale=60.0, seed=9)
+    c.check()
+
+
+@pytest.mark.parametrize("bits,dtype", [(4, "bf16"), (8, "bf16"), (4, "f32")])
+def test_decode_of_rows_that_are_not_finite(bits, dtype):
+    c = QuantCase(3, 4, 64, 200, bits, dtype, lens=[200, 100, 150], seed=4)
+    clean = c.run()
+    c.scales[1, 3, 70] = 255
+    if bits == 8:
+        c.codes[2, 149, 9] = 0x7f
+    got = c.run()
+    assert np.isnan(got[1]).all() and np.array_equal(got[0], clean[0])
+    assert np.isnan(got[2]).all() if bits == 8 else np.array_equal(got[2], clean[2])
+
+
+def test_decode_gives_the_same_bits_on_dirty_scratch_and_other_streams():
+    import torch
+    c = QuantCase(4, 20, 64, 1000, 4, lens=[1000, 3, 640, 77], seed=6)
+    c.device()
+    ws = torch.full((binding.slim_workspace_bytes_quant(4, 20, 1000, c.d, 4, "bf16"),), 0xff, dtype=torch.uint8, device="cuda")
+    a = c.call(workspace=ws)
+    b = c.call(workspace=ws)
+    own = c.call()
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        other = c.call(workspace=torch.zeros_like(ws))
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and torch.equal(a, own) and torch.equal(a, other)
+    c.check(got=a.float().cpu().numpy().astype(np.float64))
+
+
+def test_decode_is_captured_and_replayed_with_new_inputs():
+    """Append and decode of one token in a graph: replays see the lengths, rows and queries of their time."""
+    import torch
+    H, d_k, T, B, bits = 4, 64, 200, 2, 4
+    d = H * d_k
+    g = torch.Generator(device="cuda").manual_seed(3)
+    codes, scales = binding.slim_quant_cache(B, T, d, bits)
+    W = torch.randn((d, d), generator=g, device="cuda").mul_(d ** -0.5).bfloat16()
+    row, q = (torch.randn((B, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    held, lens = ints([0, 60]), ints([1, 61])
+    out = torch.empty((B, d), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(binding.slim_workspace_bytes_quant(B, H, T, d, bits, "bf16"), dtype=torch.uint8, device="cuda")
+    rows = torch.randn((B * 60, d), generator=g, device="cuda").bfloat16()
+    binding.slim_quant_append(rows, codes, scales, B, T, d, bits)
+
+    def step(out):
+        binding.slim_quant_append(row, codes, scales, B, T, d, bits, seq_lens=held)
+        binding.slim_quant_decode(q, codes, scales, W, out, B, H, T, d, bits, seq_lens=lens, workspace=ws)
+
+    step(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    for i in range(4):
+        row.normal_(generator=g)
+        q.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, want = out.clone(), torch.empty_like(out)
+        step(want)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.isfinite(got).all(), i
+        held += 1
+        lens += 1
+
+
+def test_status_of_a_shared_workspace_stays():
+    import torch
+    c = QuantCase(1, 8, 64, 100, 8, seed=1)
+    c.device()
+    ws = torch.zeros(1 << 24, dtype=torch.uint8, device="cuda")
+    c.call(workspace=ws)
+    assert binding.slim_status(ws) == 0 and not ws[:4 * 4096].any()
