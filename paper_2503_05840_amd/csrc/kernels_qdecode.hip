@@ -250,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
   typedef typename Codes16<BITS>::type W16;
   __shared__ float mref[32];
   __shared__ f32x4 join[4][NT * 4][64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ngroups = (a.H + 16 * NT - 1) / (16 * NT);
   const int b = blockIdx.z / ngroups, h0 = blockIdx.z % ngroups * 16 * NT, split = blockIdx.y;
   const int len = seq_len_of(a.seq_lens, b, a.T);
@@ -271,7 +271,9 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
     R[t] = a.ref + ((long)b * a.H + h) * a.NB;
   }
   const long row_bytes = a.d * BITS / 8;
-  const unsigned char* codes = a.codes + ((long)b * a.stride + kg * 8) * row_bytes + (long)cc * BITS / 8;
+  // (a uniform pointer and a lane's offset: a pointer a lane and row would take 32 registers)
+  const unsigned char* codes = a.codes + (long)b * a.stride * row_bytes;
+  const unsigned at = (unsigned)(kg * 8 * (int)row_bytes + cc * BITS / 8);
   const unsigned char* scales = a.scales + ((long)b * (a.d / 32) + cc / 32) * a.stride + kg * 8;
   f32x4 acc[NT][16];
 #pragma unroll
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
   auto fetch = [&](int k, Rows& x) {
     const long r0 = (long)k * 32;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x.w[i] = *(const W16*)(codes + (r0 + i) * row_bytes);
+    for (int i = 0; i < 8; ++i) x.w[i] = *(const W16*)(codes + (r0 + i) * row_bytes + at);
     x.s = *(const u32x2*)(scales + r0);
 #pragma unroll
     for (int t = 0; t < NT; ++t) { x.p[t] = *(const u32x4*)(P[t] + r0); x.r[t] = R[t][k >> 1]; }
@@ -332,55 +334,58 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
         acc[t][2 * kk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[t], __builtin_bit_cast(bf16x8, lo), acc[t][2 * kk], 0, 0, 0);
         acc[t][2 * kk + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[t], __builtin_bit_cast(bf16x8, hi), acc[t][2 * kk + 1], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);           // (all operands made ahead of the products do not fit the registers)
     };
     full_steps<0, 8>(0, pair);
   };
-  Rows x0, x1;
+  // One loop with the next rows in a second set of registers, copied: with the two sets in turn the accumulators were copied instead, and went to scratch.
   int k = blk0 * 2 + wave;
-  if (k < step1) fetch(k, x0);
-  for (; k < step1; k += 8) {
-    if (k + 4 < step1) fetch(k + 4, x1);
-    compute(k, x0);
-    if (k + 4 >= step1) break;
-    if (k + 8 < step1) fetch(k + 8, x0);
-    compute(k + 4, x1);
-  }
-  // Wave w ends with operands 4 w .. 4 w + 3 of every tile: in three rounds each wave hands the quarter of another one over.
-  auto quarter = [&](int qd, auto f) {
-    if (qd == 0) f(std::integral_constant<int, 0>{});
-    else if (qd == 1) f(std::integral_constant<int, 1>{});
-    else if (qd == 2) f(std::integral_constant<int, 2>{});
-    else f(std::integral_constant<int, 3>{});
-  };
+  if (k < step1) {
+    Rows x;
+    fetch(k, x);
 #pragma unroll 1
-  for (int r = 1; r < 4; ++r) {
-    quarter((wave + r) & 3, [&](auto Q) {
+    for (;;) {
+      Rows next;
+      int kn = min(k + 4, step1 - 1);             // (past the wave's last step: rows that nothing takes)
+      asm volatile("" : "+s"(kn));               // (pointers are made anew each time, from uniform ones: kept across the loop they take 40 registers)
+      fetch(kn, next);
+      compute(k, x);
+      k += 4;
+      if (k >= step1) break;
+      x = next;
+    }
+  }
+  // Quarter by quarter: three waves hand theirs over, the fourth adds them in the order of the waves and stores the sum.  (Constant indices: with the wave's own
+  // quarter picked at run time the accumulators went to scratch, 27 us for a step that takes 8.)
+#pragma unroll
+  for (int qd = 0; qd < 4; ++qd) {
+    if (wave != qd) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) join[wave][t * 4 + j][lane] = acc[t][decltype(Q)::value * 4 + j];
-    });
+        for (int j = 0; j < 4; ++j) join[wave][t * 4 + j][lane] = acc[t][qd * 4 + j];
+    }
     __syncthreads();
-    quarter(wave, [&](auto Q) {
+    if (wave == qd) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t) {
+        f32x4 v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[t][decltype(Q)::value * 4 + j] += join[(wave - r) & 3][t * 4 + j][lane];
-    });
+        for (int j = 0; j < 4; ++j) {
+          v[j] = acc[t][qd * 4 + j];
+#pragma unroll
+          for (int w = 1; w < 4; ++w) v[j] += join[(qd + w) & 3][t * 4 + j][lane];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int h = h0 + t * 16 + kg * 4 + i;
+          if (h < a.H && c < a.d)
+            *(f32x4*)(a.C + (((long)b * a.nsplit + split) * a.H + h) * a.d + c + qd * 4) = f32x4{v[0][i], v[1][i], v[2][i], v[3][i]};
+        }
+      }
+    }
     __syncthreads();
   }
-  if (c >= a.d) return;
-  quarter(wave, [&](auto Q) {
-    constexpr int q0 = decltype(Q)::value * 4;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int h = h0 + t * 16 + kg * 4 + i;
-        if (h >= a.H) continue;
-        *(f32x4*)(a.C + (((long)b * a.nsplit + split) * a.H + h) * a.d + c + q0) = f32x4{acc[t][q0][i], acc[t][q0 + 1][i], acc[t][q0 + 2][i], acc[t][q0 + 3][i]};
-      }
-  });
 }
 
 // The same in fp32 on the vector ALU: a thread has eight columns and eight heads, numerators are uniform.  For caches of layers that are kept in full precision.
@@ -556,25 +561,32 @@ __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
   const bool mine_there = b < a.B && c < nj;
   const long o = (long)b * a.d + (long)h * a.d_k + j0 + c;
   if (a.csw > 1) {
+    // Partial results go past the L2s (each XCD has its own) and are read past them: a fence would write all of an L2 back, 60 us for the launch.
     if (mine_there) {
-      f32x4* p = (f32x4*)(a.part + (long)rs * a.B * a.d + o);
-      p[0] = f32x4{mine[0], mine[1], mine[2], mine[3]};
-      p[1] = f32x4{mine[4], mine[5], mine[6], mine[7]};
+      unsigned long long* p = (unsigned long long*)(a.part + (long)rs * a.B * a.d + o);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        __hip_atomic_store(p + j, (unsigned long long)__float_as_uint(mine[2 * j]) | (unsigned long long)__float_as_uint(mine[2 * j + 1]) << 32, __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
     }
-    __threadfence();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) last = atomicAdd(a.counters + blockIdx.z * gridDim.x + blockIdx.x, 1) == a.csw - 1;
+    if (tid == 0)
+      last = __hip_atomic_fetch_add(a.counters + blockIdx.z * gridDim.x + blockIdx.x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.csw - 1;
     __syncthreads();
     if (!last) return;
-    __threadfence();
     if (mine_there) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) mine[j] = 0.f;
+#pragma unroll 4
       for (int s = 0; s < a.csw; ++s) {
-        const f32x4* p = (const f32x4*)(a.part + (long)s * a.B * a.d + o);
-        const f32x4 lo = p[0], hi = p[1];
+        const unsigned long long* p = (const unsigned long long*)(a.part + (long)s * a.B * a.d + o);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { mine[k] += lo[k]; mine[4 + k] += hi[k]; }
+        for (int j = 0; j < 4; ++j) {
+          const unsigned long long x = __hip_atomic_load(p + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          mine[2 * j] += __uint_as_float((unsigned)x);
+          mine[2 * j + 1] += __uint_as_float((unsigned)(x >> 32));
+        }
       }
     }
   }
@@ -619,9 +631,9 @@ void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, i
   long want = (512 + units - 1) / units;
   want = want > QP_MAX_SPLITS ? QP_MAX_SPLITS : want;
   int p = (int)((nb + want - 1) / want);
-  *per = p < 4 ? 4 : p;
+  *per = p < 2 ? 2 : p;
   *nsplit = (nb + *per - 1) / *per;
-  *most_splits = (int)((nb + 3) / 4 < want ? (nb + 3) / 4 : want);
+  *most_splits = (int)((nb + 1) / 2 < want ? (nb + 1) / 2 : want);
   const int d_k = d / H, ct = (d_k + QP_COLS - 1) / QP_COLS;
   const long tiles = (long)H * ct * ((B + QP_BATCH - 1) / QP_BATCH);
   const int least = (d + QP_MAX_ROWS - 1) / QP_MAX_ROWS, most = d / 32;
