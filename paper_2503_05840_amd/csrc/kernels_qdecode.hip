@@ -73,9 +73,10 @@ __device__ __forceinline__ float sum_over_lanes(float v) {
 // A wave takes 64 rows x 64 / P heads; a head is P lanes of eight columns (those past d_k are idle).  Rows go P at a time, lane i of a head ends with the
 // 64 / P consecutive rows from i * 64 / P on, and the scale bytes of all 64 rows are one run of a lane's group.  From the scores come softmax numerators relative
 // to a power of two per head and block: a whole exponent, so that a later change of reference is exact in every type.
-// HBM-bound (0.53 or 1.03 bytes an element); about 20 instructions a row and lane, 45 with rotated keys.
+// HBM-bound (0.53 or 1.03 bytes an element); about 20 instructions a row and lane, 35 with rotated keys.
 template <bool F32, int BITS, int P, bool ROPE>
 __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
+  __shared__ f32x4 table[ROPE && P <= 16 ? QUANT_ROWS * P * 2 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   {
     const long wgs = (long)gridDim.x * gridDim.y * gridDim.z, wg = blockIdx.x + (long)gridDim.x * (blockIdx.y + (long)gridDim.y * blockIdx.z);
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
   const bool on = h < a.H && i * 8 < a.d_k;
   const int col = on ? h * a.d_k + i * 8 : 0;
   float qf[8];
-  unsigned qb[4];
+  unsigned qb[4], qr[4];                          // pairs (q0, q1) and (-q1, q0)
   if constexpr (F32) {
     const f32x4* src = (const f32x4*)((const float*)a.q + (long)b * a.d + col);
     const f32x4 lo = src[0], hi = src[1];
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
   } else {
     const u32x4 v = *(const u32x4*)((const uint16_t*)a.q + (long)b * a.d + col);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) { qb[j] = v[j]; qf[2 * j] = __uint_as_float(v[j] << 16); qf[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u); }
+    for (int j = 0; j < 4; ++j) { qb[j] = v[j]; qr[j] = ((v[j] >> 16) ^ 0x8000u) | v[j] << 16; qf[2 * j] = __uint_as_float(v[j] << 16); qf[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u); }
   }
   const unsigned char* codes = a.codes + ((long)b * a.stride + t0) * (a.d * BITS / 8) + col * BITS / 8;
   const u32x4* sp = (const u32x4*)(a.scales + ((long)b * (a.d / 32) + col / 32) * a.stride + t0);
@@ -122,15 +123,30 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
       const Codes8<BITS>& c = w[cur][r];
       float x = 0.f;
       if constexpr (ROPE) {
-        // (rows behind the sequence, whose score is masked, have no position in the table)
-        const f32x4* cs = (const f32x4*)(a.rope + ((long)min(t0 + row, len - 1) * (a.d_k / 2) + (on ? i * 4 : 0)) * 2);
-        const f32x4 t[2] = {cs[0], cs[1]};
+        f32x4 t[2];
+        if constexpr (P <= 16) {
+          const f32x4* cs = table + (row * (P * 2) + i * 2);
+          t[0] = cs[0]; t[1] = cs[1];
+        } else {
+          // (rows behind the sequence, whose score is masked, have no position in the table)
+          const f32x4* cs = (const f32x4*)(a.rope + ((long)min(t0 + row, len - 1) * (a.d_k / 2) + (on ? i * 4 : 0)) * 2);
+          t[0] = cs[0]; t[1] = cs[1];
+        }
         auto pair = [&](auto K) {
           constexpr int k = decltype(K)::value;
-          const f32x2 y = c.template f32<k>(f);
           const float co = t[k >> 1][2 * (k & 1)], si = t[k >> 1][2 * (k & 1) + 1];
-          x = fmaf(qf[2 * k], fmaf(y[0], co, y[1] * si), x);
-          x = fmaf(qf[2 * k + 1], fmaf(y[1], co, -(y[0] * si)), x);
+          float u, w;                              // q . y and q . (y turned by a quarter): the score is u cos + w sin
+          if constexpr (F32) {
+            const f32x2 y = c.template f32<k>(f);
+            u = fmaf(qf[2 * k], y[0], qf[2 * k + 1] * y[1]);
+            w = fmaf(qf[2 * k], y[1], -(qf[2 * k + 1] * y[0]));
+          } else {
+            const bf16x2 y = __builtin_bit_cast(bf16x2, c.template bf16<k>(f));
+            u = __builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, qb[k]), 0.f, false);
+            w = __builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, qr[k]), 0.f, false);
+          }
+          x = fmaf(co, u, x);
+          x = fmaf(si, w, x);
         };
         pair(std::integral_constant<int, 0>{}); pair(std::integral_constant<int, 1>{});
         pair(std::integral_constant<int, 2>{}); pair(std::integral_constant<int, 3>{});
@@ -156,6 +172,15 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
     s[decltype(J)::value] = sums_to_lanes<P>(v, lane);
   };
   fetch(0, std::integral_constant<int, 0>{});
+  if constexpr (ROPE && P <= 16) {
+    // The 64 rows' cos and sin, which 16 and more heads share: to LDS once (32 KB for 128 columns).  Asked for from memory by every head they took as long as the codes.
+    const int per = a.d_k / 4;
+    for (int x = tid; x < QUANT_ROWS * P * 2; x += 256) {
+      const int row = x / (P * 2), k = x % (P * 2);
+      if (k < per) table[x] = *(const f32x4*)(a.rope + (long)min(t0 + row, len - 1) * a.d_k + k * 4);
+    }
+    __syncthreads();
+  }
   auto both = [&](int j, auto J) {
     if constexpr (decltype(J)::value + 1 < RP) fetch(decltype(J)::value + 1, std::integral_constant<int, (decltype(J)::value + 1) & 1>{});
     step(j, J);
@@ -256,7 +281,6 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
   const int len = seq_len_of(a.seq_lens, b, a.T);
   int blk0, blk1;
   if (!split_blocks(a, len, split, blk0, blk1)) return;
-  split_references(a, b, split, blk0, blk1, h0, 16 * NT, blockIdx.x == 0, mref);
   const int n = lane & 15, kg = lane >> 4;
   const int c = blockIdx.x * QW_COLS + n * 16;
   const int cc = min(c, a.d - 16);               // (columns past the row's end: anything, not stored)
@@ -266,7 +290,6 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int h = min(h0 + t * 16 + n, a.H - 1);  // (heads past the last: anything, not stored)
-    m[t] = mref[h - h0];
     P[t] = (const uint16_t*)a.P + ((long)b * a.H + h) * a.Tp + kg * 8;
     R[t] = a.ref + ((long)b * a.H + h) * a.NB;
   }
@@ -340,9 +363,12 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
   };
   // One loop with the next rows in a second set of registers, copied: with the two sets in turn the accumulators were copied instead, and went to scratch.
   int k = blk0 * 2 + wave;
+  Rows x;
+  if (k < step1) fetch(k, x);                      // (on its way while the references are looked up)
+  split_references(a, b, split, blk0, blk1, h0, 16 * NT, blockIdx.x == 0, mref);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) m[t] = mref[min(h0 + t * 16 + n, a.H - 1) - h0];
   if (k < step1) {
-    Rows x;
-    fetch(k, x);
 #pragma unroll 1
     for (;;) {
       Rows next;
@@ -483,25 +509,51 @@ __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
   __shared__ __align__(16) char operand[F32 ? QP_BATCH * QP_MAX_ROWS * 4 : 2 * QP_BATCH * (QP_MAX_ROWS + 8) * 2];
   __shared__ f32x4 join[4][8][64];
   __shared__ int last;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ct = (a.d_k + QP_COLS - 1) / QP_COLS;
   const int h = blockIdx.x / ct, j0 = blockIdx.x % ct * QP_COLS, rs = blockIdx.y, b0 = blockIdx.z * QP_BATCH;
   const int cr0 = rs * a.crows, rows = min(a.crows, a.d - cr0);
+  // W's first rows are on their way while the splits are merged: all of a workgroup's, 256 at the most.
+  const int nj = min(QP_COLS, a.d_k - j0), n = lane & 15, kg = lane >> 4;
+  const bool in = n * 8 < nj;
+  u32x4 w[F32 ? 1 : 2][8];
+  if constexpr (!F32) {
+    const uint16_t* W = (const uint16_t*)a.W + (long)h * a.d_k + j0 + (in ? n * 8 : 0);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      if (wave * 32 + x * 128 < rows) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[x][i] = *(const u32x4*)(W + (long)(cr0 + wave * 32 + x * 128 + kg * 8 + i) * a.d);      // (32 rows: all there or none)
+      }
+  }
   split_weights(a, b0, h, wt);
   __syncthreads();
-  // merge: four columns a thread, 16 threads a sequence
+  // Merge: four columns a lane, a wave takes whole sequences, or with fewer than four a part of the splits each.  All loads of a sequence are on their way at once.
   {
-    const int j = tid >> 4, b = b0 + j, used = __float_as_int(wt[j][QP_MAX_SPLITS]);
-    const int padded = F32 ? rows : (rows + 31) / 32 * 32;
-    for (int r = (tid & 15) * 4; r < padded; r += 64) {
+    const int seqs = min(QP_BATCH, a.B - b0), padded = F32 ? rows : (rows + 31) / 32 * 32, r = lane * 4;
+    const int G = seqs >= 3 ? 1 : seqs == 2 ? 2 : 4;
+    f32x4* parts = &join[0][0][0];
+    for (int j = wave / G; j < QP_BATCH; j += 4 / G) {
       f32x4 v = {0.f, 0.f, 0.f, 0.f};
-      if (r < rows)
-        for (int s = 0; s < used; ++s) {
-          const f32x4 x = *(const f32x4*)(a.C + (((long)b * a.nsplit + s) * a.H + h) * a.d + cr0 + r);
+      const int b = b0 + j, used = __float_as_int(wt[j][QP_MAX_SPLITS]);
+      if (r < rows) {
+        const float* src = a.C + ((long)b * a.nsplit * a.H + h) * a.d + cr0 + r;
+#pragma unroll 8
+        for (int s = wave % G; s < used; s += G) {
+          const f32x4 x = *(const f32x4*)(src + (long)s * a.H * a.d);
           const float f = wt[j][s];
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[k] = fmaf(f, x[k], v[k]);
         }
+      }
+      if (G > 1 && j == wave / G) {                // (the first turn has all sequences that there are)
+        parts[wave * 64 + lane] = v;
+        __syncthreads();
+        if (wave % G == 0)
+          for (int g = 1; g < G; ++g) v += parts[(wave + g) * 64 + lane];
+        __syncthreads();
+      }
+      if (wave % G != 0 || r >= padded) continue;
       if constexpr (F32) {
         *(f32x4*)(operand + (j * QP_MAX_ROWS + r) * 4) = v;
       } else {
@@ -515,20 +567,17 @@ __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
     }
   }
   __syncthreads();
-  const int nj = min(QP_COLS, a.d_k - j0);
   float mine[8];                                 // this thread's results: sequence tid / 16, columns 8 (tid % 16) ...
   if constexpr (!F32) {
-    const int n = lane & 15, kg = lane >> 4;
-    const bool in = n * 8 < nj;
-    const uint16_t* W = (const uint16_t*)a.W + (long)h * a.d_k + j0 + (in ? n * 8 : 0);
     f32x4 acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int r = wave * 32; r < rows; r += 128) {
-      u32x4 kt[8], t[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) kt[i] = *(const u32x4*)(W + (long)min(cr0 + r + kg * 8 + i, a.d - 1) * a.d);     // (d is a multiple of 32: no row is past the end)
-      transpose8x8(kt, t);
+    for (int x = 0; x < 2; ++x) {
+      const int r = wave * 32 + x * 128;
+      if (r >= rows) break;
+      u32x4 t[8];
+      transpose8x8(w[x], t);
       const bf16x8 hi = *(const bf16x8*)(operand + (n * (QP_MAX_ROWS + 8) + r + kg * 8) * 2);
       const bf16x8 lo = *(const bf16x8*)(operand + ((QP_BATCH + n) * (QP_MAX_ROWS + 8) + r + kg * 8) * 2);
 #pragma unroll
@@ -623,12 +672,16 @@ void scores_by_width(const QDecodeArgs& a, hipStream_t st) {
 
 int qdecode_counters(int B, int H, int d) { return H * ((d / H + QP_COLS - 1) / QP_COLS) * ((B + QP_BATCH - 1) / QP_BATCH); }
 
-// How the work is cut: splits of the weighted sum so that about 512 workgroups (two a compute unit) share it, each of 256 rows at least (a step of 32 rows for
-// every wave, twice), and row splits of W likewise.  (The splits themselves go up and down with T.)
+// How the work is cut.  Splits of the weighted sum: a workgroup for every compute unit (with two, one sequence of 16384 rows x 4096 took 18.6 us instead of 15.9, as
+// much more to write and merge), but of 1024 rows at the most where that does not make more than four a unit: sequences of a batch are not equally long (16 of up
+// to 5000 rows x 2304 in 8 bits: two splits 38.6 us, four 28.6).  128 rows at least: a step of 32 for every wave.  Row splits of W: two workgroups a unit.
+// (The splits themselves go up and down with T; `most_splits` only grows.)
 void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* most_splits, int* csw, int* crows) {
   const int nb = (T + QUANT_ROWS - 1) / QUANT_ROWS;
   const long units = dtype == DT_F32 ? (long)B * ((d + 511) / 512) * ((H + 7) / 8) : (long)B * ((d + QW_COLS - 1) / QW_COLS) * ((H + 31) / 32);
-  long want = (512 + units - 1) / units;
+  long want = (256 + units - 1) / units, even = (nb + 15) / 16;
+  if (even > 1024 / units) even = 1024 / units;
+  if (want < even) want = even;
   want = want > QP_MAX_SPLITS ? QP_MAX_SPLITS : want;
   int p = (int)((nb + want - 1) / want);
   *per = p < 2 ? 2 : p;
