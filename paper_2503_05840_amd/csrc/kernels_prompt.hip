@@ -20,41 +20,61 @@ template <int PC> __device__ __forceinline__ int v_swap(int row) { return PC >= 
 // One pass over the keys with a running reference and sum a query.  Products are 32x32x16: S^T = K Q^T, whose result has a query's scores in two lanes, so that
 // maxima and sums are the lane's own but for one exchange; its registers, rounded to bf16, are the operand of O^T += V^T P^T as they are, V's
 // operand being read in the same order of keys (transposed reads of four rows).
-template <int DKP>
+template <int DKP, bool WHOLE>
 __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
   constexpr int PC = Pitch<DKP>::pieces, NS = DKP / 16, NV = DKP / 32;
   __shared__ __align__(16) char tiles[2][2][PK * PC * 16];       // [buffer][keys, values]
   PromptTile t;
   if (!prompt_tile(a, PQ, t)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
   const int hk = t.h / (a.H / a.H_kv);
   const int i = min(t.i0 + wave * 32 + n, t.n_q - 1);          // this lane's query (past the last: the last, not stored)
   const int off = t.n_k - t.n_q;
   const int sees = a.causal ? i + off : t.n_k - 1;               // its last key
-  const int wave_first = a.causal ? min(t.i0 + wave * 32, t.n_q - 1) + off : t.n_k - 1;
   const int wave_last = a.causal ? min(t.i0 + wave * 32 + 31, t.n_q - 1) + off : t.n_k - 1;
   const int end = a.causal ? min(t.i0 + PQ, t.n_q) + off : t.n_k;     // keys that the workgroup needs
   const int all = end > 0 ? (end + PK - 1) / PK : 0, per = (all + a.nsplit - 1) / a.nsplit;
   const int tile0 = t.split * per, tile1 = min(tile0 + per, all);
-  const bool clear = a.d_k < PC * 8;
 
   const uint16_t* K = (const uint16_t*)a.k + t.k0 * a.k_pitch + (long)hk * a.d_k;
   const uint16_t* V = (const uint16_t*)a.v + t.k0 * a.v_pitch + (long)hk * a.d_k;
-  if (clear) {                                                     // pieces past d_k: zeros that nothing is loaded over
+  if constexpr (!WHOLE) {                                          // pieces past d_k: zeros that nothing is loaded over
     const u32x4 zero = {0u, 0u, 0u, 0u};
     for (int x = tid; x < 4 * PK * PC; x += 256) ((u32x4*)tiles)[x] = zero;
     __syncthreads();
   }
   const int pieces = a.d_k / 8;
+  constexpr int NX = PK * PC / 256, XR = 256 / PC;                 // loads of a wave for a tile's keys, rows between them
+  constexpr unsigned PAIR = 2 * PK * PC * 16;                      // a buffer: keys, then values
+  const int row0 = (wave * 64 + lane) / PC, place = lane % PC;
+  // (rows of one lane are 16 or more apart, or pairs of them are: their pieces are swapped alike)
+  constexpr int NC = PC == 32 ? 2 : 1;
+  unsigned ko[NC], vo[NC];
+  int ck[NC], cv[NC];
+#pragma unroll
+  for (int x = 0; x < NC; ++x) {
+    ck[x] = place ^ k_swap<PC>(row0 + x * XR);
+    cv[x] = place ^ v_swap<PC>(row0 + x * XR);
+    ko[x] = (unsigned)(row0 * (int)a.k_pitch + ck[x] * 8) * 2;
+    vo[x] = (unsigned)(row0 * (int)a.v_pitch + cv[x] * 8) * 2;
+  }
+  const unsigned lds0 = lds_address(tiles) + wave * 1024;
   auto load = [&](int tile, int buf) {
     const int key0 = tile * PK;
+    const unsigned to = lds0 + buf * PAIR;
+    if (key0 + PK <= t.n_k) {
 #pragma unroll
-    for (int x = 0; x < PK * PC / 256; ++x) {
-      const int at = (x * 4 + wave) * 64 + lane, row = at / PC, place = at % PC;
-      const long key = min(key0 + row, t.n_k - 1);                 // (rows past the last are masked)
-      const int ck = place ^ k_swap<PC>(row), cv = place ^ v_swap<PC>(row);
-      if (!clear || ck < pieces) load_to_lds(K + key * a.k_pitch + ck * 8, lds_address(tiles[buf][0]) + (x * 4 + wave) * 1024);
-      if (!clear || cv < pieces) load_to_lds(V + key * a.v_pitch + cv * 8, lds_address(tiles[buf][1]) + (x * 4 + wave) * 1024);
+      for (int x = 0; x < NX; ++x) {
+        if (WHOLE || ck[x % NC] < pieces) load_to_lds(K + (key0 + x * XR) * a.k_pitch, ko[x % NC], to + x * 4096);
+        if (WHOLE || cv[x % NC] < pieces) load_to_lds(V + (key0 + x * XR) * a.v_pitch, vo[x % NC], to + PAIR / 2 + x * 4096);
+      }
+    } else {                                                       // rows past the last: the last, masked
+#pragma unroll
+      for (int x = 0; x < NX; ++x) {
+        const long key = min(key0 + row0 + x * XR, t.n_k - 1);
+        if (WHOLE || ck[x % NC] < pieces) load_to_lds(K + key * a.k_pitch + ck[x % NC] * 8, to + x * 4096);
+        if (WHOLE || cv[x % NC] < pieces) load_to_lds(V + key * a.v_pitch + cv[x % NC] * 8, to + PAIR / 2 + x * 4096);
+      }
     }
   };
 
@@ -76,36 +96,40 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     for (int r = 0; r < 16; ++r) o[v][r] = 0.f;
   float ref = NEG_INF, sum = 0.f;
 
-  if (tile0 < tile1) load(tile0, 0);
-  for (int tile = tile0; tile < tile1; ++tile) {
-    const int buf = (tile - tile0) & 1, key0 = tile * PK;
-    tiles_barrier();
-    if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
-    if (key0 > wave_last) continue;
-    const char* kt = tiles[buf][0];
-    const char* vt = tiles[buf][1];
+  // This lane's places in the buffer of the present tile: a key's pieces, and four rows of values (rows 8 and more further on are swapped alike)
+  unsigned ka[NS], va[NV];
+#pragma unroll
+  for (int k = 0; k < NS; ++k) ka[k] = (unsigned)(n * PC + ((2 * k + half) ^ k_swap<PC>(n))) * 16;
+  {
+    const int row = 4 * half + ((lane & 15) >> 2), byte = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) va[v] = PAIR / 2 + (unsigned)(row * PC + ((v * 4 + (byte >> 4)) ^ v_swap<PC>(row))) * 16 + (byte & 15);
+  }
+  // One tile.  MASKED: some queries of the wave do not see all of its keys.
+  const char* const lds = (const char*)tiles;
+  auto attend = [&](int key0, int buf, auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const char* const vt = lds + buf * PAIR + PAIR / 2;
     f32x16 s[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
-      const int row = x * 32 + n;
 #pragma unroll
       for (int k = 0; k < NS; ++k) {
-        const bf16x8 A = *(const bf16x8*)(kt + (row * PC + ((2 * k + half) ^ k_swap<PC>(row))) * 16);
+        const bf16x8 A = *(const bf16x8*)(lds + ka[k] + x * (32 * PC * 16));
         s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, q[k], s[x], 0, 0, 0);
       }
     }
-    const bool masked = key0 + PK - 1 > wave_first;
-    unsigned long long bad = 0;                                  // rows of values that are not finite, where some queries do not see all rows
-    if (masked) {
+    unsigned long long bad = 0;                                  // rows of values that are not finite
+    if constexpr (MASKED) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (key0 + x * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > sees) s[x][r] = NEG_INF;
       u16x2 top = {0, 0};
-#pragma unroll
+#pragma unroll 4
       for (int c = 0; c < PC; ++c) {
         const u32x4 v = *(const u32x4*)(vt + (lane * PC + (c ^ (lane & (PC - 1)))) * 16);
 #pragma unroll
@@ -138,52 +162,76 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
         s[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -base));
         sum += s[x][r];
       }
-    const int tr_row = 4 * half + ((lane & 15) >> 2), tr_col = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;      // (bytes)
+    auto add_values = [&](auto with_bad) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      bf16x8 p;
+      for (int k = 0; k < 4; ++k) {
+        bf16x8 p;
 #pragma unroll
-      for (int r = 0; r < 8; ++r) p[r] = (__bf16)s[k >> 1][(k & 1) * 8 + r];
+        for (int r = 0; r < 8; ++r) p[r] = (__bf16)s[k >> 1][(k & 1) * 8 + r];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        u32x4 A;
+        for (int v = 0; v < NV; ++v) {
+          u32x4 A;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const int row = k * 16 + g * 8 + tr_row, byte = v * 64 + tr_col;
-          const char* at = vt + (row * PC + ((byte >> 4) ^ v_swap<PC>(row))) * 16 + (byte & 15);
-          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
-          A[2 * g] = x[0];
-          A[2 * g + 1] = x[1];
-        }
-        if (bad) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (bad >> (k * 16 + (e >> 2) * 8 + 4 * half + (e & 3)) & 1) A[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
-        }
-        o[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, A), p, o[v], 0, 0, 0);
-      }
-    }
-    // A row with a value that is not finite goes to the queries that see it one by one.
-    while (bad) {
-      const int row = __ffsll((long long)bad) - 1;
-      bad &= bad - 1;
-      const int reg = (row >> 5) * 16 + ((row & 31) >> 3) * 4 + (row & 3);
-      float p = 0.f;
-#pragma unroll
-      for (int x = 0; x < 32; ++x) p = x == reg ? s[x >> 4][x & 15] : p;
-      p = __shfl(p, n + 32 * ((row >> 2) & 1));
-      if (key0 + row <= sees) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int c = v * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-            const uint16_t x = *(const uint16_t*)(vt + (row * PC + ((c >> 3) ^ v_swap<PC>(row))) * 16 + (c & 7) * 2);
-            o[v][r] = fmaf(p, __uint_as_float((unsigned)x << 16), o[v][r]);
+          for (int g = 0; g < 2; ++g) {
+            const char* at = lds + va[v] + (k * 16 + g * 8) * PC * 16;
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+            A[2 * g] = x[0];
+            A[2 * g + 1] = x[1];
           }
+          if constexpr (decltype(with_bad)::value) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (bad >> (k * 16 + (e >> 2) * 8 + 4 * half + (e & 3)) & 1) A[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
+          }
+          o[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, A), p, o[v], 0, 0, 0);
+        }
+      }
+    };
+    if (!MASKED || !bad) {
+      add_values(std::false_type{});
+      return;
+    }
+    if constexpr (MASKED) {
+      add_values(std::true_type{});
+      // A row with a value that is not finite goes to the queries that see it one by one.
+      while (bad) {
+        const int row = __ffsll((long long)bad) - 1;
+        bad &= bad - 1;
+        const int reg = (row >> 5) * 16 + ((row & 31) >> 3) * 4 + (row & 3);
+        float p = 0.f;
+#pragma unroll
+        for (int x = 0; x < 32; ++x) p = x == reg ? s[x >> 4][x & 15] : p;
+        p = __shfl(p, n + 32 * ((row >> 2) & 1));
+        if (key0 + row <= sees) {
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int c = v * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+              const uint16_t x = *(const uint16_t*)(vt + (row * PC + ((c >> 3) ^ v_swap<PC>(row))) * 16 + (c & 7) * 2);
+              o[v][r] = fmaf(p, __uint_as_float((unsigned)x << 16), o[v][r]);
+            }
+        }
       }
     }
-  }
+  };
+  // Tiles that all queries of the workgroup see, then the rest
+  const int seen = (a.causal ? t.i0 + off + 1 : t.n_k) / PK, whole = min(max(seen, tile0), tile1);
+  auto turn = [&](int tile, auto masked) {
+    const int buf = (tile - tile0) & 1;
+    tiles_barrier();
+    if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
+    if (!decltype(masked)::value || tile * PK <= wave_last) attend(tile * PK, buf, masked);
+#pragma unroll
+    for (int k = 0; k < NS; ++k) ka[k] ^= PAIR;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) va[v] ^= PAIR;
+  };
+  if (tile0 < tile1) load(tile0, 0);
+#pragma unroll 1
+  for (int tile = tile0; tile < whole; ++tile) turn(tile, std::false_type{});
+#pragma unroll 1
+  for (int tile = whole; tile < tile1; ++tile) turn(tile, std::true_type{});
   sum = sum_of_halves(sum);
   if (t.i0 + wave * 32 + n >= t.n_q) return;
   const long row = (t.q0 + i) * a.H + t.h;
@@ -257,7 +305,10 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
 }
 
 template <int DKP>
-void prompt_of(const PromptArgs& a, hipStream_t st) { prompt_kernel<DKP><<<prompt_grid(a, PQ), 256, 0, st>>>(a); }
+void prompt_of(const PromptArgs& a, hipStream_t st) {
+  if (a.d_k == Pitch<DKP>::pieces * 8) prompt_kernel<DKP, true><<<prompt_grid(a, PQ), 256, 0, st>>>(a);
+  else prompt_kernel<DKP, false><<<prompt_grid(a, PQ), 256, 0, st>>>(a);
+}
 
 }  // namespace
 

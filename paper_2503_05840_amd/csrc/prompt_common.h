@@ -10,6 +10,12 @@ namespace slim {
 __device__ __forceinline__ void load_to_lds(const void* p, unsigned lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(__builtin_amdgcn_readfirstlane((int)lds)) : "memory");
 }
+// The same from a uniform pointer and a lane's offset in bytes
+__device__ __forceinline__ void load_to_lds(const void* base, unsigned offset, unsigned lds) {
+  const uint64_t p = (uint64_t)base;
+  const uint64_t u = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)p) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32;
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(u), "s"(__builtin_amdgcn_readfirstlane((int)lds)) : "memory");
+}
 __device__ __forceinline__ unsigned lds_address(const void* p) {
   return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
@@ -39,11 +45,13 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int rows, Promp
     const int mid = (lo + hi) >> 1;
     if (clamped(a.cu_q[mid], a.rows_q) / rows + mid <= place) lo = mid; else hi = mid;
   }
-  const int q0 = clamped(a.cu_q[lo], a.rows_q), q1 = clamped(a.cu_q[lo + 1], a.rows_q);
-  const int k0 = clamped(a.cu_k[lo], a.rows_k), k1 = clamped(a.cu_k[lo + 1], a.rows_k);
+  // (the same for the whole wave, and in scalar registers: pointers made from them stay there)
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int q0 = uniform(clamped(a.cu_q[lo], a.rows_q)), q1 = uniform(clamped(a.cu_q[lo + 1], a.rows_q));
+  const int k0 = uniform(clamped(a.cu_k[lo], a.rows_k)), k1 = uniform(clamped(a.cu_k[lo + 1], a.rows_k));
   t.q0 = q0; t.n_q = q1 - q0;
   t.k0 = k0; t.n_k = max(k1 - k0, 0);
-  const int j = place - (q0 / rows + lo);
+  const int j = place - uniform(q0 / rows + lo);
   t.i0 = j * rows;
   return j >= 0 && t.i0 < t.n_q;
 }

@@ -1092,6 +1092,7 @@ extern "C" int slim_quant_decode(const void* q, const void* codes, const void* s
 // ---- attention over whole prompts ----------------------------------------------------------------------
 namespace {
 
+constexpr int64_t PROMPT_MAX_PITCH = 1 << 24;      // (offsets inside a tile of 64 rows have 32 bits)
 constexpr int PROMPT_MAX_BATCH = 32768, PROMPT_MAX_ROWS = 1 << 24, PROMPT_MAX_HEADS = 4096;
 
 int check_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dtype) {
@@ -1127,6 +1128,7 @@ extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v
   if (k_pitch == 0) k_pitch = (int64_t)H_kv * d_k;
   if (v_pitch == 0) v_pitch = (int64_t)H_kv * d_k;
   const int vec = vec_elems(dtype);
+  if (q_pitch > PROMPT_MAX_PITCH || k_pitch > PROMPT_MAX_PITCH || v_pitch > PROMPT_MAX_PITCH) return SLIM_ERR_SHAPE;
   if (q_pitch < (int64_t)H * d_k || k_pitch < (int64_t)H_kv * d_k || v_pitch < (int64_t)H_kv * d_k || q_pitch % vec || k_pitch % vec || v_pitch % vec)
     return SLIM_ERR_SHAPE;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned4(cu_q) || misaligned4(cu_k)) return SLIM_ERR_ALIGN;
