@@ -162,37 +162,37 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
         s[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -base));
         sum += s[x][r];
       }
-    auto add_values = [&](auto with_bad) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        bf16x8 p;
+    for (int k = 0; k < 4; ++k) {
+      bf16x8 p;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) p[r] = (__bf16)s[k >> 1][(k & 1) * 8 + r];
+      for (int r = 0; r < 8; ++r) p[r] = (__bf16)s[k >> 1][(k & 1) * 8 + r];
+      unsigned keep[4];                                          // pairs of rows: which of them are finite
+      if constexpr (MASKED) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          u32x4 A;
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const char* at = lds + va[v] + (k * 16 + g * 8) * PC * 16;
-            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
-            A[2 * g] = x[0];
-            A[2 * g + 1] = x[1];
-          }
-          if constexpr (decltype(with_bad)::value) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (bad >> (k * 16 + (e >> 2) * 8 + 4 * half + (e & 3)) & 1) A[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
-          }
-          o[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, A), p, o[v], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) {
+          const unsigned two = (unsigned)(bad >> (k * 16 + (j >> 1) * 8 + 2 * (j & 1))) >> (4 * half);
+          keep[j] = (two & 1 ? 0u : 0xffffu) | (two & 2 ? 0u : 0xffff0000u);
         }
       }
-    };
-    if (!MASKED || !bad) {
-      add_values(std::false_type{});
-      return;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        u32x4 A;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const char* at = lds + va[v] + (k * 16 + g * 8) * PC * 16;
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+          A[2 * g] = x[0];
+          A[2 * g + 1] = x[1];
+        }
+        if constexpr (MASKED) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) A[j] &= keep[j];
+        }
+        o[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, A), p, o[v], 0, 0, 0);
+      }
     }
     if constexpr (MASKED) {
-      add_values(std::true_type{});
       // A row with a value that is not finite goes to the queries that see it one by one.
       while (bad) {
         const int row = __ffsll((long long)bad) - 1;
@@ -312,16 +312,23 @@ void prompt_of(const PromptArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Parts of the keys, where the queries alone do not fill the chip: a part has 256 keys at least.
+// Parts of the keys, where the queries alone do not fill the chip.  A workgroup's tile takes 1.2 us (bf16, 128 columns), 1.9 where two share a compute unit; the
+// parts' results are written and read in 32 bits (777 queries x 32 heads x 128 in two parts: 34 us, in one 21).
 int prompt_splits(int dtype, int B, int rows_q, int rows_k, int H, int d_k) {
-  const int rows = dtype == DT_F32 ? PROMPT_F32_ROWS : PQ;
-  const long tiles = (long)B * ((rows_q / B + rows - 1) / rows) * H;      // (as if the sequences were equally long)
-  if (tiles < 1 || tiles >= 256) return 1;
-  const long want = 512 / tiles, keys = rows_k / B / 256;
-  long n = want < keys ? want : keys;
-  n = n > 32 ? 32 : n;
-  (void)d_k;
-  return n < 1 ? 1 : (int)n;
+  const bool f32 = dtype == DT_F32;
+  const int rows = f32 ? PROMPT_F32_ROWS : PQ;
+  const double tiles = (double)B * ((rows_q / B + rows - 1) / rows) * H, keys = (double)rows_k / B / PK;      // (as if the sequences were equally long)
+  const double alone = f32 ? 1.7 * d_k / 64 : 1.2 * (d_k < 64 ? 64 : d_k) / 128, shared = f32 ? 2 * alone : 1.6 * alone;
+  int best = 1;
+  double least = 1e30;
+  for (int n = 1; n <= 32; ++n) {
+    if (n > 1 && (keys < 4 * n || tiles * n > 4096)) break;      // (a part has 256 keys at least)
+    const double per = ceil(keys / n), rounds = ceil(tiles * n / 512);
+    const double merge = n > 1 ? 4 + n * (double)rows_q * H * d_k * 8 / 4e6 : 0;
+    const double t = (tiles * n <= 256 ? per * alone : rounds * per * shared) + merge;
+    if (t < least) { least = t; best = n; }
+  }
+  return best;
 }
 
 void launch_prompt(int dtype, const PromptArgs& a, hipStream_t st) {

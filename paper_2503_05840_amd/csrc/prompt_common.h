@@ -37,9 +37,11 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int rows, Promp
   const int places = a.rows_q / rows + a.B, units = a.H * places * a.nsplit;
   const int per = (units + 7) / 8, unit = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
   if (((int)blockIdx.x >> 3) >= per || unit >= units) return false;
-  t.split = unit % a.nsplit;
-  t.h = unit / a.nsplit / places;
-  const int place = places - 1 - unit / a.nsplit % places;
+  // heads that share keys are next to each other: their workgroups read the same tiles at about the same time
+  const int G = a.H / a.H_kv, u = unit / G;
+  t.split = u % a.nsplit;
+  t.h = u / a.nsplit / places * G + unit % G;
+  const int place = places - 1 - u / a.nsplit % places;
   int lo = 0, hi = a.B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
