@@ -27,17 +27,16 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
   PromptTile t;
   if (!prompt_tile(a, PQ, t)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
-  const int hk = t.h / (a.H / a.H_kv);
   const int i = min(t.i0 + wave * 32 + n, t.n_q - 1);          // this lane's query (past the last: the last, not stored)
   const int off = t.n_k - t.n_q;
   const int sees = a.causal ? i + off : t.n_k - 1;               // its last key
   const int wave_last = a.causal ? min(t.i0 + wave * 32 + 31, t.n_q - 1) + off : t.n_k - 1;
   const int end = a.causal ? min(t.i0 + PQ, t.n_q) + off : t.n_k;     // keys that the workgroup needs
-  const int all = end > 0 ? (end + PK - 1) / PK : 0, per = (all + a.nsplit - 1) / a.nsplit;
+  const int all = end > 0 ? (end + PK - 1) / PK : 0, per = __builtin_amdgcn_readfirstlane((all + a.nsplit - 1) / a.nsplit);
   const int tile0 = t.split * per, tile1 = min(tile0 + per, all);
 
-  const uint16_t* K = (const uint16_t*)a.k + t.k0 * a.k_pitch + (long)hk * a.d_k;
-  const uint16_t* V = (const uint16_t*)a.v + t.k0 * a.v_pitch + (long)hk * a.d_k;
+  const uint16_t* K = (const uint16_t*)a.k + t.k0 * a.k_pitch + (long)t.hk * a.d_k;
+  const uint16_t* V = (const uint16_t*)a.v + t.k0 * a.v_pitch + (long)t.hk * a.d_k;
   if constexpr (!WHOLE) {                                          // pieces past d_k: zeros that nothing is loaded over
     const u32x4 zero = {0u, 0u, 0u, 0u};
     for (int x = tid; x < 4 * PK * PC; x += 256) ((u32x4*)tiles)[x] = zero;
@@ -58,15 +57,19 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     ko[x] = (unsigned)(row0 * (int)a.k_pitch + ck[x] * 8) * 2;
     vo[x] = (unsigned)(row0 * (int)a.v_pitch + cv[x] * 8) * 2;
   }
+  const uint64_t k_first = scalar((uint64_t)K), v_first = scalar((uint64_t)V), k_step = scalar((uint64_t)a.k_pitch * (2 * XR)), v_step = scalar((uint64_t)a.v_pitch * (2 * XR));
   const unsigned lds0 = lds_address(tiles) + wave * 1024;
   auto load = [&](int tile, int buf) {
-    const int key0 = tile * PK;
     const unsigned to = lds0 + buf * PAIR;
+    const int key0 = tile * PK;
     if (key0 + PK <= t.n_k) {
+      uint64_t kp = k_first + (uint64_t)(unsigned)(tile * NX) * k_step, vp = v_first + (uint64_t)(unsigned)(tile * NX) * v_step;
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
-        if (WHOLE || ck[x % NC] < pieces) load_to_lds(K + (key0 + x * XR) * a.k_pitch, ko[x % NC], to + x * 4096);
-        if (WHOLE || cv[x % NC] < pieces) load_to_lds(V + (key0 + x * XR) * a.v_pitch, vo[x % NC], to + PAIR / 2 + x * 4096);
+        if (WHOLE || ck[x % NC] < pieces) load_to_lds(kp, ko[x % NC], to + x * 4096);
+        if (WHOLE || cv[x % NC] < pieces) load_to_lds(vp, vo[x % NC], to + PAIR / 2 + x * 4096);
+        kp += k_step;
+        vp += v_step;
       }
     } else {                                                       // rows past the last: the last, masked
 #pragma unroll
@@ -78,6 +81,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     }
   };
 
+  if (tile0 < tile1) load(tile0, 0);
   bf16x8 q[NS];
   {
     const uint16_t* src = (const uint16_t*)a.q + (t.q0 + i) * a.q_pitch + (long)t.h * a.d_k;
@@ -88,6 +92,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
       if (c < a.d_k) x = *(const u32x4*)(src + c);
       q[s] = __builtin_bit_cast(bf16x8, x);
     }
+    own_loads_done();
   }
   f32x16 o[NV];
 #pragma unroll
@@ -111,6 +116,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     constexpr bool MASKED = decltype(masked)::value;
     const char* const vt = lds + buf * PAIR + PAIR / 2;
     f32x16 s[2];
+    __builtin_amdgcn_s_setprio(1);                 // (the SIMD's other wave fills in: sequences of 8000 and 5000 keys x 24 heads x 96 75 -> 71 us)
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -121,6 +127,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
         s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, q[k], s[x], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     unsigned long long bad = 0;                                  // rows of values that are not finite
     if constexpr (MASKED) {
 #pragma unroll
@@ -128,14 +135,19 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (key0 + x * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > sees) s[x][r] = NEG_INF;
-      u16x2 top = {0, 0};
+      // (a lane a row: zero times what is not finite is NaN, and stays)
+      float top = 0.f;
+      const bf16x2 zero = {(__bf16)0.f, (__bf16)0.f};
 #pragma unroll 4
       for (int c = 0; c < PC; ++c) {
         const u32x4 v = *(const u32x4*)(vt + (lane * PC + (c ^ (lane & (PC - 1)))) * 16);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[y] & 0x7fff7fffu));
+        for (int y = 0; y < 4; ++y) {
+          const unsigned two = v[y];
+          top = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), zero, top, false);
+        }
       }
-      bad = __ballot(top[0] >= 0x7f80 || top[1] >= 0x7f80);
+      bad = __ballot(top != 0.f);
     }
     float m = NEG_INF;
 #pragma unroll
@@ -167,14 +179,6 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
       bf16x8 p;
 #pragma unroll
       for (int r = 0; r < 8; ++r) p[r] = (__bf16)s[k >> 1][(k & 1) * 8 + r];
-      unsigned keep[4];                                          // pairs of rows: which of them are finite
-      if constexpr (MASKED) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const unsigned two = (unsigned)(bad >> (k * 16 + (j >> 1) * 8 + 2 * (j & 1))) >> (4 * half);
-          keep[j] = (two & 1 ? 0u : 0xffffu) | (two & 2 ? 0u : 0xffff0000u);
-        }
-      }
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         u32x4 A;
@@ -185,9 +189,12 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
           A[2 * g] = x[0];
           A[2 * g + 1] = x[1];
         }
-        if constexpr (MASKED) {
+        if (MASKED && bad) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) A[j] &= keep[j];
+          for (int j = 0; j < 4; ++j) {                          // pairs of rows: which of them are finite
+            const unsigned two = (unsigned)(bad >> (k * 16 + (j >> 1) * 8 + 2 * (j & 1))) >> (4 * half);
+            A[j] &= (two & 1 ? 0u : 0xffffu) | (two & 2 ? 0u : 0xffff0000u);
+          }
         }
         o[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, A), p, o[v], 0, 0, 0);
       }
@@ -219,7 +226,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
   const int seen = (a.causal ? t.i0 + off + 1 : t.n_k) / PK, whole = min(max(seen, tile0), tile1);
   auto turn = [&](int tile, auto masked) {
     const int buf = (tile - tile0) & 1;
-    tiles_barrier();
+    tiles_barrier<0>();
     if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
     if (!decltype(masked)::value || tile * PK <= wave_last) attend(tile * PK, buf, masked);
 #pragma unroll
@@ -227,7 +234,6 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
 #pragma unroll
     for (int v = 0; v < NV; ++v) va[v] ^= PAIR;
   };
-  if (tile0 < tile1) load(tile0, 0);
 #pragma unroll 1
   for (int tile = tile0; tile < whole; ++tile) turn(tile, std::false_type{});
 #pragma unroll 1

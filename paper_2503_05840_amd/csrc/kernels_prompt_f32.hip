@@ -23,18 +23,17 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(Pro
   __shared__ __align__(16) char tiles[2][2][PK * PC * 16];       // [buffer][keys, values]
   PromptTile t;
   if (!prompt_tile(a, PROMPT_F32_ROWS, t)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
-  const int hk = t.h / (a.H / a.H_kv);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
   const int i = min(t.i0 + wave * 16 + n, t.n_q - 1);
   const int off = t.n_k - t.n_q;
   const int sees = a.causal ? i + off : t.n_k - 1;
   const int wave_first = a.causal ? min(t.i0 + wave * 16, t.n_q - 1) + off : t.n_k - 1;
   const int wave_last = a.causal ? min(t.i0 + wave * 16 + 15, t.n_q - 1) + off : t.n_k - 1;
   const int end = a.causal ? min(t.i0 + PROMPT_F32_ROWS, t.n_q) + off : t.n_k;
-  const int all = end > 0 ? (end + PK - 1) / PK : 0, per = (all + a.nsplit - 1) / a.nsplit;
+  const int all = end > 0 ? (end + PK - 1) / PK : 0, per = __builtin_amdgcn_readfirstlane((all + a.nsplit - 1) / a.nsplit);
   const int tile0 = t.split * per, tile1 = min(tile0 + per, all);
-  const float* K = (const float*)a.k + t.k0 * a.k_pitch + (long)hk * a.d_k;
-  const float* V = (const float*)a.v + t.k0 * a.v_pitch + (long)hk * a.d_k;
+  const float* K = (const float*)a.k + t.k0 * a.k_pitch + (long)t.hk * a.d_k;
+  const float* V = (const float*)a.v + t.k0 * a.v_pitch + (long)t.hk * a.d_k;
   const bool clear = a.d_k < PC * 4;
   if (clear) {
     const u32x4 zero = {0u, 0u, 0u, 0u};
@@ -53,6 +52,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(Pro
       if (!clear || place < pieces) load_to_lds(V + key * a.v_pitch + place * 4, lds_address(tiles[buf][1]) + (x * 4 + wave) * 1024);
     }
   };
+  if (tile0 < tile1) load(tile0, 0);
   f32x4 q[NS];
   {
     const float* src = (const float*)a.q + (t.q0 + i) * a.q_pitch + (long)t.h * a.d_k;
@@ -62,6 +62,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(Pro
       q[s] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (c < a.d_k) q[s] = *(const f32x4*)(src + c);
     }
+    own_loads_done();
   }
   f32x4 o[NV][4];
 #pragma unroll
@@ -69,10 +70,9 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(Pro
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[v][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float ref = NEG_INF, sum = 0.f;
-  if (tile0 < tile1) load(tile0, 0);
   for (int tile = tile0; tile < tile1; ++tile) {
     const int buf = (tile - tile0) & 1, key0 = tile * PK;
-    tiles_barrier();
+    tiles_barrier<0>();
     if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
     if (key0 > wave_last) continue;
     const char* kt = tiles[buf][0];

@@ -10,22 +10,30 @@ namespace slim {
 __device__ __forceinline__ void load_to_lds(const void* p, unsigned lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(__builtin_amdgcn_readfirstlane((int)lds)) : "memory");
 }
-// The same from a uniform pointer and a lane's offset in bytes
-__device__ __forceinline__ void load_to_lds(const void* base, unsigned offset, unsigned lds) {
-  const uint64_t p = (uint64_t)base;
-  const uint64_t u = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)p) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32;
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(u), "s"(__builtin_amdgcn_readfirstlane((int)lds)) : "memory");
+// A value that is the same for the whole wave, in scalar registers
+__device__ __forceinline__ uint64_t scalar(uint64_t v) {
+  uint64_t u = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)v) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
+  asm volatile("" : "+s"(u));
+  return u;
+}
+// The same from such a pointer and a lane's offset in bytes
+__device__ __forceinline__ void load_to_lds(uint64_t base, unsigned offset, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane((int)lds)) : "memory");
 }
 __device__ __forceinline__ unsigned lds_address(const void* p) {
   return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
-// The tiles that this wave asked for are there, then everybody's; and everybody is done with the buffer that is filled next.
-__device__ __forceinline__ void tiles_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// The tiles that this wave asked for are there but for the last LEFT loads, then everybody's; and everybody is done with the buffer that is filled next.
+template <int LEFT>
+__device__ __forceinline__ void tiles_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LEFT) : "memory"); }
+
+// This wave's own loads are there.  (The builtin, which the compiler counts: it would wait for them at their first use, inside a loop, and for the tiles on their way too.)
+__device__ __forceinline__ void own_loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 struct PromptTile {
   long q0, k0;            // first rows of the sequence
   int n_q, n_k, i0;       // its rows, and the tile's first query
-  int h, split;
+  int h, hk, split;       // head, its keys' head, part of the keys
 };
 
 __device__ __forceinline__ int clamped(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
@@ -38,17 +46,19 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int rows, Promp
   const int per = (units + 7) / 8, unit = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
   if (((int)blockIdx.x >> 3) >= per || unit >= units) return false;
   // heads that share keys are next to each other: their workgroups read the same tiles at about the same time
-  const int G = a.H / a.H_kv, u = unit / G;
-  t.split = u % a.nsplit;
-  t.h = u / a.nsplit / places * G + unit % G;
-  const int place = places - 1 - u / a.nsplit % places;
+  // (All of it is the same for the whole wave, and is told so: pointers made from it stay in scalar registers.)
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int G = uniform(a.H / a.H_kv), u = uniform(unit / G), r = unit - u * G;
+  const int w = uniform(u / a.nsplit);
+  t.split = u - w * a.nsplit;
+  t.hk = uniform(w / places);
+  t.h = t.hk * G + r;
+  const int place = places - 1 - (w - t.hk * places);
   int lo = 0, hi = a.B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (clamped(a.cu_q[mid], a.rows_q) / rows + mid <= place) lo = mid; else hi = mid;
   }
-  // (the same for the whole wave, and in scalar registers: pointers made from them stay there)
-  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int q0 = uniform(clamped(a.cu_q[lo], a.rows_q)), q1 = uniform(clamped(a.cu_q[lo + 1], a.rows_q));
   const int k0 = uniform(clamped(a.cu_k[lo], a.rows_k)), k1 = uniform(clamped(a.cu_k[lo + 1], a.rows_k));
   t.q0 = q0; t.n_q = q1 - q0;
