@@ -322,9 +322,9 @@ void prompt_of(const PromptArgs& a, hipStream_t st) {
 // parts' results are written and read in 32 bits (777 queries x 32 heads x 128 in two parts: 34 us, in one 21).
 int prompt_splits(int dtype, int B, int rows_q, int rows_k, int H, int d_k) {
   const bool f32 = dtype == DT_F32;
-  const int rows = f32 ? PROMPT_F32_ROWS : PQ;
+  const int rows = f32 ? prompt_f32_rows(d_k) : PQ;
   const double tiles = (double)B * ((rows_q / B + rows - 1) / rows) * H, keys = (double)rows_k / B / PK;      // (as if the sequences were equally long)
-  const double alone = f32 ? 1.7 * d_k / 64 : 1.2 * (d_k < 64 ? 64 : d_k) / 128, shared = f32 ? 2 * alone : 1.6 * alone;
+  const double alone = f32 ? 3.4 * d_k / 64 : 1.2 * (d_k < 64 ? 64 : d_k) / 128, shared = f32 ? 2 * alone : 1.6 * alone;
   int best = 1;
   double least = 1e30;
   for (int n = 1; n <= 32; ++n) {

@@ -51,42 +51,37 @@ template <bool F32, int BITS>
 __global__ __launch_bounds__(256) void quant_append_kernel(QuantArgs a) {
   __shared__ long at[TILE_T];                  // row of all caches, -1: nowhere
   __shared__ unsigned char sc[TILE_C / 32][TILE_T];
-  const int tid = threadIdx.x, r0 = blockIdx.x * TILE_T, c0 = blockIdx.y * TILE_C;
+  const int tid = threadIdx.x, cols = (a.d + TILE_C - 1) / TILE_C, r0 = blockIdx.x / cols * TILE_T, c0 = blockIdx.x % cols * TILE_C;
+  const int c = c0 + (tid & 31) * 8, rr = tid >> 5;
+  const bool in = c < a.d;
+  // (all loads without a branch, so that they are on their way together: rows and columns past the end are the last ones again, and not stored)
+  const int cc = in ? c : 0;
+  u32x4 v[8][F32 ? 2 : 1];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const long r = min(r0 + rr + 8 * i, a.n_rows - 1);
+    const u32x4* src = F32 ? (const u32x4*)((const float*)a.rows + r * a.pitch + cc) : (const u32x4*)((const uint16_t*)a.rows + r * a.pitch + cc);
+#pragma unroll
+    for (int k = 0; k < (F32 ? 2 : 1); ++k) v[i][k] = src[k];
+  }
   if (tid < TILE_T) {
     int b; long t;
     place_of(a, r0 + tid, b, t);
     at[tid] = b < 0 || t < 0 ? -1 : b * a.stride + t;
-  }
-  const int c = c0 + (tid & 31) * 8, rr = tid >> 5;
-  const bool in = c < a.d;
-  float x[8][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + rr + 8 * i;
-    if (in && r < a.n_rows) {
-      if constexpr (F32) {
-        const f32x4* src = (const f32x4*)((const float*)a.rows + (long)r * a.pitch + c);
-        const f32x4 lo = src[0], hi = src[1];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { x[i][j] = lo[j]; x[i][4 + j] = hi[j]; }
-      } else {
-        const u32x4 v = *(const u32x4*)((const uint16_t*)a.rows + (long)r * a.pitch + c);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { x[i][2 * j] = __uint_as_float(v[j] << 16); x[i][2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u); }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
-    }
   }
   __syncthreads();
   constexpr int EMAX = BITS == 4 ? 2 : 8;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     // The largest magnitude as bits: of floats without a sign the order is that of the integers, and what is not finite is above all others.
+    float x[8];
     unsigned m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[i][j]) & 0x7fffffffu);
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (F32) x[j] = __uint_as_float(v[i][j >> 2][j & 3]);
+      else x[j] = __uint_as_float(j & 1 ? v[i][0][j >> 1] & 0xffff0000u : v[i][0][j >> 1] << 16);
+      m = max(m, __float_as_uint(x[j]) & 0x7fffffffu);
+    }
     m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, true));
     m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xf, 0xf, true));
     // Its exponent, one more over a significand of 1.75: 6 and 448 are that much of their binade, so that an element is cut off by a seventh of itself at the
@@ -98,21 +93,21 @@ __global__ __launch_bounds__(256) void quant_append_kernel(QuantArgs a) {
     if (in && to >= 0) {
       if constexpr (BITS == 4) {
         unsigned w = 0;
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][0], x[i][1], scale, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][2], x[i][3], scale, 1);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][4], x[i][5], scale, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][6], x[i][7], scale, 3);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
         *(unsigned*)(a.codes + to * (a.d / 2) + c / 2) = s == 255u ? 0u : w;
       } else {
         // (Only magnitudes above 1.75 x 2^127 are over 448 of the largest scale; the conversion would make NaN of them.)
         const float top = 448.f * pow2_of(254 - EMAX);
         s16x2 w0 = {0, 0}, w1 = {0, 0};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[i][j] = fminf(fmaxf(x[i][j], -top), top);
-        w0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w0, x[i][0], x[i][1], scale, false);
-        w0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w0, x[i][2], x[i][3], scale, true);
-        w1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w1, x[i][4], x[i][5], scale, false);
-        w1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w1, x[i][6], x[i][7], scale, true);
+        for (int j = 0; j < 8; ++j) x[j] = fminf(fmaxf(x[j], -top), top);
+        w0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w0, x[0], x[1], scale, false);
+        w0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w0, x[2], x[3], scale, true);
+        w1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w1, x[4], x[5], scale, false);
+        w1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w1, x[6], x[7], scale, true);
         const u32x2 w = {__builtin_bit_cast(unsigned, w0), __builtin_bit_cast(unsigned, w1)};
         *(u32x2*)(a.codes + to * a.d + c) = s == 255u ? u32x2{0u, 0u} : w;
       }
@@ -135,7 +130,7 @@ template <bool F32, int BITS>
 __global__ __launch_bounds__(256) void quant_read_kernel(QuantArgs a) {
   __shared__ long at[TILE_T];                  // row of all caches, -1: a row of zeros, -2: no row
   __shared__ unsigned char sc[TILE_C / 32][TILE_T];
-  const int tid = threadIdx.x, r0 = blockIdx.x * TILE_T, c0 = blockIdx.y * TILE_C;
+  const int tid = threadIdx.x, cols = (a.d + TILE_C - 1) / TILE_C, r0 = blockIdx.x / cols * TILE_T, c0 = blockIdx.x % cols * TILE_C;
   if (tid < TILE_T) {
     int b; long t;
     place_of(a, r0 + tid, b, t);
@@ -147,12 +142,9 @@ __global__ __launch_bounds__(256) void quant_read_kernel(QuantArgs a) {
   u32x2 w[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const long from = at[rr + 8 * i];
-    w[i] = u32x2{0u, 0u};
-    if (in && from >= 0) {
-      if constexpr (BITS == 4) w[i][0] = *(const unsigned*)(a.codes + from * (a.d / 2) + c / 2);
-      else w[i] = *(const u32x2*)(a.codes + from * a.d + c);
-    }
+    const long from = max(at[rr + 8 * i], 0l);   // (without a branch: a row of zeros or none reads the first row's codes, for nothing)
+    if constexpr (BITS == 4) w[i][0] = *(const unsigned*)(a.codes + from * (a.d / 2) + (in ? c : 0) / 2);
+    else w[i] = *(const u32x2*)(a.codes + from * a.d + (in ? c : 0));
   }
 #pragma unroll
   for (int k = 0; k < TILE_C / 32 / 4; ++k) {
@@ -172,6 +164,7 @@ __global__ __launch_bounds__(256) void quant_read_kernel(QuantArgs a) {
     if (!in || at[row] == -2) continue;
     const float scale = pow2_of(sc[(tid & 31) >> 2][row]);
     const long o = (long)(r0 + row) * a.pitch + c;
+    if (at[row] == -1) w[i] = u32x2{0u, 0u};
     if constexpr (F32) {
       f32x2 v[4];
       if constexpr (BITS == 4) {
@@ -206,10 +199,13 @@ __global__ __launch_bounds__(256) void quant_read_kernel(QuantArgs a) {
   }
 }
 
+// Neighbouring workgroups have neighbouring columns: with neighbouring rows instead, 18560 rows of 4096 columns were read in pieces 8 KB apart at any one time.
+unsigned tiles_of(const QuantArgs& a) { return (unsigned)((a.n_rows + TILE_T - 1) / TILE_T) * (unsigned)((a.d + TILE_C - 1) / TILE_C); }
+
 }  // namespace
 
 void launch_quant_append(int dtype, int bits, const QuantArgs& a, hipStream_t st) {
-  const dim3 grid((a.n_rows + TILE_T - 1) / TILE_T, (a.d + TILE_C - 1) / TILE_C);
+  const unsigned grid = tiles_of(a);
   if (dtype == DT_F32) {
     if (bits == 4) quant_append_kernel<true, 4><<<grid, 256, 0, st>>>(a);
     else quant_append_kernel<true, 8><<<grid, 256, 0, st>>>(a);
@@ -220,7 +216,7 @@ void launch_quant_append(int dtype, int bits, const QuantArgs& a, hipStream_t st
 }
 
 void launch_quant_read(int dtype, int bits, const QuantArgs& a, hipStream_t st) {
-  const dim3 grid((a.n_rows + TILE_T - 1) / TILE_T, (a.d + TILE_C - 1) / TILE_C);
+  const unsigned grid = tiles_of(a);
   if (dtype == DT_F32) {
     if (bits == 4) quant_read_kernel<true, 4><<<grid, 256, 0, st>>>(a);
     else quant_read_kernel<true, 8><<<grid, 256, 0, st>>>(a);

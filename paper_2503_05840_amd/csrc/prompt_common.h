@@ -84,6 +84,6 @@ __device__ __forceinline__ float sum_of_halves(float v) {
 }
 
 void launch_prompt_f32(const PromptArgs& a, hipStream_t st);
-constexpr int PROMPT_F32_ROWS = 64;          // queries of a workgroup
+int prompt_f32_rows(int d_k);
 
 }  // namespace slim

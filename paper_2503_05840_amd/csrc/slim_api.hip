@@ -958,7 +958,7 @@ extern "C" int slim_tree_commit(void* Kcache, const int32_t* path, const int32_t
 namespace {
 
 // Bounds that keep grids, LDS tables and 32-bit offsets inside their ranges
-constexpr int QUANT_MAX_BATCH = 32768, QUANT_MAX_WIDTH = 1 << 20, QUANT_MAX_HEADS = 1024, QUANT_MAX_HEAD_WIDTH = 512, QUANT_MAX_CONTEXT = 1 << 24;
+constexpr int QUANT_MAX_BATCH = 32768, QUANT_MAX_WIDTH = 1 << 20, QUANT_MAX_HEADS = 1024, QUANT_MAX_HEAD_WIDTH = 512, QUANT_MAX_CONTEXT = 1 << 24, QUANT_MAX_PACKED = 1 << 24;
 
 // What the calls on such a cache check alike: its format, rows and width.
 int check_quant(int B, int T, int d, int bits, const slim_opts* o, int* dtype, long* t_stride) {
@@ -981,7 +981,7 @@ int quant_rows(bool write, const void* src, const int32_t* cu_rows, void* codes,
   int dtype; long t_stride;
   if (int rc = check_quant(B, T, d, bits, o, &dtype, &t_stride)) return rc;
   if (pitch == 0) pitch = d;
-  if (n_rows < 0 || pitch < d || pitch % vec_elems(dtype) != 0) return SLIM_ERR_SHAPE;
+  if (n_rows < 0 || n_rows > QUANT_MAX_PACKED || pitch > (1ll << 40) || pitch < d || pitch % vec_elems(dtype) != 0) return SLIM_ERR_SHAPE;
   if (!cu_rows && n_rows % B != 0) return SLIM_ERR_SHAPE;
   if (misaligned(src) || misaligned(dst) || misaligned(codes) || misaligned(scales) || misaligned4(cu_rows)) return SLIM_ERR_ALIGN;
   if (o && o->seq_lens_host)
