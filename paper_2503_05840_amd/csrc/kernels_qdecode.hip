@@ -77,7 +77,7 @@ __device__ __forceinline__ float sum_over_lanes(float v) {
 template <bool F32, int BITS, int P, bool ROPE>
 __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
   __shared__ f32x4 table[ROPE && P <= 16 ? QUANT_ROWS * P * 2 : 1];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   {
     const long wgs = (long)gridDim.x * gridDim.y * gridDim.z, wg = blockIdx.x + (long)gridDim.x * (blockIdx.y + (long)gridDim.y * blockIdx.z);
     for (long i = wg * 256 + tid; i < a.ncounters; i += wgs * 256) a.counters[i] = 0;
@@ -101,7 +101,12 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) { qb[j] = v[j]; qr[j] = ((v[j] >> 16) ^ 0x8000u) | v[j] << 16; qf[2 * j] = __uint_as_float(v[j] << 16); qf[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u); }
   }
-  const unsigned char* codes = a.codes + ((long)b * a.stride + t0) * (a.d * BITS / 8) + col * BITS / 8;
+  if (!on) {                                      // (a lane past its head's columns counts nothing: a row that is not finite is that for its whole sequence)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { qb[j] = qr[j] = 0u; qf[2 * j] = qf[2 * j + 1] = 0.f; }
+  }
+  const unsigned char* codes = a.codes + ((long)b * a.stride + t0) * (a.d * BITS / 8);
+  const unsigned at_col = (unsigned)(col * BITS / 8);
   const u32x4* sp = (const u32x4*)(a.scales + ((long)b * (a.d / 32) + col / 32) * a.stride + t0);
   u32x4 sc[4];
 #pragma unroll
@@ -111,7 +116,7 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
   Codes8<BITS> w[2][P];
   auto fetch = [&](int j, auto buf) {
 #pragma unroll
-    for (int r = 0; r < P; ++r) w[buf.value][r].load(codes + (long)(r * RP + j) * row_bytes);
+    for (int r = 0; r < P; ++r) w[buf.value][r].load(codes + (long)(r * RP + j) * row_bytes + at_col);
   };
   auto step = [&](int j, auto J) {
     constexpr int cur = decltype(J)::value & 1;
@@ -167,20 +172,21 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
         pair(std::integral_constant<int, 0>{}); pair(std::integral_constant<int, 1>{});
         pair(std::integral_constant<int, 2>{}); pair(std::integral_constant<int, 3>{});
       }
-      v[r] = on ? x : 0.f;
+      v[r] = x;
     }
     s[decltype(J)::value] = sums_to_lanes<P>(v, lane);
   };
-  fetch(0, std::integral_constant<int, 0>{});
+  if ((int)(blockIdx.y * 4 + wave) * HW < a.H) fetch(0, std::integral_constant<int, 0>{});
   if constexpr (ROPE && P <= 16) {
     // The 64 rows' cos and sin, which 16 and more heads share: to LDS once (32 KB for 128 columns).  Asked for from memory by every head they took as long as the codes.
     const int per = a.d_k / 4;
     for (int x = tid; x < QUANT_ROWS * P * 2; x += 256) {
       const int row = x / (P * 2), k = x % (P * 2);
-      if (k < per) table[x] = *(const f32x4*)(a.rope + (long)min(t0 + row, len - 1) * a.d_k + k * 4);
+      table[x] = k < per ? *(const f32x4*)(a.rope + (long)min(t0 + row, len - 1) * a.d_k + k * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
     __syncthreads();
   }
+  if ((int)(blockIdx.y * 4 + wave) * HW >= a.H) return;  // (no head for this wave)
   auto both = [&](int j, auto J) {
     if constexpr (decltype(J)::value + 1 < RP) fetch(decltype(J)::value + 1, std::integral_constant<int, (decltype(J)::value + 1) & 1>{});
     step(j, J);
@@ -528,32 +534,13 @@ __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
   }
   split_weights(a, b0, h, wt);
   __syncthreads();
-  // Merge: four columns a lane, a wave takes whole sequences, or with fewer than four a part of the splits each.  All loads of a sequence are on their way at once.
+  // Merge: four columns a lane.  A wave takes four sequences, or with one or two of them a quarter or half of the splits; sixteen loads are on their way at once.
   {
     const int seqs = min(QP_BATCH, a.B - b0), padded = F32 ? rows : (rows + 31) / 32 * 32, r = lane * 4;
-    const int G = seqs >= 3 ? 1 : seqs == 2 ? 2 : 4;
-    f32x4* parts = &join[0][0][0];
-    for (int j = wave / G; j < QP_BATCH; j += 4 / G) {
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
-      const int b = b0 + j, used = __float_as_int(wt[j][QP_MAX_SPLITS]);
-      if (r < rows) {
-        const float* src = a.C + ((long)b * a.nsplit * a.H + h) * a.d + cr0 + r;
-#pragma unroll 8
-        for (int s = wave % G; s < used; s += G) {
-          const f32x4 x = *(const f32x4*)(src + (long)s * a.H * a.d);
-          const float f = wt[j][s];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = fmaf(f, x[k], v[k]);
-        }
-      }
-      if (G > 1 && j == wave / G) {                // (the first turn has all sequences that there are)
-        parts[wave * 64 + lane] = v;
-        __syncthreads();
-        if (wave % G == 0)
-          for (int g = 1; g < G; ++g) v += parts[(wave + g) * 64 + lane];
-        __syncthreads();
-      }
-      if (wave % G != 0 || r >= padded) continue;
+    const float* src = a.C + (long)h * a.d + cr0 + min(r, rows - 4);
+    const long step = (long)a.H * a.d;
+    auto store = [&](int j, f32x4 v) {
+      if (r >= padded) return;
       if constexpr (F32) {
         *(f32x4*)(operand + (j * QP_MAX_ROWS + r) * 4) = v;
       } else {
@@ -564,6 +551,60 @@ __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
         *(bf16x4*)(operand + (j * (QP_MAX_ROWS + 8) + r) * 2) = hi;
         *(bf16x4*)(operand + ((QP_BATCH + j) * (QP_MAX_ROWS + 8) + r) * 2) = lo;
       }
+    };
+    // (behind the last split: the last again, with a weight of zero)
+    if (seqs > 2) {
+      int used[4], most = 0;
+      f32x4 v[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        used[y] = __builtin_amdgcn_readfirstlane(__float_as_int(wt[wave * 4 + y][QP_MAX_SPLITS]));
+        most = max(most, used[y]);
+        v[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      for (int s0 = 0; s0 < most; s0 += 4) {
+        f32x4 x[4][4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[y][i] = *(const f32x4*)(src + ((long)min(b0 + wave * 4 + y, a.B - 1) * a.nsplit + max(min(s0 + i, used[y] - 1), 0)) * step);
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (s0 + i < used[y]) {
+              const float f = wt[wave * 4 + y][s0 + i];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[y][k] = fmaf(f, x[y][i][k], v[y][k]);
+            }
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) store(wave * 4 + y, v[y]);
+    } else {
+      f32x4* parts = &join[0][0][0];
+      const int G = seqs == 2 ? 2 : 4, j = wave / G;
+      const int used = __builtin_amdgcn_readfirstlane(__float_as_int(wt[j][QP_MAX_SPLITS]));
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int s0 = wave % G; s0 < used; s0 += 16 * G) {
+        f32x4 x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = *(const f32x4*)(src + ((long)(b0 + j) * a.nsplit + min(s0 + i * G, used - 1)) * step);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (s0 + i * G < used) {
+            const float f = wt[j][s0 + i * G];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = fmaf(f, x[i][k], v[k]);
+          }
+      }
+      parts[wave * 64 + lane] = v;
+      __syncthreads();
+      if (wave % G == 0) {
+        for (int g = 1; g < G; ++g) v += parts[(wave + g) * 64 + lane];
+        store(j, v);
+      }
+      for (int z = 4 / G + wave; z < QP_BATCH; z += 4) store(z, f32x4{0.f, 0.f, 0.f, 0.f});       // (rows of the operand without a sequence)
     }
   }
   __syncthreads();
@@ -627,7 +668,7 @@ __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
     if (mine_there) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) mine[j] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
       for (int s = 0; s < a.csw; ++s) {
         const unsigned long long* p = (const unsigned long long*)(a.part + (long)s * a.B * a.d + o);
 #pragma unroll
@@ -674,7 +715,7 @@ int qdecode_counters(int B, int H, int d) { return H * ((d / H + QP_COLS - 1) / 
 
 // How the work is cut.  Splits of the weighted sum: a workgroup for every compute unit (with two, one sequence of 16384 rows x 4096 took 18.6 us instead of 15.9, as
 // much more to write and merge), but of 1024 rows at the most where that does not make more than four a unit: sequences of a batch are not equally long (16 of up
-// to 5000 rows x 2304 in 8 bits: two splits 38.6 us, four 28.6).  128 rows at least: a step of 32 for every wave.  Row splits of W: two workgroups a unit.
+// to 5000 rows x 2304 in 8 bits: two splits 38.6 us, four 28.6).  128 rows at least: a step of 32 for every wave.  Row splits of W: a workgroup a unit, 256 rows at the most.
 // (The splits themselves go up and down with T; `most_splits` only grows.)
 void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* most_splits, int* csw, int* crows) {
   const int nb = (T + QUANT_ROWS - 1) / QUANT_ROWS;
@@ -690,7 +731,7 @@ void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, i
   const int d_k = d / H, ct = (d_k + QP_COLS - 1) / QP_COLS;
   const long tiles = (long)H * ct * ((B + QP_BATCH - 1) / QP_BATCH);
   const int least = (d + QP_MAX_ROWS - 1) / QP_MAX_ROWS, most = d / 32;
-  long c = (512 + tiles - 1) / tiles;
+  long c = (256 + tiles - 1) / tiles;
   if (c < least) c = least;
   if (c > most) c = most;
   *crows = (int)(((d + c - 1) / c + 31) / 32 * 32);
