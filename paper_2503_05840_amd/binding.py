@@ -486,12 +486,33 @@ def _rows_ptr(t, rows, width, dtype, what):
     return t.data_ptr(), (t.stride(0) if rows > 1 else width)
 
 
+@functools.lru_cache(maxsize=None)
+def _current_device(torch):
+    """A function that returns the current device's number (as _current_stream: the raw one where this torch has it)."""
+    return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _one_device(*tensors):
     """Kernels run on the current device, on its current stream."""
     import torch
-    on = {t.device.index for t in tensors if t is not None and t.is_cuda}
-    if on and on != {torch.cuda.current_device()}:
-        raise ValueError("tensors must be on the current device")
+    here = None
+    for t in tensors:
+        if t is None or t.get_device() < 0:               # (host tensors are refused where their address is taken)
+            continue
+        if here is None:
+            here = _current_device(torch)()
+        if t.get_device() != here:
+            raise ValueError("tensors must be on the current device")
+
+
+def _call_opts(dtype, seq_lens, seq_lens_host, t_stride, workspace, stage_ms, rope_table):
+    """_opts for calls without variants and layouts, made in one piece (half the time); rope_table is checked, workspace contiguous."""
+    import torch
+    keep = None if seq_lens_host is None else np.ascontiguousarray(seq_lens_host, dtype=np.int32)
+    return SlimOpts(DTYPES[dtype], None if seq_lens is None else seq_lens.data_ptr(), None if keep is None else keep.ctypes.data, int(t_stride or 0),
+                    None if workspace is None else _dev_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                    _current_stream(torch)(), VARIANT_AUTO, None if stage_ms is None else ctypes.cast(stage_ms, ctypes.POINTER(ctypes.c_float)),
+                    None if rope_table is None else _dev_ptr(rope_table), 0, K_ROWMAJOR), keep
 
 
 def _offsets_ptr(cu, B, what):
@@ -520,7 +541,7 @@ def slim_quant_append(rows, codes, scales, B, T, d, bits, cu_rows=None, dtype="b
     n = rows.shape[0]
     at, pitch = _rows_ptr(rows, n, d, dtype, "rows")
     ptrs = (at, _offsets_ptr(cu_rows, B, "cu_rows"), *_quant_ptrs(codes, scales, B, T, d, bits, t_stride))
-    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, None, VARIANT_AUTO, stage_ms)
+    o, keep = _call_opts(dtype, seq_lens, seq_lens_host, t_stride, None, stage_ms, None)
     rc = load().slim_quant_append(*ptrs, B, n, T, d, bits, pitch, ctypes.byref(o))
     if rc != SLIM_OK:
         raise SlimError(rc, "slim_quant_append")
@@ -534,7 +555,7 @@ def slim_quant_read(codes, scales, rows, B, T, d, bits, cu_rows=None, dtype="bf1
     n = rows.shape[0]
     at, pitch = _rows_ptr(rows, n, d, dtype, "rows")
     ptrs = (*_quant_ptrs(codes, scales, B, T, d, bits, t_stride), _offsets_ptr(cu_rows, B, "cu_rows"), at)
-    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, None, VARIANT_AUTO, stage_ms)
+    o, keep = _call_opts(dtype, seq_lens, seq_lens_host, t_stride, None, stage_ms, None)
     rc = load().slim_quant_read(*ptrs, B, n, T, d, bits, pitch, ctypes.byref(o))
     if rc != SLIM_OK:
         raise SlimError(rc, "slim_quant_read")
@@ -550,10 +571,8 @@ def slim_quant_decode(q, codes, scales, W_KV, out, B, H, T, d, bits, dtype="bf16
     _one_device(q, codes, scales, W_KV, out, seq_lens, workspace, rope_table)
     if rope_table is not None and (rope_table.dtype != torch.float32 or rope_table.numel() < T * (d // H)):
         raise ValueError("rope_table must be float32 and hold T positions")
-    if workspace is not None:
-        _dev_ptr(workspace)
     ptrs = (_tree_ptr(q, (B, d), el), *_quant_ptrs(codes, scales, B, T, d, bits, t_stride), _tree_ptr(W_KV, (d, d), el), _tree_ptr(out, (B, d), el))
-    o, keep = _opts(dtype, seq_lens, seq_lens_host, t_stride, workspace, VARIANT_AUTO, stage_ms, rope_table)
+    o, keep = _call_opts(dtype, seq_lens, seq_lens_host, t_stride, workspace, stage_ms, rope_table)
     rc = load().slim_quant_decode(*ptrs, B, H, T, d, bits, ctypes.byref(o))
     if rc != SLIM_OK:
         raise SlimError(rc, "slim_quant_decode")
@@ -566,12 +585,10 @@ def slim_prompt_attention(q, k, v, cu_q, out, B, H, H_kv, d_k, cu_k=None, causal
     _one_device(q, k, v, out, cu_q, cu_k, workspace)
     (qp, q_pitch), (kp, k_pitch), (vp, v_pitch) = (_rows_ptr(t, r, w * d_k, dtype, n)
                                                    for t, r, w, n in ((q, rows_q, H, "q"), (k, rows_k, H_kv, "k"), (v, rows_k, H_kv, "v")))
-    if workspace is not None:
-        _dev_ptr(workspace)
     if cu_q is None:
         raise ValueError("cu_q: the offsets of the sequences are needed")
     ptrs = (qp, kp, vp, _offsets_ptr(cu_q, B, "cu_q"), _offsets_ptr(cu_k, B, "cu_k"), _tree_ptr(out, (rows_q, H * d_k), _element(dtype)))
-    o, keep = _opts(dtype, None, None, 0, workspace, VARIANT_AUTO, stage_ms)
+    o, keep = _call_opts(dtype, None, None, 0, workspace, stage_ms, None)
     rc = load().slim_prompt_attention(*ptrs, B, rows_q, rows_k, H, H_kv, d_k, int(causal), q_pitch, k_pitch, v_pitch, ctypes.byref(o))
     if rc != SLIM_OK:
         raise SlimError(rc, "slim_prompt_attention")

@@ -983,6 +983,7 @@ int quant_rows(bool write, const void* src, const int32_t* cu_rows, void* codes,
   if (pitch == 0) pitch = d;
   if (n_rows < 0 || n_rows > QUANT_MAX_PACKED || pitch > (1ll << 40) || pitch < d || pitch % vec_elems(dtype) != 0) return SLIM_ERR_SHAPE;
   if (!cu_rows && n_rows % B != 0) return SLIM_ERR_SHAPE;
+  if (((long)n_rows + 63) / 64 * ((d + 255) / 256) >= 1 << 24) return SLIM_ERR_SHAPE;     // (workgroups of 256 threads, 32 bits of those)
   if (misaligned(src) || misaligned(dst) || misaligned(codes) || misaligned(scales) || misaligned4(cu_rows)) return SLIM_ERR_ALIGN;
   if (o && o->seq_lens_host)
     for (int b = 0; b < B; ++b)
@@ -1025,9 +1026,10 @@ QDecodePlan qdecode_layout(QDecodeArgs& a, int dtype) {
   return p;
 }
 
-int check_qdecode(int H, int d) {
+int check_qdecode(int B, int H, int d, int dtype) {
   if (H < 1 || H > QUANT_MAX_HEADS || d % H != 0 || d / H % 8 != 0 || d / H > QUANT_MAX_HEAD_WIDTH) return SLIM_ERR_SHAPE;
-  return SLIM_OK;
+  const int heads = dtype == SLIM_F32 ? 8 : 32;       // of a workgroup of the weighted sum; sequences and their groups of heads are a grid's last dimension
+  return (long)B * ((H + heads - 1) / heads) > 65535 ? SLIM_ERR_SHAPE : SLIM_OK;
 }
 
 }  // namespace
@@ -1046,7 +1048,7 @@ extern "C" size_t slim_workspace_bytes_quant(int B, int H, int T, int d, int bit
   slim_opts o{};
   o.dtype = dtype;
   long ts;
-  if (check_quant(B, T, d, bits, &o, &dtype, &ts) || check_qdecode(H, d)) return 0;
+  if (check_quant(B, T, d, bits, &o, &dtype, &ts) || check_qdecode(B, H, d, dtype)) return 0;
   QDecodeArgs a{};
   a.B = B; a.H = H; a.T = T; a.d = d; a.d_k = d / H; a.bits = bits;
   return qdecode_layout(a, dtype).total;
@@ -1057,7 +1059,7 @@ extern "C" int slim_quant_decode(const void* q, const void* codes, const void* s
   if (!q || !codes || !scales || !W_KV || !out) return SLIM_ERR_ARG;
   int dtype; long t_stride;
   if (int rc = check_quant(B, T, d, bits, o, &dtype, &t_stride)) return rc;
-  if (int rc = check_qdecode(H, d)) return rc;
+  if (int rc = check_qdecode(B, H, d, dtype)) return rc;
   if (misaligned(q) || misaligned(codes) || misaligned(scales) || misaligned(W_KV) || misaligned(out)) return SLIM_ERR_ALIGN;
   const float* rope = o ? o->rope_table : nullptr;
   if (rope && misaligned(rope)) return SLIM_ERR_ALIGN;
@@ -1100,7 +1102,7 @@ int check_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dt
   if (H < 1 || H > PROMPT_MAX_HEADS || H_kv < 1 || H % H_kv != 0 || d_k < 1 || d_k > PROMPT_MAX_WIDTH) return SLIM_ERR_SHAPE;
   if (dtype != SLIM_F32 && dtype != SLIM_BF16) return SLIM_ERR_DTYPE;
   if (d_k % vec_elems(dtype) != 0) return SLIM_ERR_SHAPE;
-  return SLIM_OK;
+  return (long)H * (rows_q / 64 + B + 8) >= 1 << 24 ? SLIM_ERR_SHAPE : SLIM_OK;           // (workgroups of 256 threads, 32 bits of those)
 }
 
 size_t prompt_bytes(int nsplit, int rows_q, int H, int d_k) {

@@ -96,6 +96,21 @@ def test_columns_of_one_buffer():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_past_32_bit_offsets(dtype):
+    """Columns of a buffer of 2^20 columns a row: rows from 2048 on are past 2^31 elements."""
+    import torch
+    n, e = 2200, 2 * 64
+    c = PromptCase([n], [n], 2, 2, 64, dtype, seed=9)
+    want = c.run()
+    wide = torch.zeros((n, 1 << 20), dtype=c.dev["q"].dtype, device="cuda")
+    for i, name in enumerate(("q", "k", "v")):
+        at = slice((1 << 20) - (i + 1) * e, (1 << 20) - i * e)
+        wide[:, at] = c.dev[name]
+        c.dev[name] = wide[:, at]
+    assert np.array_equal(c.call().float().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_offsets_that_are_out_of_range_stay_inside(dtype):
     """Offsets are device data: whatever they are, only rows that there are get read and written."""
     import torch

@@ -124,6 +124,22 @@ def test_rows_past_32_bit_offsets(bits):
     assert int(codes.ne(0).any(-1).sum()) == B
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+def test_decode_past_32_bit_offsets(bits):
+    import torch
+    H, d, T, B, n = 8, 512, 1 << 20, 17, 130                     # 4.6 or 9.1 GB of codes; the last sequence's are past 2^32 bytes
+    codes, scales = binding.slim_quant_cache(B, T, d, bits)
+    small = QuantCase(1, H, d // H, n, bits, seed=12)
+    small.device()
+    codes[B - 1, :small.rows], scales[B - 1, :, :small.rows] = small.dev["codes"][0], small.dev["scales"][0]
+    lens = ints([0] * (B - 1) + [n])
+    out = torch.full((B, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    q = small.dev["q"].expand(B, d).contiguous()
+    binding.slim_quant_decode(q, codes, scales, small.dev["W"], out, B, H, T, d, bits, seq_lens=lens)
+    small.check(got=out[B - 1:].float().cpu().numpy().astype(np.float64))
+    assert (out[:B - 1] == 0).all()
+
+
 DECODE = [  # B, H, d_k, T, lens
     (1, 1, 32, 1, None), (1, 4, 64, 63, None), (2, 4, 64, 65, [1, 65]), (3, 20, 64, 300, [0, 300, 129]), (1, 12, 72, 200, None), (2, 4, 128, 520, [64, 511]),
     (1, 40, 32, 100, None), (2, 24, 96, 130, [130, 33]), (17, 2, 48, 90, list(range(1, 18))), (1, 3, 160, 70, None), (1, 2, 272, 140, None), (1, 32, 128, 97, None)]

@@ -71,7 +71,9 @@ def test_formats_and_rows_of_a_cache(call):
 def test_packed_rows(call):
     plain = dict(p1=None) if call is _append else dict(p2=None)
     assert call(_swap(4, **plain), n=7) == SHAPE               # 7 rows are not as many for each of two sequences
-    assert call(n=-2) == SHAPE
+    for n in (-2, (1 << 24) + 2):
+        assert call(n=n) == SHAPE
+    assert call(n=1 << 24, d=1 << 18, pitch=1 << 18) == SHAPE    # more workgroups than a launch has
     assert call(pitch=-512) == ARG
     for pitch in (511, 504, 516):
         assert call(pitch=pitch) == SHAPE
@@ -81,6 +83,7 @@ def test_packed_rows(call):
 def test_decode_heads_and_workspace():
     for kw in (dict(H=0), dict(H=7), dict(H=128), dict(H=2048, d=1 << 14), dict(H=1, d=544)):
         assert _decode(**kw) == SHAPE, kw
+    assert _decode(B=32768, H=64, d=2048, o=_opts(t_stride=64)) == SHAPE                     # more groups of heads than a grid has places
     assert _decode(o=_opts(rope_table=4104)) == ALIGN
     need = binding.slim_workspace_bytes_quant(2, 8, 64, 512, 4, "bf16")
     assert need > 0
@@ -102,11 +105,11 @@ def test_decode_workspace_grows_with_the_context(dtype):
 
 def test_prompt_shapes_options_and_workspace():
     for kw in (dict(B=0), dict(B=1 << 16), dict(rows_q=-1), dict(rows_k=-1), dict(H=0), dict(H_kv=0), dict(H=6, H_kv=4), dict(d_k=0), dict(d_k=60), dict(d_k=264),
-               dict(rows_q=(1 << 24) + 1), dict(H=8192, H_kv=1)):
+               dict(rows_q=(1 << 24) + 1), dict(H=8192, H_kv=1), dict(H=4096, H_kv=1, rows_q=1 << 20, rows_k=1 << 20)):
         assert _prompt(**kw) == SHAPE, kw
     assert _prompt(_swap(6, p4=None), rows_q=40, rows_k=41) == SHAPE
     assert _prompt(pitches=(-512, 0, 0)) == ARG
-    for pitches in ((504, 0, 0), (516, 0, 0), (0, 120, 0), (0, 0, 120), (0, 132, 0)):
+    for pitches in (((1 << 24) + 8, 0, 0), (504, 0, 0), (516, 0, 0), (0, 120, 0), (0, 0, 120), (0, 132, 0)):
         assert _prompt(pitches=pitches) == SHAPE, pitches
     assert _prompt(o=_opts(dtype=2)) == DTYPE
     assert _prompt(d_k=36) == SHAPE                              # 16-byte vectors of bf16
