@@ -30,7 +30,8 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
   const int i = min(t.i0 + wave * 32 + n, t.n_q - 1);          // this lane's query (past the last: the last, not stored)
   const int off = t.n_k - t.n_q;
   const int sees = a.causal ? i + off : t.n_k - 1;               // its last key
-  const int wave_last = a.causal ? min(t.i0 + wave * 32 + 31, t.n_q - 1) + off : t.n_k - 1;
+  const int wave_last = t.i0 + wave * 32 >= t.n_q ? -1                  // (no query: the wave only takes part in the loads)
+                        : a.causal ? min(t.i0 + wave * 32 + 31, t.n_q - 1) + off : t.n_k - 1;
   const int end = a.causal ? min(t.i0 + PQ, t.n_q) + off : t.n_k;     // keys that the workgroup needs
   const int all = end > 0 ? (end + PK - 1) / PK : 0, per = __builtin_amdgcn_readfirstlane((all + a.nsplit - 1) / a.nsplit);
   const int tile0 = t.split * per, tile1 = min(tile0 + per, all);
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     const int buf = (tile - tile0) & 1;
     tiles_barrier<0>();
     if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
-    if (!decltype(masked)::value || tile * PK <= wave_last) attend(tile * PK, buf, masked);
+    if (tile * PK <= wave_last) attend(tile * PK, buf, masked);
 #pragma unroll
     for (int k = 0; k < NS; ++k) ka[k] ^= PAIR;
 #pragma unroll

@@ -32,7 +32,8 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(Pro
     i[y] = min(i0 + y * 16 + n, t.n_q - 1);
     sees[y] = a.causal ? i[y] + off : t.n_k - 1;
   }
-  const int wave_last = a.causal ? min(i0 + 16 * QT - 1, t.n_q - 1) + off : t.n_k - 1;
+  const int wave_last = i0 >= t.n_q ? -1                                // (no query: the wave only takes part in the loads)
+                        : a.causal ? min(i0 + 16 * QT - 1, t.n_q - 1) + off : t.n_k - 1;
   const int end = a.causal ? min(t.i0 + PQ, t.n_q) + off : t.n_k;     // keys that the workgroup needs
   const int all = end > 0 ? (end + PK - 1) / PK : 0, per = __builtin_amdgcn_readfirstlane((all + a.nsplit - 1) / a.nsplit);
   const int tile0 = t.split * per, tile1 = min(tile0 + per, all);
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(Pro
     const int buf = (tile - tile0) & 1;
     tiles_barrier<0>();
     if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
-    if (!decltype(masked)::value || tile * PK <= wave_last) attend(tile * PK, buf, masked);
+    if (tile * PK <= wave_last) attend(tile * PK, buf, masked);
 #pragma unroll
     for (int k = 0; k < NS; ++k) ka[k] ^= PAIR;
     va ^= PAIR;
