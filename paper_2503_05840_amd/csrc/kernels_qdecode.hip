@@ -237,30 +237,43 @@ __device__ __forceinline__ bool split_blocks(const QDecodeArgs& a, int len, int 
 }
 
 // References of up to 32 heads for a split: the largest of its blocks, to LDS; the first column block notes them and the sums for the merge.
-// Eight threads a head.
-__device__ __forceinline__ void split_references(const QDecodeArgs& a, int b, int split, int blk0, int blk1, int h0, int nh, bool note, float* mref) {
-  const int tid = threadIdx.x, j = tid >> 3, k = tid & 7, h = h0 + j;
-  float m = NEG_INF, l = 0.f;
-  if (j < nh && h < a.H) {
+// Eight threads a head.  The first two blocks of a thread are asked for before the rows (loads come back in order).
+struct SplitReferences {
+  float ref[2], sum[2];
+  __device__ __forceinline__ void ask(const QDecodeArgs& a, int b, int blk0, int blk1, int h0, int nh) {
+    const int j = threadIdx.x >> 3, k = threadIdx.x & 7, h = min(h0 + j, a.H - 1);
     const long at = ((long)b * a.H + h) * a.NB;
-    for (int blk = blk0 + k; blk < blk1; blk += 8) m = fmaxf(m, a.ref[at + blk]);
-  }
-  m = max_over_lanes<8>(m);
-  if (j < nh && h < a.H && note) {
-    const long at = ((long)b * a.H + h) * a.NB;
-    for (int blk = blk0 + k; blk < blk1; blk += 8) l += a.sum[at + blk] * exp2f(a.ref[at + blk] - m);
-  }
-  l = sum_over_lanes<8>(l);
-  if (k == 0 && j < nh) {
-    mref[j] = m;
-    if (note && h < a.H) {
-      const long at = ((long)b * a.nsplit + split) * a.H + h;
-      a.sref[at] = m;
-      a.ssum[at] = l;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int blk = min(blk0 + k + 8 * i, blk1 - 1);
+      ref[i] = a.ref[at + blk];
+      sum[i] = a.sum[at + blk];
     }
   }
-  __syncthreads();
-}
+  __device__ __forceinline__ void finish(const QDecodeArgs& a, int b, int split, int blk0, int blk1, int h0, int nh, bool note, float* mref) const {
+    const int j = threadIdx.x >> 3, k = threadIdx.x & 7, h = min(h0 + j, a.H - 1);
+    const long at = ((long)b * a.H + h) * a.NB;
+    float m = fmaxf(ref[0], ref[1]), l = 0.f;          // (a block twice does not change the largest)
+    for (int blk = blk0 + k + 16; blk < blk1; blk += 8) m = fmaxf(m, a.ref[at + blk]);
+    m = max_over_lanes<8>(m);
+    if (note) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (blk0 + k + 8 * i < blk1) l += sum[i] * exp2f(ref[i] - m);
+      for (int blk = blk0 + k + 16; blk < blk1; blk += 8) l += a.sum[at + blk] * exp2f(a.ref[at + blk] - m);
+      l = sum_over_lanes<8>(l);
+    }
+    if (k == 0 && j < nh) {
+      mref[j] = m;
+      if (note && h0 + j < a.H) {
+        const long o = ((long)b * a.nsplit + split) * a.H + h0 + j;
+        a.sref[o] = m;
+        a.ssum[o] = l;
+      }
+    }
+    lds_barrier();
+  }
+};
 
 template <int BITS> struct Codes16;              // 16 columns of a row
 template <> struct Codes16<4> { typedef u32x2 type; };
@@ -280,7 +293,7 @@ template <int BITS, int NT>
 __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
   typedef typename Codes16<BITS>::type W16;
   __shared__ float mref[32];
-  __shared__ f32x4 join[4][NT * 4][64];
+  __shared__ f32x4 join[4][3][4][64];            // [from][to: waves after it][operand]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ngroups = (a.H + 16 * NT - 1) / (16 * NT);
   const int b = blockIdx.z / ngroups, h0 = blockIdx.z % ngroups * 16 * NT, split = blockIdx.y;
@@ -369,9 +382,11 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
   };
   // One loop with the next rows in a second set of registers, copied: with the two sets in turn the accumulators were copied instead, and went to scratch.
   int k = blk0 * 2 + wave;
+  SplitReferences refs;
+  refs.ask(a, b, blk0, blk1, h0, 16 * NT);
   Rows x;
-  if (k < step1) fetch(k, x);                      // (on its way while the references are looked up)
-  split_references(a, b, split, blk0, blk1, h0, 16 * NT, blockIdx.x == 0, mref);
+  if (k < step1) fetch(k, x);
+  refs.finish(a, b, split, blk0, blk1, h0, 16 * NT, blockIdx.x == 0, mref);
 #pragma unroll
   for (int t = 0; t < NT; ++t) m[t] = mref[min(h0 + t * 16 + n, a.H - 1) - h0];
   if (k < step1) {
@@ -387,26 +402,27 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
       x = next;
     }
   }
-  // Quarter by quarter: three waves hand theirs over, the fourth adds them in the order of the waves and stores the sum.  (Constant indices: with the wave's own
-  // quarter picked at run time the accumulators went to scratch, 27 us for a step that takes 8.)
+  // Wave w ends with operands 4 w .. 4 w + 3 of every tile: for each tile the waves hand the others their quarters and add what they get in the order
+  // of the waves from their own on.  (Constant indices: with the wave's own quarter picked at run time the accumulators went to scratch, 27 us for a launch
+  // that takes 8.  One quarter after the other, three waves looking on, took 3.6 us.)
 #pragma unroll
-  for (int qd = 0; qd < 4; ++qd) {
-    if (wave != qd) {
+  for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+    for (int qd = 0; qd < 4; ++qd)
+      if (wave != qd) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) join[wave][t * 4 + j][lane] = acc[t][qd * 4 + j];
-    }
-    __syncthreads();
-    if (wave == qd) {
+        for (int j = 0; j < 4; ++j) join[wave][(qd - wave - 1) & 3][j][lane] = acc[t][qd * 4 + j];
+      }
+    lds_barrier();
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
+    for (int qd = 0; qd < 4; ++qd)
+      if (wave == qd) {
         f32x4 v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           v[j] = acc[t][qd * 4 + j];
 #pragma unroll
-          for (int w = 1; w < 4; ++w) v[j] += join[(qd + w) & 3][t * 4 + j][lane];
+          for (int w = 1; w < 4; ++w) v[j] += join[(qd + w) & 3][3 - w][j][lane];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -415,8 +431,7 @@ __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
             *(f32x4*)(a.C + (((long)b * a.nsplit + split) * a.H + h) * a.d + c + qd * 4) = f32x4{v[0][i], v[1][i], v[2][i], v[3][i]};
         }
       }
-    }
-    __syncthreads();
+    if (t + 1 < NT) lds_barrier();
   }
 }
 
@@ -431,7 +446,9 @@ __global__ __launch_bounds__(256) void qweighted_f32_kernel(QDecodeArgs a) {
   const int len = seq_len_of(a.seq_lens, b, a.T);
   int blk0, blk1;
   if (!split_blocks(a, len, split, blk0, blk1)) return;
-  split_references(a, b, split, blk0, blk1, h0, 8, blockIdx.x == 0, mref);
+  SplitReferences refs;
+  refs.ask(a, b, blk0, blk1, h0, 8);
+  refs.finish(a, b, split, blk0, blk1, h0, 8, blockIdx.x == 0, mref);
   const int c = blockIdx.x * 512 + lane * 8, cc = min(c, a.d - 8);
   const long row_bytes = a.d * BITS / 8;
   const unsigned char* codes = a.codes + (long)b * a.stride * row_bytes + (long)cc * BITS / 8;
