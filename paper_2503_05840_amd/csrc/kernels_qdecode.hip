@@ -226,6 +226,151 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
   }
 }
 
+// The same for heads of 32 CH columns (32, 64, 96, 128): four lanes a head, 8 CH columns each, none idle.  A wave has eight heads x 16 rows, in two halves of the
+// lanes eight rows each; four waves a block of 64 rows, which meet in LDS for its reference; eight waves sixteen heads, which share the table.
+// (With 16 lanes a head, rotated keys of 96 columns kept a quarter of the lanes idle where the vector ALU is what bounds.)
+template <bool F32, int BITS, int CH, bool ROPE>
+__global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
+  constexpr int P = 4, RP = 2, DK = 32 * CH;
+  __shared__ f32x4 table[ROPE ? QUANT_ROWS * DK / 4 : 1];
+  __shared__ float most[2][4][8], total[2][4][8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  {
+    const long wgs = (long)gridDim.x * gridDim.y * gridDim.z, wg = blockIdx.x + (long)gridDim.x * (blockIdx.y + (long)gridDim.y * blockIdx.z);
+    for (long i = wg * 512 + tid; i < a.ncounters; i += wgs * 512) a.counters[i] = 0;
+  }
+  const int b = blockIdx.z, t0 = blockIdx.x * QUANT_ROWS;
+  const int len = seq_len_of(a.seq_lens, b, a.T);
+  if (t0 >= len) return;
+  const int set = wave >> 2, part = wave & 3;      // eight heads, sixteen rows
+  const int i = lane & 3, slot = (lane >> 2) & 7, half = lane >> 5;
+  const int h = blockIdx.y * 16 + set * 8 + slot, hc = min(h, a.H - 1);      // (heads past the last: the last again, not stored)
+  const int col = hc * DK + i * 8 * CH, first = part * 16 + half * 8;         // this lane's columns and first row of the block
+  const long row_bytes = (long)a.d * BITS / 8;
+  const unsigned char* codes = a.codes + ((long)b * a.stride + t0 + part * 16) * row_bytes;
+  const unsigned at = (unsigned)(half * 8 * (int)row_bytes + col * BITS / 8);
+  Codes8<BITS> w[P * RP][CH];
+#pragma unroll
+  for (int r = 0; r < P * RP; ++r)
+#pragma unroll
+    for (int k = 0; k < CH; ++k) w[r][k].load(codes + (long)r * row_bytes + at + k * BITS);
+  constexpr int NSC = CH == 3 ? 3 : 1;             // groups that the chunks of eight columns lie in (24 columns: two, which of them is the lane's)
+  u32x2 sc[NSC];
+#pragma unroll
+  for (int k = 0; k < NSC; ++k) sc[k] = *(const u32x2*)(a.scales + ((long)b * (a.d / 32) + (col + 8 * k) / 32) * a.stride + t0 + first);
+  float qf[F32 ? 8 * CH : 1];
+  unsigned qb[4 * CH], qr[4 * CH];
+  if constexpr (F32) {
+    const f32x4* src = (const f32x4*)((const float*)a.q + (long)b * a.d + col);
+#pragma unroll
+    for (int j = 0; j < 2 * CH; ++j) {
+      const f32x4 v = src[j];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) qf[4 * j + k] = v[k];
+    }
+  } else {
+    const u32x4* src = (const u32x4*)((const uint16_t*)a.q + (long)b * a.d + col);
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const u32x4 v = src[j];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { qb[4 * j + k] = v[k]; qr[4 * j + k] = ((v[k] >> 16) ^ 0x8000u) | v[k] << 16; }
+    }
+  }
+  if constexpr (ROPE) {
+    // (rows behind the sequence, whose score is masked, have no position in the table)
+    for (int x = tid; x < QUANT_ROWS * DK / 4; x += 512) {
+      const int row = x / (DK / 4), k = x % (DK / 4);
+      table[x] = *(const f32x4*)(a.rope + (long)min(t0 + row, len - 1) * DK + k * 4);
+    }
+    __syncthreads();
+  }
+  if ((int)blockIdx.y * 16 + set * 8 >= a.H) return;  // (eight heads that there are not: the barriers below are of the waves that stay)
+  float s[RP];
+#pragma unroll
+  for (int j = 0; j < RP; ++j) {
+    float v[P];
+#pragma unroll
+    for (int r = 0; r < P; ++r) {
+      const int row = r * RP + j;                  // lane i ends with rows 2 i and 2 i + 1
+      float x = 0.f;
+      auto chunk = [&](int, auto C) {
+        constexpr int ch = decltype(C)::value;
+        const float f = scale_of(sc[NSC == 1 ? 0 : ch][row >> 2], row & 3);
+        const Codes8<BITS>& c = w[row][ch];
+        f32x4 t[2];
+        if constexpr (ROPE) {
+          const f32x4* cs = table + (first + row) * (DK / 4) + (i * CH + ch) * 2;
+          t[0] = cs[0]; t[1] = cs[1];
+        }
+        auto pair = [&](int, auto K) {
+          constexpr int k = decltype(K)::value, kk = 4 * ch + k;
+          if constexpr (ROPE) {
+            const float co = t[k >> 1][2 * (k & 1)], si = t[k >> 1][2 * (k & 1) + 1];
+            float u, y;                            // q . y and q . (y turned by a quarter): the score is u cos + w sin
+            if constexpr (F32) {
+              const f32x2 z = c.template f32<k>(f);
+              u = fmaf(qf[2 * kk], z[0], qf[2 * kk + 1] * z[1]);
+              y = fmaf(qf[2 * kk], z[1], -(qf[2 * kk + 1] * z[0]));
+            } else {
+              const bf16x2 z = __builtin_bit_cast(bf16x2, c.template bf16<k>(f));
+              u = __builtin_amdgcn_fdot2_f32_bf16(z, __builtin_bit_cast(bf16x2, qb[kk]), 0.f, false);
+              y = __builtin_amdgcn_fdot2_f32_bf16(z, __builtin_bit_cast(bf16x2, qr[kk]), 0.f, false);
+            }
+            x = fmaf(co, u, x);
+            x = fmaf(si, y, x);
+          } else if constexpr (F32) {
+            const f32x2 z = c.template f32<k>(f);
+            x = fmaf(qf[2 * kk], z[0], x);
+            x = fmaf(qf[2 * kk + 1], z[1], x);
+          } else {
+            x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, c.template bf16<k>(f)), __builtin_bit_cast(bf16x2, qb[kk]), x, false);
+          }
+        };
+        full_steps<0, 4>(0, pair);
+      };
+      full_steps<0, CH>(0, chunk);
+      v[r] = x;
+    }
+    s[j] = sums_to_lanes<P>(v, lane);
+  }
+  // numerators, against the block's reference
+  float m = NEG_INF;
+#pragma unroll
+  for (int j = 0; j < RP; ++j) {
+    s[j] = t0 + first + i * RP + j < len ? s[j] * a.qscale : NEG_INF;
+    m = fmaxf(m, s[j]);
+  }
+  m = max_over_lanes<P>(m);
+  m = fmaxf(m, __shfl_xor(m, 32));
+  if (i == 0 && half == 0) most[set][part][slot] = m;
+  lds_barrier();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m = fmaxf(m, most[set][k][slot]);
+  const float ref = m == NEG_INF ? 0.f : ceilf(m);
+  float l = 0.f, p[RP];
+#pragma unroll
+  for (int j = 0; j < RP; ++j) {
+    p[j] = exp2f(s[j] - ref);
+    if constexpr (!F32) p[j] = (float)(__bf16)p[j];       // rounded where it enters the product with K, and the sum is of what enters
+    l += p[j];
+  }
+  l = sum_over_lanes<P>(l);
+  l += __shfl_xor(l, 32);
+  if (i == 0 && half == 0) total[set][part][slot] = l;
+  const long o = ((long)b * a.H + hc) * a.Tp + t0 + first + i * RP;
+  if (h < a.H) {
+    if constexpr (F32) *(f32x2*)((float*)a.P + o) = f32x2{p[0], p[1]};
+    else *(bf16x2*)((uint16_t*)a.P + o) = bf16x2{(__bf16)p[0], (__bf16)p[1]};
+  }
+  lds_barrier();
+  if (part == 0 && i == 0 && half == 0 && h < a.H) {
+    const long x = ((long)b * a.H + h) * a.NB + blockIdx.x;
+    a.ref[x] = ref;
+    a.sum[x] = (total[set][0][slot] + total[set][1][slot]) + (total[set][2][slot] + total[set][3][slot]);
+  }
+}
+
 // ---- weighted sum of K ----------------------------------------------------------------------------------
 
 // A split's blocks of one sequence: [blk0, blk1), none where the sequence is shorter
@@ -717,9 +862,19 @@ void scores_of(const QDecodeArgs& a, hipStream_t st) {
   if (a.rope) qscores_kernel<F32, BITS, P, true><<<grid, 256, 0, st>>>(a);
   else qscores_kernel<F32, BITS, P, false><<<grid, 256, 0, st>>>(a);
 }
+template <bool F32, int BITS, int CH>
+void even_scores(const QDecodeArgs& a, hipStream_t st) {
+  const dim3 grid(a.NB, (a.H + 15) / 16, a.B);
+  if (a.rope) qscores_even_kernel<F32, BITS, CH, true><<<grid, 512, 0, st>>>(a);
+  else qscores_even_kernel<F32, BITS, CH, false><<<grid, 512, 0, st>>>(a);
+}
 template <bool F32, int BITS>
 void scores_by_width(const QDecodeArgs& a, hipStream_t st) {
-  if (a.d_k <= 32) scores_of<F32, BITS, 4>(a, st);
+  if (a.d_k == 32) even_scores<F32, BITS, 1>(a, st);
+  else if (a.d_k == 64) even_scores<F32, BITS, 2>(a, st);
+  else if (a.d_k == 96) even_scores<F32, BITS, 3>(a, st);
+  else if (a.d_k == 128) even_scores<F32, BITS, 4>(a, st);
+  else if (a.d_k <= 32) scores_of<F32, BITS, 4>(a, st);
   else if (a.d_k <= 64) scores_of<F32, BITS, 8>(a, st);
   else if (a.d_k <= 128) scores_of<F32, BITS, 16>(a, st);
   else if (a.d_k <= 256) scores_of<F32, BITS, 32>(a, st);
