@@ -39,21 +39,40 @@ struct PromptTile {
 __device__ __forceinline__ int clamped(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
 
 // Workgroup -> head, tile of `rows` queries, split of the keys.  Sequence b's tiles have places from cu_q[b] / rows + b on: never more tiles than places up to the
-// next one's, so that no workgroup needs a sum over the batch; places behind a sequence's last tile are empty.  Workgroups are dealt to the 8 XCDs round
-// robin: each XCD gets a run of consecutive heads, whose keys and values then stay in its L2.  The longest rows of a causal sequence come first.
+// next one's, so that no workgroup needs a sum over the batch; places behind a sequence's last tile are empty.
+// Workgroups are dealt to the 8 XCDs round robin, each with an L2 of its own: an XCD has whole key heads (8 places of `full` of them at a time) and its share of the
+// `rem` heads that are left, whose places go to the XCDs in turn.  Of all these the last places come first: the tiles of a causal sequence that see the
+// most keys, so that what is left at the end is short (6000 queries x 32 heads x 128, heads one after the other: 381 us).
+struct PromptPlaces {
+  int places, full, rem, block;                   // block: key heads' places of an XCD in eight places
+  __host__ __device__ PromptPlaces(const PromptArgs& a, int rows) {
+    places = a.rows_q / rows + a.B;
+    full = a.H_kv / 8;
+    rem = a.H_kv % 8;
+    block = 8 * full + rem;
+  }
+};
 __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int rows, PromptTile& t) {
-  const int places = a.rows_q / rows + a.B, units = a.H * places * a.nsplit;
-  const int per = (units + 7) / 8, unit = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
-  if (((int)blockIdx.x >> 3) >= per || unit >= units) return false;
-  // heads that share keys are next to each other: their workgroups read the same tiles at about the same time
+  const PromptPlaces pp(a, rows);
   // (All of it is the same for the whole wave, and is told so: pointers made from it stay in scalar registers.)
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-  const int G = uniform(a.H / a.H_kv), u = uniform(unit / G), r = unit - u * G;
-  const int w = uniform(u / a.nsplit);
+  const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3;
+  const int G = uniform(a.H / a.H_kv), u = uniform(slot / G), w = uniform(u / a.nsplit);
   t.split = u - w * a.nsplit;
-  t.hk = uniform(w / places);
-  t.h = t.hk * G + r;
-  const int place = places - 1 - (w - t.hk * places);
+  const int blk = uniform(w / pp.block), x = w - blk * pp.block;
+  int place;
+  if (x < 8 * pp.full) {
+    const int p = uniform(x / pp.full);
+    place = blk * 8 + p;
+    t.hk = xcd * pp.full + x - p * pp.full;
+  } else {
+    const int v = (x - 8 * pp.full) * 8 + xcd, p = uniform(v / pp.rem);
+    place = blk * 8 + p;
+    t.hk = 8 * pp.full + v - p * pp.rem;
+  }
+  if (place >= pp.places) return false;
+  place = pp.places - 1 - place;
+  t.h = t.hk * G + slot - u * G;
   int lo = 0, hi = a.B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -68,7 +87,8 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs& a, int rows, Promp
   return j >= 0 && t.i0 < t.n_q;
 }
 inline unsigned prompt_grid(const PromptArgs& a, int rows) {
-  return 8u * (unsigned)(((long)a.H * (a.rows_q / rows + a.B) * a.nsplit + 7) / 8);
+  const PromptPlaces pp(a, rows);
+  return 8u * (unsigned)((pp.places + 7) / 8) * (unsigned)pp.block * (unsigned)(a.H / a.H_kv * a.nsplit);
 }
 
 // max / sum over the lanes l and l ^ 32
