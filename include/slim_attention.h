@@ -50,7 +50,8 @@ extern "C" {
 #define SLIM_ERR_TIMEOUT   -10   /* slim_status: a wait between workgroups ran out, or workgroups could
                                     not meet where they were expected to (outputs NaN)            */
 #define SLIM_ERR_LAYOUT    -11   /* opts->k_layout: rows per sequence not a multiple of 32, or a shape or
-                                    dtype whose kernels read row-major caches only              */
+                                    dtype whose kernels read row-major caches only; a cache in 4 or 8
+                                    bits: rows per sequence not a multiple of 64                 */
 
 /* ---- element types of the cache and of packed weights -------------------------------- */
 #define SLIM_F32   0

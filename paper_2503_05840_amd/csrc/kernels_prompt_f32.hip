@@ -17,7 +17,7 @@ __device__ __forceinline__ float max_of_groups(float v) {
 // As in bf16, on 16x16x4 products: S^T = K Q^T has a query in the four lanes l % 16, four consecutive keys in the registers of each; register i of all four
 // is the operand of a product over the keys 4 g + i (g the lane's group), V's rows are read to fit.  Operands of the first product come four at a time: lane
 // group g holds columns 4 g .. 4 g + 3 of 16, a product takes one of the four from each.  QT tiles of queries a wave share what is read of K and V.
-// Bound by the matrix cores' fp32 rate.
+// Bound by the matrix cores' fp32 rate: 4 x 1500 queries x 20 heads x 64, full, 387 us, 119 TFLOP/s of 154.
 template <int DKP, bool WHOLE, int QT>
 __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(PromptArgs a) {
   constexpr int PC = Pitch<DKP>::pieces, NS = DKP / 16, NV = (DKP + 63) / 64, PQ = 64 * QT;

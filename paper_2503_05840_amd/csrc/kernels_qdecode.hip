@@ -1,5 +1,7 @@
 // The decode step of slim attention over a K-cache in 4 or 8 bits (its format: kernels_quant.hip): scores, weighted sum of K, merge + projection through W_KV.
 // Three launches; none of their workgroups waits for another.  What a code stands for is exact in bf16, so that K enters both products without a rounding.
+// The codes are read twice: the numerators of all heads weigh every column, and the H x d sums of one pass would fill the registers of a compute unit each, whose partial
+// results (512 KB a unit at 32 heads x 4096) are more bytes than the second pass.  1 x 16384 rows x 32 x 128 in 4 bits: 9 + 15 + 13.5 us.
 #include "device_common.h"
 #include "slim_kernels.h"
 
@@ -73,7 +75,8 @@ __device__ __forceinline__ float sum_over_lanes(float v) {
 // A wave takes 64 rows x 64 / P heads; a head is P lanes of eight columns (those past d_k are idle).  Rows go P at a time, lane i of a head ends with the
 // 64 / P consecutive rows from i * 64 / P on, and the scale bytes of all 64 rows are one run of a lane's group.  From the scores come softmax numerators relative
 // to a power of two per head and block: a whole exponent, so that a later change of reference is exact in every type.
-// HBM-bound (0.53 or 1.03 bytes an element); about 20 instructions a row and lane, 35 with rotated keys.
+// HBM-bound (0.53 or 1.03 bytes an element); about 20 instructions a row and lane, 37 with rotated keys, where the vector ALU bounds.  For heads of other widths than
+// the next kernel's.
 template <bool F32, int BITS, int P, bool ROPE>
 __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
   __shared__ f32x4 table[ROPE && P <= 16 ? QUANT_ROWS * P * 2 : 1];
@@ -228,7 +231,8 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
 
 // The same for heads of 32 CH columns (32, 64, 96, 128): four lanes a head, 8 CH columns each, none idle.  A wave has eight heads x 16 rows, in two halves of the
 // lanes eight rows each; four waves a block of 64 rows, which meet in LDS for its reference; eight waves sixteen heads, which share the table.
-// (With 16 lanes a head, rotated keys of 96 columns kept a quarter of the lanes idle where the vector ALU is what bounds.)
+// With 16 lanes a head, heads of 96 columns kept a quarter of the lanes idle: 16 sequences of 600..5000 rows x 24 heads in 8 bits, rotary 35 us and now 31, without 22.7
+// and now 19.9 (5.5 TB/s of codes).  1 x 16384 x 32 x 128 in 4 bits 9 us.
 template <bool F32, int BITS, int CH, bool ROPE>
 __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
   constexpr int P = 4, RP = 2, DK = 32 * CH;
@@ -433,7 +437,8 @@ constexpr int QW_COLS = 256;                     // columns of a workgroup: 16 l
 
 // C[h][c] = sum_t p[h][t] K[t][c] on 16x16x32 matrix instructions: rows are heads, the contraction is over 32 cache rows, a lane holds eight rows x 16 columns and
 // makes one column of operands after the other.  The four waves take every fourth 32 rows of the split and join through LDS in a fixed order.
-// Bound by HBM for the codes where a sequence is long.
+// Bound by HBM for the codes where a sequence is long: 1 x 16384 rows x 32 x 128 in 4 bits 15 us, 7 of them the stream (5.1 TB/s), the rest the start (2.5), the waves'
+// join and partial sums; 16 sequences of 600..5000 rows x 24 x 96 in 8 bits 28.6 us.
 template <int BITS, int NT>
 __global__ __launch_bounds__(256, 2) void qweighted_kernel(QDecodeArgs a) {
   typedef typename Codes16<BITS>::type W16;
@@ -670,7 +675,8 @@ __device__ __forceinline__ void split_weights(const QDecodeArgs& a, int b0, int 
 
 // out[b][h d_k + j] = sum_c C[b][h][c] W[c][h d_k + j].  A workgroup takes a head, up to 128 of its columns, 16 sequences and a row split of W: it merges the
 // splits' partial sums into LDS (as bf16 hi + lo, which keeps 16 bits of them; W is bf16), multiplies on 16x16x32 matrix instructions, and whoever of a
-// head's row splits comes last adds their results in the order of their numbers.  HBM-bound on W for small batches.
+// head's row splits comes last adds their results in the order of their numbers.  HBM-bound on W for small batches: 1 x 4096 x 4096 12 us, 6.4 of them W at 5.2 TB/s, 2 the
+// start, 3 the meeting of the row splits.  (Sixteen columns and all rows a workgroup, which needs no meeting, took 16: pieces of 32 bytes.)
 template <bool F32>
 __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
   __shared__ float wt[QP_BATCH][QP_MAX_SPLITS + 1];

@@ -42,7 +42,7 @@ __device__ __forceinline__ int clamped(int v, int hi) { return v < 0 ? 0 : (v > 
 // next one's, so that no workgroup needs a sum over the batch; places behind a sequence's last tile are empty.
 // Workgroups are dealt to the 8 XCDs round robin, each with an L2 of its own: an XCD has whole key heads (8 places of `full` of them at a time) and its share of the
 // `rem` heads that are left, whose places go to the XCDs in turn.  Of all these the last places come first: the tiles of a causal sequence that see the
-// most keys, so that what is left at the end is short (6000 queries x 32 heads x 128, heads one after the other: 381 us).
+// most keys, so that what is left at the end is short (6000 queries x 32 heads x 128, heads one after the other 381 us, this way 352).
 struct PromptPlaces {
   int places, full, rem, block;                   // block: key heads' places of an XCD in eight places
   __host__ __device__ PromptPlaces(const PromptArgs& a, int rows) {

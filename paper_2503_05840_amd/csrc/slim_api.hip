@@ -297,7 +297,7 @@ extern "C" const char* slim_strerror(int code) {
     case SLIM_ERR_ILLCOND: return "W_K ill-conditioned (rcond < 1e-12); W_KV written but unreliable";
     case SLIM_ERR_LAUNCH: return "HIP allocation or launch error";
     case SLIM_ERR_SEQLEN: return "sequence length outside [1, T]";
-    case SLIM_ERR_LAYOUT: return "banded K-cache: rows per sequence not a multiple of 32, or no kernel reads that layout for this shape / dtype / call";
+    case SLIM_ERR_LAYOUT: return "banded K-cache: rows per sequence not a multiple of 32, or no kernel reads that layout for this shape / dtype / call; cache in 4 or 8 bits: rows per sequence not a multiple of 64";
     case SLIM_ERR_TIMEOUT: return "a wait between workgroups ran out in the latest fast-path call on this workspace, or they did not run where they were to meet; its outputs are NaN";
     default: return "unknown slim status";
   }

@@ -20,6 +20,31 @@ def test_against_fp64(n_q, n_k, H, H_kv, d_k, dtype, causal):
     PromptCase(n_q, n_k, H, H_kv, d_k, dtype, causal, seed=sum(n_k) + d_k, tail=3).check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,H_kv", [(9, 9), (20, 20), (7, 1), (24, 12), (26, 13)])
+def test_heads_that_do_not_share_out_evenly(dtype, H, H_kv):
+    """Every head and tile is somebody's, whatever is left over the eight XCDs."""
+    PromptCase([260, 70, 5], [260, 70, 5], H, H_kv, 32, dtype, seed=H).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_no_keys_at_all_and_rows_before_the_first_sequence(dtype, causal):
+    import torch
+    c = PromptCase([3], [0], 2, 2, 64, dtype, causal)
+    assert (c.run() == 0).all()
+    c = PromptCase([40, 90], [40, 90], 2, 1, 64, dtype, causal, seed=1)
+    want = c.run()
+    cut = 7                                                      # the first sequence starts seven rows later
+    c.dev["cu_q"] = ints([cut, 40, 130])
+    got = c.call().float().cpu().numpy()
+    assert (got[:cut] == 77.0).all() and np.array_equal(got[40:], want[40:])
+    d = PromptCase([40 - cut], [40 - cut], 2, 1, 64, dtype, causal)
+    d.q, d.k, d.v = c.q[cut:40], c.k[cut:40], c.v[cut:40]
+    assert np.array_equal(got[cut:40], d.run())
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("d_k", [4, 36, 100, 180, 252])
 def test_widths_of_fp32_vectors(d_k):
     PromptCase([70, 5], [70, 5], 2, 1, d_k, "f32", seed=d_k).check()

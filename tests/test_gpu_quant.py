@@ -85,6 +85,26 @@ def test_rows_that_are_not_finite_or_do_not_fit(bits):
     assert torch.equal(held, codes) and (out == 0).all()
 
 
+def test_offsets_that_begin_later_or_are_out_of_range():
+    """Packed rows before the first offset belong to nobody; offsets are device data, and whatever they are, only rows that there are get read and written."""
+    import torch
+    rng = np.random.default_rng(8)
+    d, T = 96, 128
+    rows = up(rng.standard_normal((20, d)), "bf16")
+    codes, scales = binding.slim_quant_cache(2, T, d, 4)
+    binding.slim_quant_append(rows, codes, scales, 2, T, d, 4, cu_rows=ints([5, 12, 20]))
+    want, s = orc.quantise(rows.double().cpu().numpy(), 4)
+    c = codes.cpu().numpy()
+    assert (c[0, :7] == orc.pack(want, 4)[5:12]).all() and (c[1, :8] == orc.pack(want, 4)[12:]).all() and not c[0, 7:].any() and not c[1, 8:].any()
+    out = torch.full_like(rows, 77.0)
+    binding.slim_quant_read(codes, scales, out, 2, T, d, 4, cu_rows=ints([5, 12, 20]))
+    assert (out[:5] == 77.0).all() and np.array_equal(out[5:].double().cpu().numpy(), orc.values(want, s, 4)[5:])
+    for cu in ([0, 9, 5000], [-4, 9, 20], [15, 3, 20], [1 << 30, 0, -1]):
+        binding.slim_quant_append(rows, codes, scales, 2, T, d, 4, cu_rows=ints(cu))
+        binding.slim_quant_read(codes, scales, out, 2, T, d, 4, cu_rows=ints(cu))
+    torch.cuda.synchronize()
+
+
 def test_columns_of_a_wider_buffer_and_no_rows():
     import torch
     rng = np.random.default_rng(5)
