@@ -243,21 +243,31 @@ __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
     const long wgs = (long)gridDim.x * gridDim.y * gridDim.z, wg = blockIdx.x + (long)gridDim.x * (blockIdx.y + (long)gridDim.y * blockIdx.z);
     for (long i = wg * 512 + tid; i < a.ncounters; i += wgs * 512) a.counters[i] = 0;
   }
-  const int b = blockIdx.z, t0 = blockIdx.x * QUANT_ROWS;
+  // Blocks of the same rows follow each other over the heads and sequences: they take cos and sin from the L2s.  (Which comes first moves on by one from rows to rows:
+  // an XCD would get the same sequences and heads all along, and the others the short ones.)
+  const int groups = (a.H + 15) / 16, blk = blockIdx.z * gridDim.y + blockIdx.y;
+  const unsigned at_block = (blockIdx.x + (unsigned)blk) % gridDim.x;
+  const int b = at_block / groups, hg = at_block % groups;
   const int len = seq_len_of(a.seq_lens, b, a.T);
-  if (t0 >= len) return;
+  if (blk >= (len + QUANT_ROWS - 1) / QUANT_ROWS) return;
+  const int t0 = blk * QUANT_ROWS;
   const int set = wave >> 2, part = wave & 3;      // eight heads, sixteen rows
   const int i = lane & 3, slot = (lane >> 2) & 7, half = lane >> 5;
-  const int h = blockIdx.y * 16 + set * 8 + slot, hc = min(h, a.H - 1);      // (heads past the last: the last again, not stored)
+  const int h = hg * 16 + set * 8 + slot, hc = min(h, a.H - 1);      // (heads past the last: the last again, not stored)
   const int col = hc * DK + i * 8 * CH, first = part * 16 + half * 8;         // this lane's columns and first row of the block
   const long row_bytes = (long)a.d * BITS / 8;
   const unsigned char* codes = a.codes + ((long)b * a.stride + t0 + part * 16) * row_bytes;
   const unsigned at = (unsigned)(half * 8 * (int)row_bytes + col * BITS / 8);
-  Codes8<BITS> w[P * RP][CH];
+  constexpr int PER_THREAD = DK / 32;               // table entries: 64 DK / 4 over 512 threads
+  f32x4 turn[ROPE ? PER_THREAD : 1];
+  if constexpr (ROPE) {
+    // (rows behind the sequence, whose score is masked, have no position in the table)
 #pragma unroll
-  for (int r = 0; r < P * RP; ++r)
-#pragma unroll
-    for (int k = 0; k < CH; ++k) w[r][k].load(codes + (long)r * row_bytes + at + k * BITS);
+    for (int x = 0; x < PER_THREAD; ++x) {
+      const int at_entry = tid + x * 512, row = at_entry / (DK / 4), k = at_entry % (DK / 4);
+      turn[x] = *(const f32x4*)(a.rope + (long)min(t0 + row, len - 1) * DK + k * 4);
+    }
+  }
   constexpr int NSC = CH == 3 ? 3 : 1;             // groups that the chunks of eight columns lie in (24 columns: two, which of them is the lane's)
   u32x2 sc[NSC];
 #pragma unroll
@@ -281,15 +291,21 @@ __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
       for (int k = 0; k < 4; ++k) { qb[4 * j + k] = v[k]; qr[4 * j + k] = ((v[k] >> 16) ^ 0x8000u) | v[k] << 16; }
     }
   }
+  // (Loads come back in order: what all rows need first, then the rows as they are taken.)
+  Codes8<BITS> w[P * RP][CH];
+#pragma unroll
+  for (int j = 0; j < RP; ++j)
+#pragma unroll
+    for (int r = 0; r < P; ++r)
+#pragma unroll
+      for (int k = 0; k < CH; ++k) w[r * RP + j][k].load(codes + (long)(r * RP + j) * row_bytes + at + k * BITS);
+  __builtin_amdgcn_sched_barrier(0);
   if constexpr (ROPE) {
-    // (rows behind the sequence, whose score is masked, have no position in the table)
-    for (int x = tid; x < QUANT_ROWS * DK / 4; x += 512) {
-      const int row = x / (DK / 4), k = x % (DK / 4);
-      table[x] = *(const f32x4*)(a.rope + (long)min(t0 + row, len - 1) * DK + k * 4);
-    }
-    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < PER_THREAD; ++x) table[tid + x * 512] = turn[x];
+    lds_barrier();
   }
-  if ((int)blockIdx.y * 16 + set * 8 >= a.H) return;  // (eight heads that there are not: the barriers below are of the waves that stay)
+  if (hg * 16 + set * 8 >= a.H) return;  // (eight heads that there are not: the barriers below are of the waves that stay)
   float s[RP];
 #pragma unroll
   for (int j = 0; j < RP; ++j) {
@@ -369,7 +385,7 @@ __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
   }
   lds_barrier();
   if (part == 0 && i == 0 && half == 0 && h < a.H) {
-    const long x = ((long)b * a.H + h) * a.NB + blockIdx.x;
+    const long x = ((long)b * a.H + h) * a.NB + blk;
     a.ref[x] = ref;
     a.sum[x] = (total[set][0][slot] + total[set][1][slot]) + (total[set][2][slot] + total[set][3][slot]);
   }
@@ -870,7 +886,7 @@ void scores_of(const QDecodeArgs& a, hipStream_t st) {
 }
 template <bool F32, int BITS, int CH>
 void even_scores(const QDecodeArgs& a, hipStream_t st) {
-  const dim3 grid(a.NB, (a.H + 15) / 16, a.B);
+  const dim3 grid((a.H + 15) / 16 * a.B, a.NB < 32768 ? a.NB : 32768, (a.NB + 32767) / 32768);
   if (a.rope) qscores_even_kernel<F32, BITS, CH, true><<<grid, 512, 0, st>>>(a);
   else qscores_even_kernel<F32, BITS, CH, false><<<grid, 512, 0, st>>>(a);
 }
