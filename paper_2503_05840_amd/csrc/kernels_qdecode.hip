@@ -677,15 +677,27 @@ __device__ __forceinline__ void split_weights(const QDecodeArgs& a, int b0, int 
   const int j = threadIdx.x >> 4, k = threadIdx.x & 15, b = b0 + j;
   const int len = b < a.B ? seq_len_of(a.seq_lens, b, a.T) : 0;
   const int nb = (len + QUANT_ROWS - 1) / QUANT_ROWS, used = (nb + a.per - 1) / a.per;
-  float m = NEG_INF, l = 0.f;
-  for (int s = k; s < used; s += 16) m = fmaxf(m, a.sref[((long)b * a.nsplit + s) * a.H + h]);
-  m = max_over_lanes<16>(m);
-  for (int s = k; s < used; s += 16) {
-    const long at = ((long)b * a.nsplit + s) * a.H + h;
-    l += a.ssum[at] * exp2f(a.sref[at] - m);
+  const long at = (long)min(b, a.B - 1) * a.nsplit * a.H + h;
+  float ref[QP_MAX_SPLITS / 16], sum[QP_MAX_SPLITS / 16], m = NEG_INF, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < QP_MAX_SPLITS / 16; ++i) {       // (all on their way at once; splits that the sequence does not have hold anything)
+    const long s = at + (long)min(k + 16 * i, a.nsplit - 1) * a.H;
+    ref[i] = a.sref[s];
+    sum[i] = a.ssum[s];
   }
+#pragma unroll
+  for (int i = 0; i < QP_MAX_SPLITS / 16; ++i) {
+    if (k + 16 * i >= used) { ref[i] = NEG_INF; sum[i] = 0.f; }
+    m = fmaxf(m, ref[i]);
+  }
+  m = max_over_lanes<16>(m);
+#pragma unroll
+  for (int i = 0; i < QP_MAX_SPLITS / 16; ++i)
+    if (k + 16 * i < used) l += sum[i] * (ref[i] = exp2f(ref[i] - m));
   l = sum_over_lanes<16>(l);
-  for (int s = k; s < a.nsplit; s += 16) wt[j][s] = s < used ? exp2f(a.sref[((long)b * a.nsplit + s) * a.H + h] - m) / l : 0.f;
+#pragma unroll
+  for (int i = 0; i < QP_MAX_SPLITS / 16; ++i)
+    if (k + 16 * i < a.nsplit) wt[j][k + 16 * i] = k + 16 * i < used ? ref[i] / l : 0.f;
   if (k == 0) wt[j][QP_MAX_SPLITS] = __int_as_float(used);
 }
 
