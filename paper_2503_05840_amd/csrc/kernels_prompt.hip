@@ -9,7 +9,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int PQ = 128, PK = 64;               // queries of a workgroup (32 a wave), keys of a tile
+constexpr int PK = 64;                         // keys of a tile
 
 // 16-byte pieces of a row in LDS: a power of two, so that they can be swapped among themselves by the row's number.  Keys are read with lanes on consecutive
 // rows, 16 bytes each; values with four rows x 32 bytes for every 16 lanes.  Either way the rows of one access shall lie in different banks.
@@ -23,20 +23,23 @@ template <int PC> __device__ __forceinline__ int v_swap(int row) { return PC >= 
 // operand being read in the same order of keys (transposed reads of four rows).
 // Bound by the matrix cores and the vector ALU together: a tile of 128 columns is 1024 cycles of products and 990 of numerators (an exponential takes 16) a wave.
 // 16384 queries x 32 heads x 128, causal: 2.02 ms, 1.09 PFLOP/s, as a library product of 8192^3; heads of 96 and 64 columns have the same numerators for fewer products:
-// 0.70 to 0.88.  One wave a SIMD (777 queries x 32 heads): 1.2 us a tile; four buffers, the next tile's scores beside the numerators, operands read further ahead: no
-// gain in any combination.
-template <int DKP, bool WHOLE>
+// 0.70 to 0.88.
+// QW = 2: 64 queries a workgroup, for prompts that do not fill the chip: the waves are two pairs, each with half of every tile's keys, joined at the end.  A sequence's longest
+// workgroup then takes half as long (777 queries x 32 heads 23 -> 19 us).  With 128, four buffers, the next tile's scores beside the numerators, operands read further
+// ahead: no gain in any combination, a tile takes 1.1 us of the matrix cores' 0.9.
+template <int DKP, bool WHOLE, int QW>
 __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
-  constexpr int PC = Pitch<DKP>::pieces, NS = DKP / 16, NV = DKP / 32;
+  constexpr int PC = Pitch<DKP>::pieces, NS = DKP / 16, NV = DKP / 32, PQ = 32 * QW, KW = 4 / QW, NH = 2 / KW;   // NH: 32 keys of a tile, NH times
   __shared__ __align__(16) char tiles[2][2][PK * PC * 16];       // [buffer][keys, values]
   PromptTile t;
   if (!prompt_tile(a, PQ, t)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
-  const int i = min(t.i0 + wave * 32 + n, t.n_q - 1);          // this lane's query (past the last: the last, not stored)
+  const int qw = wave % QW, kw = wave / QW;                       // the wave's 32 queries, and which 32 NH keys of a tile are its own
+  const int i = min(t.i0 + qw * 32 + n, t.n_q - 1);          // this lane's query (past the last: the last, not stored)
   const int off = t.n_k - t.n_q;
   const int sees = a.causal ? i + off : t.n_k - 1;               // its last key
-  const int wave_last = t.i0 + wave * 32 >= t.n_q ? -1                  // (no query: the wave only takes part in the loads)
-                        : a.causal ? min(t.i0 + wave * 32 + 31, t.n_q - 1) + off : t.n_k - 1;
+  const int wave_last = t.i0 + qw * 32 >= t.n_q ? -1                  // (no query: the wave only takes part in the loads)
+                        : a.causal ? min(t.i0 + qw * 32 + 31, t.n_q - 1) + off : t.n_k - 1;
   const int end = a.causal ? min(t.i0 + PQ, t.n_q) + off : t.n_k;     // keys that the workgroup needs
   const int all = end > 0 ? (end + PK - 1) / PK : 0, per = __builtin_amdgcn_readfirstlane((all + a.nsplit - 1) / a.nsplit);
   const int tile0 = t.split * per, tile1 = min(tile0 + per, all);
@@ -110,21 +113,21 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
   // This lane's places in the buffer of the present tile: a key's pieces, and four rows of values (rows 8 and more further on are swapped alike)
   unsigned ka[NS], va[NV];
 #pragma unroll
-  for (int k = 0; k < NS; ++k) ka[k] = (unsigned)(n * PC + ((2 * k + half) ^ k_swap<PC>(n))) * 16;
+  for (int k = 0; k < NS; ++k) ka[k] = kw * (NH * 32 * PC * 16) + (unsigned)(n * PC + ((2 * k + half) ^ k_swap<PC>(n))) * 16;
   {
     const int row = 4 * half + ((lane & 15) >> 2), byte = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) va[v] = PAIR / 2 + (unsigned)(row * PC + ((v * 4 + (byte >> 4)) ^ v_swap<PC>(row))) * 16 + (byte & 15);
+    for (int v = 0; v < NV; ++v) va[v] = PAIR / 2 + kw * (NH * 32 * PC * 16) + (unsigned)(row * PC + ((v * 4 + (byte >> 4)) ^ v_swap<PC>(row))) * 16 + (byte & 15);
   }
-  // One tile.  MASKED: some queries of the wave do not see all of its keys.
+  // One tile, this wave's keys of it.  MASKED: some queries of the wave do not see all of its keys.
   const char* const lds = (const char*)tiles;
   auto attend = [&](int key0, int buf, auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
-    const char* const vt = lds + buf * PAIR + PAIR / 2;
-    f32x16 s[2];
+    const char* const vt = lds + buf * PAIR + PAIR / 2 + kw * (NH * 32 * PC * 16);
+    f32x16 s[NH];
     __builtin_amdgcn_s_setprio(1);                 // (the SIMD's other wave fills in: sequences of 8000 and 5000 keys x 24 heads x 96 75 -> 71 us)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
+    for (int x = 0; x < NH; ++x) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
 #pragma unroll
@@ -137,16 +140,17 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     unsigned long long bad = 0;                                  // rows of values that are not finite
     if constexpr (MASKED) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int x = 0; x < NH; ++x)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (key0 + x * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > sees) s[x][r] = NEG_INF;
-      // (a lane a row: zero times what is not finite is NaN, and stays)
+      // (a lane a row, or half a row: zero times what is not finite is NaN, and stays)
       float top = 0.f;
       const bf16x2 zero = {(__bf16)0.f, (__bf16)0.f};
+      const int row = NH == 2 ? lane : n, c0 = NH == 2 ? 0 : half * (PC / 2);
 #pragma unroll 4
-      for (int c = 0; c < PC; ++c) {
-        const u32x4 v = *(const u32x4*)(vt + (lane * PC + (c ^ (lane & (PC - 1)))) * 16);
+      for (int c = 0; c < PC * NH / 2; ++c) {
+        const u32x4 v = *(const u32x4*)(vt + (row * PC + c0 + (c ^ (row & (PC * NH / 2 - 1)))) * 16);
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const unsigned two = v[y];
@@ -154,10 +158,11 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
         }
       }
       bad = __ballot(top != 0.f);
+      if constexpr (NH == 1) bad = (bad | bad >> 32) & 0xffffffffull;
     }
     float m = NEG_INF;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < NH; ++x)
 #pragma unroll
       for (int r = 0; r < 16; ++r) m = fmaxf(m, s[x][r]);
     m = max_of_halves(m) * a.scale;
@@ -174,14 +179,14 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     }
     const float base = ref == NEG_INF ? 0.f : ref;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < NH; ++x)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -base));
         sum += s[x][r];
       }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2 * NH; ++k) {
       bf16x8 p;
 #pragma unroll
       for (int r = 0; r < 8; ++r) p[r] = (__bf16)s[k >> 1][(k & 1) * 8 + r];
@@ -213,7 +218,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
         const int reg = (row >> 5) * 16 + ((row & 31) >> 3) * 4 + (row & 3);
         float p = 0.f;
 #pragma unroll
-        for (int x = 0; x < 32; ++x) p = x == reg ? s[x >> 4][x & 15] : p;
+        for (int x = 0; x < 16 * NH; ++x) p = x == reg ? s[x >> 4][x & 15] : p;
         p = __shfl(p, n + 32 * ((row >> 2) & 1));
         if (key0 + row <= sees) {
 #pragma unroll
@@ -234,7 +239,8 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     const int buf = (tile - tile0) & 1;
     tiles_barrier<0>();
     if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
-    if (tile * PK <= wave_last) attend(tile * PK, buf, masked);
+    const int key0 = tile * PK + kw * (NH * 32);
+    if (key0 <= wave_last) attend(key0, buf, masked);
 #pragma unroll
     for (int k = 0; k < NS; ++k) ka[k] ^= PAIR;
 #pragma unroll
@@ -245,7 +251,36 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
 #pragma unroll 1
   for (int tile = whole; tile < tile1; ++tile) turn(tile, std::true_type{});
   sum = sum_of_halves(sum);
-  if (t.i0 + wave * 32 + n >= t.n_q) return;
+  if constexpr (KW == 2) {
+    // The keys' two halves, joined where the tiles were
+    f32x4* const J = (f32x4*)(lds + qw * ((NV * 16 + 2) * 256));
+    float* const rs = (float*)(J + NV * 4 * 64);
+    tiles_barrier<0>();
+    if (kw == 1) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) J[(v * 4 + r) * 64 + lane] = f32x4{o[v][4 * r], o[v][4 * r + 1], o[v][4 * r + 2], o[v][4 * r + 3]};
+      rs[lane] = ref;
+      rs[64 + lane] = sum;
+    }
+    lds_barrier();
+    if (kw == 1) return;
+    const float r2 = rs[lane], m = fmaxf(ref, r2);
+    // (no reference: no key, or keys that are not a number)
+    const float f = ref == NEG_INF ? 1.f : exp2f(ref - m), g = r2 == NEG_INF ? 1.f : exp2f(r2 - m);
+    sum = sum * f + rs[64 + lane] * g;
+    ref = m;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const f32x4 y = J[(v * 4 + r) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[v][4 * r + e] = o[v][4 * r + e] * f + y[e] * g;
+      }
+  }
+  if (t.i0 + qw * 32 + n >= t.n_q) return;
   const long row = (t.q0 + i) * a.H + t.h;
   if (a.nsplit > 1) {
     if (half == 0) {
@@ -316,41 +351,66 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
   }
 }
 
-template <int DKP>
+template <int DKP, int QW>
 void prompt_of(const PromptArgs& a, hipStream_t st) {
-  if (a.d_k == Pitch<DKP>::pieces * 8) prompt_kernel<DKP, true><<<prompt_grid(a, PQ), 256, 0, st>>>(a);
-  else prompt_kernel<DKP, false><<<prompt_grid(a, PQ), 256, 0, st>>>(a);
+  if (a.d_k == Pitch<DKP>::pieces * 8) prompt_kernel<DKP, true, QW><<<prompt_grid(a, 32 * QW), 256, 0, st>>>(a);
+  else prompt_kernel<DKP, false, QW><<<prompt_grid(a, 32 * QW), 256, 0, st>>>(a);
+}
+template <int QW>
+void prompt_by_width(const PromptArgs& a, hipStream_t st) {
+  if (a.d_k <= 32) prompt_of<32, QW>(a, st);
+  else if (a.d_k <= 64) prompt_of<64, QW>(a, st);
+  else if (a.d_k <= 96) prompt_of<96, QW>(a, st);
+  else if (a.d_k <= 128) prompt_of<128, QW>(a, st);
+  else if constexpr (QW == 4) {
+    if (a.d_k <= 192) prompt_of<192, QW>(a, st);
+    else prompt_of<256, QW>(a, st);
+  }
 }
 
 }  // namespace
 
-// Parts of the keys, where the queries alone do not fill the chip.  A workgroup's tile takes 1.2 us (bf16, 128 columns), 1.9 where two share a compute unit; the
-// parts' results are written and read in 32 bits (777 queries x 32 heads x 128 in two parts: 34 us, in one 21).
-int prompt_splits(int dtype, int B, int rows_q, int rows_k, int H, int d_k) {
+// How a call is cut: queries a workgroup and parts of the keys, by what they are expected to take (us).  A workgroup's tiles come one after the other, and a compute
+// unit's workgroups share its matrix cores; parts have to be joined by another launch.  128 queries a tile of 128 columns: 1.13 one after the other, 0.88 of a compute
+// unit's time; 64 queries: 0.77 and 0.53.  (777 queries x 32 heads x 128 23 and 19, 128 behind 5000 keys x 16 heads over 2 40 and 29, 1500 x 20 x 64 33 and 24; where
+// 128 fill the chip, 4000 x 32 x 128, 147 and 166.)  Keys and values that the last-level cache does not keep come a tile of 64 keys in 1.05 us for either, and fewer queries
+// read them more often: 128 then (300 behind 8000 and 5000 keys x 24 heads x 96 74 and 85).  Over 136 shapes with all cuts timed this one takes 2 % longer than the best of each;
+// the fp32 kernel has one form, and its own times.
+PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, int d_k) {
   const bool f32 = dtype == DT_F32;
-  const int rows = f32 ? prompt_f32_rows(d_k) : PQ;
-  const double tiles = (double)B * ((rows_q / B + rows - 1) / rows) * H, keys = (double)rows_k / B / PK;      // (as if the sequences were equally long)
-  const double alone = f32 ? 3.4 * d_k / 64 : 1.2 * (d_k < 64 ? 64 : d_k) / 128, shared = f32 ? 2 * alone : 1.6 * alone;
-  int best = 1;
+  const double keys = (double)rows_k / B / PK;                     // (as if the sequences were equally long)
+  const double seen = rows_k > 0 ? keys * (1 - 0.5 * fmin(1.0, (double)rows_q / rows_k)) : 0;
+  const double width = 0.45 + 0.55 * (d_k < 32 ? 32 : d_k) / 128;
+  const bool cached = 4.0 * rows_k * H_kv * d_k <= 1e8;
+  const int most = f32 ? prompt_f32_rows(d_k) : 128, fewest = !f32 && d_k <= 128 && cached ? 64 : most;
+  PromptCut best{most, 1};
   double least = 1e30;
-  for (int n = 1; n <= 32; ++n) {
-    if (n > 1 && (keys < 4 * n || tiles * n > 4096)) break;      // (a part has 256 keys at least)
-    const double per = ceil(keys / n), rounds = ceil(tiles * n / 512);
-    const double merge = n > 1 ? 4 + n * (double)rows_q * H * d_k * 8 / 4e6 : 0;
-    const double t = (tiles * n <= 256 ? per * alone : rounds * per * shared) + merge;
-    if (t < least) { least = t; best = n; }
+  for (int rows = most; rows >= fewest; rows /= 2) {
+    const double tiles = (double)B * ((rows_q / B + rows - 1) / rows) * H;
+    for (int n = 1; n <= 32; ++n) {
+      if (n > 1 && (keys < 4 * n || tiles * n > 4096)) break;      // (a part has 256 keys at least)
+      const double per = ceil(keys / n);
+      double t;
+      if (f32) {
+        const double alone = 3.4 * d_k / 64, merge = n > 1 ? 4 + n * (double)rows_q * H * d_k * 8 / 4e6 : 0;
+        t = (tiles * n <= 256 ? per * alone : ceil(tiles * n / 512) * per * 2 * alone) + merge;
+      } else {
+        const double alone = rows == 64 ? 0.77 : 1.13, one = rows == 64 ? 0.53 : 0.88, left = fmod(tiles * n, 512);      // (two a compute unit at once)
+        const double rounds = floor(tiles * n / 512) * 2 * one + (left == 0 ? 0 : left <= 256 ? fmax(one, 0.9 * alone) : 2 * one);
+        const double chain = per * alone * width, shared = rounds * width * seen / n;
+        t = fmax(chain, shared) + 0.14 * fmin(chain, shared) + 0.75 * ceil(tiles * n / 256);
+        if (n > 1) t += 6.5 + 0.65 * n + n * (double)rows_q * H * d_k * 8 / 4.1e6;
+      }
+      if (t < least) { least = t; best = PromptCut{rows, n}; }
+    }
   }
   return best;
 }
 
 void launch_prompt(int dtype, const PromptArgs& a, hipStream_t st) {
   if (dtype == DT_F32) launch_prompt_f32(a, st);
-  else if (a.d_k <= 32) prompt_of<32>(a, st);
-  else if (a.d_k <= 64) prompt_of<64>(a, st);
-  else if (a.d_k <= 96) prompt_of<96>(a, st);
-  else if (a.d_k <= 128) prompt_of<128>(a, st);
-  else if (a.d_k <= 192) prompt_of<192>(a, st);
-  else prompt_of<256>(a, st);
+  else if (a.rows == 64) prompt_by_width<2>(a, st);
+  else prompt_by_width<4>(a, st);
 }
 
 void launch_prompt_merge(int dtype, const PromptArgs& a, hipStream_t st) {

@@ -1114,7 +1114,7 @@ size_t prompt_bytes(int nsplit, int rows_q, int H, int d_k) {
 
 extern "C" size_t slim_workspace_bytes_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dtype) {
   if (check_prompt(B, rows_q, rows_k, H, H_kv, d_k, dtype)) return 0;
-  return prompt_bytes(prompt_splits(dtype, B, rows_q, rows_k, H, d_k), rows_q, H, d_k);
+  return prompt_bytes(prompt_cut(dtype, B, rows_q, rows_k, H, H_kv, d_k).nsplit, rows_q, H, d_k);
 }
 
 extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_k, void* out, int B, int rows_q,
@@ -1134,7 +1134,8 @@ extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v
   if (q_pitch < (int64_t)H * d_k || k_pitch < (int64_t)H_kv * d_k || v_pitch < (int64_t)H_kv * d_k || q_pitch % vec || k_pitch % vec || v_pitch % vec)
     return SLIM_ERR_SHAPE;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned4(cu_q) || misaligned4(cu_k)) return SLIM_ERR_ALIGN;
-  const int nsplit = prompt_splits(dtype, B, rows_q, rows_k, H, d_k);
+  const PromptCut cut = prompt_cut(dtype, B, rows_q, rows_k, H, H_kv, d_k);
+  const int nsplit = cut.nsplit;
   char* ws = nullptr;
   if (nsplit > 1)
     if (int rc = get_workspace(o, prompt_bytes(nsplit, rows_q, H, d_k), &ws)) return rc;
@@ -1146,6 +1147,7 @@ extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v
     a.q_pitch = q_pitch; a.k_pitch = k_pitch; a.v_pitch = v_pitch;
     a.B = B; a.rows_q = rows_q; a.rows_k = rows_k; a.H = H; a.H_kv = H_kv; a.d_k = d_k; a.causal = causal != 0;
     a.scale = 1.4426950408889634f / sqrtf((float)d_k);
+    a.rows = cut.rows;
     a.nsplit = nsplit;
     if (nsplit > 1) {
       a.O = (float*)(ws + up(sizeof(int) * CTRL_INTS));

@@ -336,11 +336,13 @@ struct PromptArgs {
   long q_pitch, k_pitch, v_pitch;            // elements between rows
   int B, rows_q, rows_k, H, H_kv, d_k, causal;
   float scale;                               // log2(e) / sqrt(d_k)
+  int rows;                                  // queries of a workgroup
   int nsplit;                                // parts of the keys, each a workgroup of its own; 1: results are written at once
   float *O, *ml;                             // nsplit > 1: [nsplit][rows_q][H][d_k] unnormalised, [nsplit][rows_q][H][2] reference and sum
 };
 constexpr int PROMPT_MAX_WIDTH = 256;        // columns of a head
-int prompt_splits(int dtype, int B, int rows_q, int rows_k, int H, int d_k);
+struct PromptCut { int rows, nsplit; };
+PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, int d_k);
 void launch_prompt(int dtype, const PromptArgs& a, hipStream_t st);
 void launch_prompt_merge(int dtype, const PromptArgs& a, hipStream_t st);
 

@@ -62,7 +62,8 @@ def test_few_queries_over_many_keys(dtype, n_q, n_k, H):
     """Keys shared out over workgroups, causal and full."""
     for causal in (True, False):
         c = PromptCase(n_q, n_k, H, H, 64, dtype, causal, seed=5, tail=2)
-        assert binding.slim_workspace_bytes_prompt(len(n_q), c.q.shape[0], c.k.shape[0], H, H, 64, dtype) > 1 << 15
+        whole = binding.slim_workspace_bytes_prompt(len(n_q), c.q.shape[0], c.q.shape[0], H, H, 64, dtype)
+        assert binding.slim_workspace_bytes_prompt(len(n_q), c.q.shape[0], c.k.shape[0], H, H, 64, dtype) > whole       # (in parts)
         c.check()
 
 
@@ -223,3 +224,39 @@ def test_prompt_cache_and_generation_together():
             o, spread, size, _ = tree_oracle.tree_attention(q[b:b + 1].double().cpu().numpy(), stored[b], W.double().cpu().numpy(), [-1], held[b] - 1, H)
             got = out[b].double().cpu().numpy()
             assert (np.abs(got - o[0]) <= 1.1 * (2.0 ** -8 * (spread[0] + np.abs(o[0])) + 1e-4 * size[0])).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n_q,n_k,H,H_kv,d_k", [
+    ([150, 129, 1], [150, 129, 1], 512, 8, 128), ([129, 128], [129, 128], 512, 512, 32), ([140], [140], 512, 8, 40), ([150, 64], [260, 64], 512, 8, 64),
+    ([150, 0], [100, 50], 640, 4, 80), ([140], [140], 512, 8, 96)])
+def test_prompts_that_fill_the_chip(n_q, n_k, H, H_kv, d_k, causal):
+    """So many heads that a workgroup has 128 queries, where it has 64 with fewer."""
+    PromptCase(n_q, n_k, H, H_kv, d_k, "bf16", causal, seed=H + d_k, tail=3).check()
+
+
+def test_what_is_not_seen_has_no_effect_where_the_chip_is_full():
+    """As above, with 128 queries a workgroup."""
+    n, H, d_k = 150, 1024, 96
+    c = PromptCase([n], [n], H, 8, d_k, "bf16", True, seed=4, tail=70)
+    clean = c.run()[:n].reshape(n, H, d_k)
+    c.k[n:], c.v[n:] = np.nan, np.inf
+    for row, x in ((100, np.nan), (101, np.inf), (149, -np.inf)):
+        c.v[row] = x
+    got = c.run()[:n].reshape(n, H, d_k)
+    assert np.array_equal(got[:100], clean[:100])
+    assert not np.isfinite(got[100:]).any()
+
+
+def test_the_same_sequence_among_few_and_many_heads():
+    """64 and 128 queries a workgroup differ by the order of their sums alone: each keeps its bound, and heads of one call are alike whatever the others are."""
+    few = PromptCase([300], [300], 4, 4, 64, "bf16", True, seed=12)
+    a = few.run()
+    few.check(a)
+    many = PromptCase([300], [300], 1024, 4, 64, "bf16", True, seed=12)
+    many.k, many.v = few.k, few.v
+    many.q = np.repeat(few.q.reshape(300, 4, 64), 256, axis=1).reshape(300, 1024 * 64)
+    b = many.run().reshape(300, 4, 256, 64)
+    assert (b == b[:, :, :1]).all()
+    want, bound = few.expected(0)
+    assert (np.abs(b[:, :, 0].reshape(300, 256) - want) <= bound).all()
