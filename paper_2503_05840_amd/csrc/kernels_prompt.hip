@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
     constexpr bool MASKED = decltype(masked)::value;
     const char* const vt = lds + buf * PAIR + PAIR / 2 + kw * (NH * 32 * PC * 16);
     f32x16 s[NH];
-    __builtin_amdgcn_s_setprio(1);                 // (the SIMD's other wave fills in: sequences of 8000 and 5000 keys x 24 heads x 96 75 -> 71 us)
+    __builtin_amdgcn_s_setprio(1);                 // (the SIMD's other wave fills in: 8000 and 6854 keys x 24 heads x 96 75 -> 71 us)
 #pragma unroll
     for (int x = 0; x < NH; ++x) {
 #pragma unroll
@@ -374,7 +374,7 @@ void prompt_by_width(const PromptArgs& a, hipStream_t st) {
 // unit's workgroups share its matrix cores; parts have to be joined by another launch.  128 queries a tile of 128 columns: 1.13 one after the other, 0.88 of a compute
 // unit's time; 64 queries: 0.77 and 0.53.  (777 queries x 32 heads x 128 23 and 19, 128 behind 5000 keys x 16 heads over 2 40 and 29, 1500 x 20 x 64 33 and 24; where
 // 128 fill the chip, 4000 x 32 x 128, 147 and 166.)  Keys and values that the last-level cache does not keep come a tile of 64 keys in 1.05 us for either, and fewer queries
-// read them more often: 128 then (300 behind 8000 and 5000 keys x 24 heads x 96 74 and 85).  Over 136 shapes with all cuts timed this one takes 2 % longer than the best of each;
+// read them more often: 128 then (the last 300 of 8000 and 6854 rows x 24 heads x 96 74 and 85).  Over 147 shapes with all cuts timed this one takes 2 % longer than the best of each;
 // the fp32 kernel has one form, and its own times.
 PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, int d_k) {
   const bool f32 = dtype == DT_F32;

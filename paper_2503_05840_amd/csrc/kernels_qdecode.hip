@@ -1,7 +1,7 @@
 // The decode step of slim attention over a K-cache in 4 or 8 bits (its format: kernels_quant.hip): scores, weighted sum of K, merge + projection through W_KV.
 // Three launches; none of their workgroups waits for another.  What a code stands for is exact in bf16, so that K enters both products without a rounding.
 // The codes are read twice: the numerators of all heads weigh every column, and the H x d sums of one pass would fill the registers of a compute unit each, whose partial
-// results (512 KB a unit at 32 heads x 4096) are more bytes than the second pass.  1 x 16384 rows x 32 x 128 in 4 bits: 9 + 15 + 13.5 us.
+// results (512 KB a unit at 32 heads x 4096) are more bytes than the second pass.  1 x 16384 rows x 32 x 128 in 4 bits: 9 + 15 + 12.6 us.
 #include "device_common.h"
 #include "slim_kernels.h"
 
@@ -231,8 +231,9 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
 
 // The same for heads of 32 CH columns (32, 64, 96, 128): four lanes a head, 8 CH columns each, none idle.  A wave has eight heads x 16 rows, in two halves of the
 // lanes eight rows each; four waves a block of 64 rows, which meet in LDS for its reference; eight waves sixteen heads, which share the table.
-// With 16 lanes a head, heads of 96 columns kept a quarter of the lanes idle: 16 sequences of 600..5000 rows x 24 heads in 8 bits, rotary 35 us and now 31, without 22.7
-// and now 19.9 (5.5 TB/s of codes).  1 x 16384 x 32 x 128 in 4 bits 9 us.
+// With 16 lanes a head, heads of 96 columns kept a quarter of the lanes idle: 16 sequences of 600..5000 rows x 24 heads in 8 bits, rotary 35 us and then 31, without 22.7
+// and 19.9 (5.5 TB/s of codes).  Rotary with what all rows need ahead of the codes 29.7, of which the vector ALU has 14; for six waves a SIMD the registers do not do (36).
+// 1 x 16384 x 32 x 128 in 4 bits 9 us.
 template <bool F32, int BITS, int CH, bool ROPE>
 __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
   constexpr int P = 4, RP = 2, DK = 32 * CH;
@@ -703,7 +704,7 @@ __device__ __forceinline__ void split_weights(const QDecodeArgs& a, int b0, int 
 
 // out[b][h d_k + j] = sum_c C[b][h][c] W[c][h d_k + j].  A workgroup takes a head, up to 128 of its columns, 16 sequences and a row split of W: it merges the
 // splits' partial sums into LDS (as bf16 hi + lo, which keeps 16 bits of them; W is bf16), multiplies on 16x16x32 matrix instructions, and whoever of a
-// head's row splits comes last adds their results in the order of their numbers.  HBM-bound on W for small batches: 1 x 4096 x 4096 12 us, 6.4 of them W at 5.2 TB/s, 2 the
+// head's row splits comes last adds their results in the order of their numbers.  HBM-bound on W for small batches: 1 x 4096 x 4096 12.6 us, 6.4 of them W at 5.2 TB/s, 2 the
 // start, 3 the meeting of the row splits.  (Sixteen columns and all rows a workgroup, which needs no meeting, took 16: pieces of 32 bytes.)
 template <bool F32>
 __global__ __launch_bounds__(256) void qproject_kernel(QDecodeArgs a) {
