@@ -569,7 +569,7 @@ def slim_quant_decode(q, codes, scales, W_KV, out, B, H, T, d, bits, dtype="bf16
     el = _element(dtype)
     _lens_ok(seq_lens, seq_lens_host, B)
     _one_device(q, codes, scales, W_KV, out, seq_lens, workspace, rope_table)
-    if rope_table is not None and (rope_table.dtype != torch.float32 or rope_table.numel() < T * (d // H)):
+    if rope_table is not None and (rope_table.dtype != torch.float32 or rope_table.numel() < T * (d // max(H, 1))):
         raise ValueError("rope_table must be float32 and hold T positions")
     ptrs = (_tree_ptr(q, (B, d), el), *_quant_ptrs(codes, scales, B, T, d, bits, t_stride), _tree_ptr(W_KV, (d, d), el), _tree_ptr(out, (B, d), el))
     o, keep = _call_opts(dtype, seq_lens, seq_lens_host, t_stride, workspace, stage_ms, rope_table)

@@ -160,6 +160,27 @@ def test_decode_past_32_bit_offsets(bits):
     assert (out[:B - 1] == 0).all()
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("d_k", [32, 40])
+def test_decode_of_more_than_two_million_rows(bits, d_k):
+    """More blocks of 64 rows than a grid's second dimension is given; the rows that count are behind them."""
+    H, first, n = 4, 32768 * 64, 70
+    small = QuantCase(1, H, d_k, n, bits, seed=21, q_scale=60.0)
+    most = np.array([(small.K[0][:, h * d_k:(h + 1) * d_k] @ small.q[0, h * d_k:(h + 1) * d_k]).max() for h in range(H)]) / np.sqrt(d_k)
+    assert (most > 60).all()                                     # (2^21 rows of zeros have a score of 0 each: 1e-20 of the sum)
+    small.device()
+    codes, scales = binding.slim_quant_cache(1, first + n, H * d_k, bits)
+    codes[0, first:first + small.rows], scales[0, :, first:first + small.rows] = small.dev["codes"][0], small.dev["scales"][0]
+    out = small.dev["q"].clone().fill_(float("nan"))
+    binding.slim_quant_decode(small.dev["q"], codes, scales, small.dev["W"], out, 1, H, first + n, H * d_k, bits)
+    small.check(got=out.float().cpu().numpy().astype(np.float64))
+
+
+@pytest.mark.parametrize("dtype,H,d_k,base", [("bf16", 40, 32, 10000.0), ("bf16", 24, 96, None), ("f32", 18, 64, 10000.0)])
+def test_decode_of_unequal_sequences_with_more_than_sixteen_heads(dtype, H, d_k, base):
+    QuantCase(5, H, d_k, 700, 8, dtype, lens=[700, 1, 64, 65, 333], base=base, seed=H).check()
+
+
 DECODE = [  # B, H, d_k, T, lens
     (1, 1, 32, 1, None), (1, 4, 64, 63, None), (2, 4, 64, 65, [1, 65]), (3, 20, 64, 300, [0, 300, 129]), (1, 12, 72, 200, None), (2, 4, 128, 520, [64, 511]),
     (1, 40, 32, 100, None), (2, 24, 96, 130, [130, 33]), (17, 2, 48, 90, list(range(1, 18))), (1, 3, 160, 70, None), (1, 2, 272, 140, None), (1, 32, 128, 97, None)]
