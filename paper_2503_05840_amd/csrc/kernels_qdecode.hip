@@ -230,42 +230,41 @@ __global__ __launch_bounds__(256) void qscores_kernel(QDecodeArgs a) {
 }
 
 // The same for heads of 32 CH columns (32, 64, 96, 128): four lanes a head, 8 CH columns each, none idle.  A wave has eight heads x 16 rows, in two halves of the
-// lanes eight rows each; four waves a block of 64 rows, which meet in LDS for its reference; eight waves sixteen heads, which share the table.
-// With 16 lanes a head, heads of 96 columns kept a quarter of the lanes idle: 16 sequences of 600..5000 rows x 24 heads in 8 bits, rotary 35 us and then 31, without 22.7
-// and 19.9 (5.5 TB/s of codes).  Rotary with what all rows need ahead of the codes 29.7, of which the vector ALU has 14; for six waves a SIMD the registers do not do (36).
-// 1 x 16384 x 32 x 128 in 4 bits 9 us.
+// lanes eight rows each; the four waves have a block of 64 rows, and meet in LDS for its reference.
+// With 16 lanes a head, heads of 96 columns kept a quarter of the lanes idle: 16 sequences of 600..5000 rows x 24 heads in 8 bits, rotary 35 us, without 22.7; now
+// 24.6 and 19.3 (5.6 TB/s of codes).  Rotary, the vector ALU has 14 of it.  Eight waves, whose sixteen heads shared the table, had fewer workgroups to fill one's waits with
+// another's work: 29.7, and 31.3 with q and the table behind the codes; registers for five waves a SIMD spill (37).  1 x 16384 x 32 x 128 in 4 bits 9 us.
 template <bool F32, int BITS, int CH, bool ROPE>
-__global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
+__global__ __launch_bounds__(256) void qscores_even_kernel(QDecodeArgs a) {
   constexpr int P = 4, RP = 2, DK = 32 * CH;
   __shared__ f32x4 table[ROPE ? QUANT_ROWS * DK / 4 : 1];
-  __shared__ float most[2][4][8], total[2][4][8];
+  __shared__ float most[4][8], total[4][8];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   {
     const long wgs = (long)gridDim.x * gridDim.y * gridDim.z, wg = blockIdx.x + (long)gridDim.x * (blockIdx.y + (long)gridDim.y * blockIdx.z);
-    for (long i = wg * 512 + tid; i < a.ncounters; i += wgs * 512) a.counters[i] = 0;
+    for (long i = wg * 256 + tid; i < a.ncounters; i += wgs * 256) a.counters[i] = 0;
   }
   // Blocks of the same rows follow each other over the heads and sequences: they take cos and sin from the L2s.  (Which comes first moves on by one from rows to rows:
   // an XCD would get the same sequences and heads all along, and the others the short ones.)
-  const int groups = (a.H + 15) / 16, blk = blockIdx.z * gridDim.y + blockIdx.y;
+  const int groups = (a.H + 7) / 8, blk = blockIdx.z * gridDim.y + blockIdx.y;
   const unsigned at_block = (blockIdx.x + (unsigned)blk) % gridDim.x;
   const int b = at_block / groups, hg = at_block % groups;
   const int len = seq_len_of(a.seq_lens, b, a.T);
   if (blk >= (len + QUANT_ROWS - 1) / QUANT_ROWS) return;
   const int t0 = blk * QUANT_ROWS;
-  const int set = wave >> 2, part = wave & 3;      // eight heads, sixteen rows
   const int i = lane & 3, slot = (lane >> 2) & 7, half = lane >> 5;
-  const int h = hg * 16 + set * 8 + slot, hc = min(h, a.H - 1);      // (heads past the last: the last again, not stored)
-  const int col = hc * DK + i * 8 * CH, first = part * 16 + half * 8;         // this lane's columns and first row of the block
+  const int h = hg * 8 + slot, hc = min(h, a.H - 1);      // (heads past the last: the last again, not stored)
+  const int col = hc * DK + i * 8 * CH, first = wave * 16 + half * 8;         // this lane's columns and first row of the block
   const long row_bytes = (long)a.d * BITS / 8;
-  const unsigned char* codes = a.codes + ((long)b * a.stride + t0 + part * 16) * row_bytes;
+  const unsigned char* codes = a.codes + ((long)b * a.stride + t0 + wave * 16) * row_bytes;
   const unsigned at = (unsigned)(half * 8 * (int)row_bytes + col * BITS / 8);
-  constexpr int PER_THREAD = DK / 32;               // table entries: 64 DK / 4 over 512 threads
+  constexpr int PER_THREAD = DK / 16;               // table entries: 64 DK / 4 over 256 threads
   f32x4 turn[ROPE ? PER_THREAD : 1];
   if constexpr (ROPE) {
     // (rows behind the sequence, whose score is masked, have no position in the table)
 #pragma unroll
     for (int x = 0; x < PER_THREAD; ++x) {
-      const int at_entry = tid + x * 512, row = at_entry / (DK / 4), k = at_entry % (DK / 4);
+      const int at_entry = tid + x * 256, row = at_entry / (DK / 4), k = at_entry % (DK / 4);
       turn[x] = *(const f32x4*)(a.rope + (long)min(t0 + row, len - 1) * DK + k * 4);
     }
   }
@@ -303,10 +302,9 @@ __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
   __builtin_amdgcn_sched_barrier(0);
   if constexpr (ROPE) {
 #pragma unroll
-    for (int x = 0; x < PER_THREAD; ++x) table[tid + x * 512] = turn[x];
+    for (int x = 0; x < PER_THREAD; ++x) table[tid + x * 256] = turn[x];
     lds_barrier();
   }
-  if (hg * 16 + set * 8 >= a.H) return;  // (eight heads that there are not: the barriers below are of the waves that stay)
   float s[RP];
 #pragma unroll
   for (int j = 0; j < RP; ++j) {
@@ -364,10 +362,10 @@ __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
   }
   m = max_over_lanes<P>(m);
   m = fmaxf(m, __shfl_xor(m, 32));
-  if (i == 0 && half == 0) most[set][part][slot] = m;
+  if (i == 0 && half == 0) most[wave][slot] = m;
   lds_barrier();
 #pragma unroll
-  for (int k = 0; k < 4; ++k) m = fmaxf(m, most[set][k][slot]);
+  for (int k = 0; k < 4; ++k) m = fmaxf(m, most[k][slot]);
   const float ref = m == NEG_INF ? 0.f : ceilf(m);
   float l = 0.f, p[RP];
 #pragma unroll
@@ -378,17 +376,17 @@ __global__ __launch_bounds__(512) void qscores_even_kernel(QDecodeArgs a) {
   }
   l = sum_over_lanes<P>(l);
   l += __shfl_xor(l, 32);
-  if (i == 0 && half == 0) total[set][part][slot] = l;
+  if (i == 0 && half == 0) total[wave][slot] = l;
   const long o = ((long)b * a.H + hc) * a.Tp + t0 + first + i * RP;
   if (h < a.H) {
     if constexpr (F32) *(f32x2*)((float*)a.P + o) = f32x2{p[0], p[1]};
     else *(bf16x2*)((uint16_t*)a.P + o) = bf16x2{(__bf16)p[0], (__bf16)p[1]};
   }
   lds_barrier();
-  if (part == 0 && i == 0 && half == 0 && h < a.H) {
+  if (wave == 0 && i == 0 && half == 0 && h < a.H) {
     const long x = ((long)b * a.H + h) * a.NB + blk;
     a.ref[x] = ref;
-    a.sum[x] = (total[set][0][slot] + total[set][1][slot]) + (total[set][2][slot] + total[set][3][slot]);
+    a.sum[x] = (total[0][slot] + total[1][slot]) + (total[2][slot] + total[3][slot]);
   }
 }
 
@@ -899,9 +897,9 @@ void scores_of(const QDecodeArgs& a, hipStream_t st) {
 }
 template <bool F32, int BITS, int CH>
 void even_scores(const QDecodeArgs& a, hipStream_t st) {
-  const dim3 grid((a.H + 15) / 16 * a.B, a.NB < 32768 ? a.NB : 32768, (a.NB + 32767) / 32768);
-  if (a.rope) qscores_even_kernel<F32, BITS, CH, true><<<grid, 512, 0, st>>>(a);
-  else qscores_even_kernel<F32, BITS, CH, false><<<grid, 512, 0, st>>>(a);
+  const dim3 grid((a.H + 7) / 8 * a.B, a.NB < 32768 ? a.NB : 32768, (a.NB + 32767) / 32768);
+  if (a.rope) qscores_even_kernel<F32, BITS, CH, true><<<grid, 256, 0, st>>>(a);
+  else qscores_even_kernel<F32, BITS, CH, false><<<grid, 256, 0, st>>>(a);
 }
 template <bool F32, int BITS>
 void scores_by_width(const QDecodeArgs& a, hipStream_t st) {
