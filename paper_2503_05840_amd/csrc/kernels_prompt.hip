@@ -378,17 +378,20 @@ void prompt_by_width(const PromptArgs& a, hipStream_t st) {
 // the fp32 kernel has one form, and its own times.
 PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, int d_k) {
   const bool f32 = dtype == DT_F32;
-  const double keys = (double)rows_k / B / PK;                     // (as if the sequences were equally long)
-  const double seen = rows_k > 0 ? keys * (1 - 0.5 * fmin(1.0, (double)rows_q / rows_k)) : 0;
+  const int busy = rows_q < B ? rows_q : B;                        // sequences that can have queries; the others' places are empty
+  const double keys = (double)rows_k / B / PK;                     // (as if the sequences were equally long, and so the queries of those)
+  const double seen = rows_k > 0 && busy > 0 ? keys * (1 - 0.5 * fmin(1.0, (double)rows_q / rows_k * ((double)B / busy))) : 0;
   const double width = 0.45 + 0.55 * (d_k < 32 ? 32 : d_k) / 128;
   const bool cached = 4.0 * rows_k * H_kv * d_k <= 1e8;
   const int most = f32 ? prompt_f32_rows(d_k) : 128, fewest = !f32 && d_k <= 128 && cached ? 64 : most;
   PromptCut best{most, 1};
+  if (busy == 0) return best;
   double least = 1e30;
   for (int rows = most; rows >= fewest; rows /= 2) {
-    const double tiles = (double)B * ((rows_q / B + rows - 1) / rows) * H;
+    const double tiles = (double)busy * ((rows_q / busy + rows - 1) / rows) * H;
+    const long places = ((long)rows_q / rows + B + 7) / 8 * 8 * H;   // workgroups of a part, the empty ones among them
     for (int n = 1; n <= 32; ++n) {
-      if (n > 1 && (keys < 4 * n || tiles * n > 4096)) break;      // (a part has 256 keys at least)
+      if (n > 1 && (keys < 4 * n || tiles * n > 4096 || places * n >= 1 << 24)) break;      // (a part has 256 keys at least; a launch has 32 bits of threads)
       const double per = ceil(keys / n);
       double t;
       if (f32) {

@@ -51,3 +51,14 @@ def one_pass_tiles(B, H, T, d_model):
     """Head tiles of a workgroup of the one-pass X-cache kernel."""
     i = ctypes.c_int
     return _rule("_ZN4slim12xfused_tilesEiiii", i, i, i, i, i)(B, H, d_model, one_pass_splits(B, H, T, d_model)[0])
+
+
+class _PromptCut(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("parts", ctypes.c_int)]
+
+
+def prompt_cut(dtype, B, rows_q, rows_k, H, H_kv, d_k):
+    """Queries of a workgroup of prompt attention, and parts of the keys."""
+    i = ctypes.c_int
+    c = _rule("_ZN4slim10prompt_cutEiiiiiii", _PromptCut, *[i] * 7)(binding.DTYPES[dtype], B, rows_q, rows_k, H, H_kv, d_k)
+    return c.rows, c.parts
