@@ -1,4 +1,6 @@
 // Attention over whole prompts in bf16: causal or full, grouped heads, packed sequences.
+#include <algorithm>
+
 #include "prompt_common.h"
 
 namespace slim {
@@ -390,8 +392,8 @@ PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, 
   for (int rows = most; rows >= fewest; rows /= 2) {
     const double tiles = (double)busy * ((rows_q / busy + rows - 1) / rows) * H;
     const long places = ((long)rows_q / rows + B + 7) / 8 * 8 * H;   // workgroups of a part, the empty ones among them
-    for (int n = 1; n <= 32; ++n) {
-      if (n > 1 && (keys < 4 * n || tiles * n > 4096 || places * n >= 1 << 24)) break;      // (a part has 256 keys at least; a launch has 32 bits of threads)
+    for (int n = 1; n <= PROMPT_MAX_PARTS; ++n) {
+      if (n > 1 && (keys * PK < PROMPT_PART_KEYS * n || tiles * n > PROMPT_PART_TILES || places * n >= 1 << 24)) break;      // (a launch has 32 bits of threads)
       const double per = ceil(keys / n);
       double t;
       if (f32) {
@@ -408,6 +410,12 @@ PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, 
     }
   }
   return best;
+}
+
+// A sequence has at most `rows` queries for each of its workgroups, and one more in the mean, which the cut rounds off.
+size_t prompt_most_part_rows(int dtype, int rows_q, int rows_k, int H, int d_k) {
+  const size_t parts = std::min(rows_k / PROMPT_PART_KEYS, PROMPT_MAX_PARTS), rows = dtype == DT_F32 ? prompt_f32_rows(d_k) : 128;
+  return parts > 1 ? std::min(parts * rows_q * H, PROMPT_PART_TILES * (rows + 1)) : 0;
 }
 
 void launch_prompt(int dtype, const PromptArgs& a, hipStream_t st) {

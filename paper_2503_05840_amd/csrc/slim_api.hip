@@ -1105,16 +1105,21 @@ int check_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dt
   return (long)H * (rows_q / 64 + B + 8) >= 1 << 24 ? SLIM_ERR_SHAPE : SLIM_OK;           // (workgroups of 256 threads, 32 bits of those)
 }
 
-size_t prompt_bytes(int nsplit, int rows_q, int H, int d_k) {
+// part_rows: parts x queries x heads
+size_t prompt_bytes(size_t part_rows, int d_k) {
   // (the control block: as above)
-  return up(sizeof(int) * CTRL_INTS) + (nsplit > 1 ? up(sizeof(float) * (size_t)nsplit * rows_q * H * d_k) + up(sizeof(float) * 2 * (size_t)nsplit * rows_q * H) : 0);
+  return up(sizeof(int) * CTRL_INTS) + up(sizeof(float) * part_rows * d_k) + up(sizeof(float) * 2 * part_rows);
 }
+
+// What a caller's workspace holds for a call.  The parts that a call is cut into go up and down with its sizes; the bound only grows, so that a workspace sized for the
+// largest prompt, context and batch serves every smaller call: at most 4096 workgroups' queries, 275 MB at 128 columns.
+size_t prompt_workspace(int dtype, int rows_q, int rows_k, int H, int d_k) { return prompt_bytes(prompt_most_part_rows(dtype, rows_q, rows_k, H, d_k), d_k); }
 
 }  // namespace
 
 extern "C" size_t slim_workspace_bytes_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dtype) {
   if (check_prompt(B, rows_q, rows_k, H, H_kv, d_k, dtype)) return 0;
-  return prompt_bytes(prompt_cut(dtype, B, rows_q, rows_k, H, H_kv, d_k).nsplit, rows_q, H, d_k);
+  return prompt_workspace(dtype, rows_q, rows_k, H, d_k);
 }
 
 extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_k, void* out, int B, int rows_q,
@@ -1137,8 +1142,10 @@ extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v
   const PromptCut cut = prompt_cut(dtype, B, rows_q, rows_k, H, H_kv, d_k);
   const int nsplit = cut.nsplit;
   char* ws = nullptr;
+  // (the library's own scratch grows by what this call takes)
+  const size_t part_rows = (size_t)nsplit * rows_q * H;
   if (nsplit > 1)
-    if (int rc = get_workspace(o, prompt_bytes(nsplit, rows_q, H, d_k), &ws)) return rc;
+    if (int rc = get_workspace(o, o && o->workspace ? prompt_workspace(dtype, rows_q, rows_k, H, d_k) : prompt_bytes(part_rows, d_k), &ws)) return rc;
   hipStream_t st = o ? (hipStream_t)o->stream : nullptr;
   StageTimer tm(o, st);
   if (rows_q > 0) {
@@ -1151,7 +1158,7 @@ extern "C" int slim_prompt_attention(const void* q, const void* k, const void* v
     a.nsplit = nsplit;
     if (nsplit > 1) {
       a.O = (float*)(ws + up(sizeof(int) * CTRL_INTS));
-      a.ml = (float*)((char*)a.O + up(sizeof(float) * (size_t)nsplit * rows_q * H * d_k));
+      a.ml = (float*)((char*)a.O + up(sizeof(float) * part_rows * d_k));
     }
     launch_prompt(dtype, a, st);
     if (nsplit > 1) launch_prompt_merge(dtype, a, st);

@@ -341,8 +341,11 @@ struct PromptArgs {
   float *O, *ml;                             // nsplit > 1: [nsplit][rows_q][H][d_k] unnormalised, [nsplit][rows_q][H][2] reference and sum
 };
 constexpr int PROMPT_MAX_WIDTH = 256;        // columns of a head
+constexpr int PROMPT_MAX_PARTS = 32, PROMPT_PART_KEYS = 256, PROMPT_PART_TILES = 4096;      // parts of the keys at the most, keys of a part at the least, workgroups with queries in all
 struct PromptCut { int rows, nsplit; };
 PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, int d_k);
+// Parts x queries x heads of a call that is cut, at the most, and of every smaller one (0: none of them is cut)
+size_t prompt_most_part_rows(int dtype, int rows_q, int rows_k, int H, int d_k);
 void launch_prompt(int dtype, const PromptArgs& a, hipStream_t st);
 void launch_prompt_merge(int dtype, const PromptArgs& a, hipStream_t st);
 
