@@ -201,7 +201,7 @@ int slim_variant_for(int B, int H, int T, int d, int dtype);
 /* Upper bound of the device scratch slim_decode / vanilla_kv_decode need for this shape.  None of the
  * slim_workspace_bytes* functions shrinks as T grows: a workspace sized for a cache's capacity serves
  * every shorter context of the same B, H and widths (one of slim_workspace_bytes_tree every smaller batch and
- * tree as well, one of slim_workspace_bytes_prompt any fewer queries, keys and sequences). */
+ * tree as well, one of slim_workspace_bytes_quant every smaller batch, one of slim_workspace_bytes_prompt any fewer queries, keys and sequences). */
 size_t slim_workspace_bytes(int B, int H, int T, int d, int dtype);
 /* The same for slim_decode_xcache (projection width H*d_k, cache width d_model). */
 size_t slim_workspace_bytes_xcache(int B, int H, int T, int d_model, int d_k, int dtype);

@@ -2,6 +2,8 @@
 // Three launches; none of their workgroups waits for another.  What a code stands for is exact in bf16, so that K enters both products without a rounding.
 // The codes are read twice: the numerators of all heads weigh every column, and the H x d sums of one pass would fill the registers of a compute unit each, whose partial
 // results (512 KB a unit at 32 heads x 4096) are more bytes than the second pass.  1 x 16384 rows x 32 x 128 in 4 bits: 9 + 15 + 12.6 us.
+#include <algorithm>
+
 #include "device_common.h"
 #include "slim_kernels.h"
 
@@ -921,26 +923,38 @@ int qdecode_counters(int B, int H, int d) { return H * ((d / H + QP_COLS - 1) / 
 // How the work is cut.  Splits of the weighted sum: a workgroup for every compute unit (with two, one sequence of 16384 rows x 4096 took 18.6 us instead of 15.9, as
 // much more to write and merge), but of 1024 rows at the most where that does not make more than four a unit: sequences of a batch are not equally long (16 of up
 // to 5000 rows x 2304 in 8 bits: two splits 38.6 us, four 28.6).  128 rows at least: a step of 32 for every wave.  Row splits of W: a workgroup a unit, 256 rows at the most.
-// (The splits themselves go up and down with T; `most_splits` only grows.)
-void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* most_splits, int* csw, int* crows) {
+static long weighted_units(int dtype, int H, int d) {          // workgroups of a split of one sequence
+  return dtype == DT_F32 ? (long)((d + 511) / 512) * ((H + 7) / 8) : (long)((d + QW_COLS - 1) / QW_COLS) * ((H + 31) / 32);
+}
+static long wanted_splits(int nb, long units) {
+  const long want = (256 + units - 1) / units, even = std::min<long>((nb + 15) / 16, 1024 / units);
+  return std::min<long>(std::max(want, even), QP_MAX_SPLITS);
+}
+static long wanted_row_splits(int d, long tiles) {
+  return std::min<long>(std::max<long>((256 + tiles - 1) / tiles, (d + QP_MAX_ROWS - 1) / QP_MAX_ROWS), d / 32);
+}
+void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* csw, int* crows) {
   const int nb = (T + QUANT_ROWS - 1) / QUANT_ROWS;
-  const long units = dtype == DT_F32 ? (long)B * ((d + 511) / 512) * ((H + 7) / 8) : (long)B * ((d + QW_COLS - 1) / QW_COLS) * ((H + 31) / 32);
-  long want = (256 + units - 1) / units, even = (nb + 15) / 16;
-  if (even > 1024 / units) even = 1024 / units;
-  if (want < even) want = even;
-  want = want > QP_MAX_SPLITS ? QP_MAX_SPLITS : want;
-  int p = (int)((nb + want - 1) / want);
-  *per = p < 2 ? 2 : p;
+  const long want = wanted_splits(nb, B * weighted_units(dtype, H, d));
+  *per = std::max((int)((nb + want - 1) / want), 2);
   *nsplit = (nb + *per - 1) / *per;
-  *most_splits = (int)((nb + 1) / 2 < want ? (nb + 1) / 2 : want);
-  const int d_k = d / H, ct = (d_k + QP_COLS - 1) / QP_COLS;
-  const long tiles = (long)H * ct * ((B + QP_BATCH - 1) / QP_BATCH);
-  const int least = (d + QP_MAX_ROWS - 1) / QP_MAX_ROWS, most = d / 32;
-  long c = (256 + tiles - 1) / tiles;
-  if (c < least) c = least;
-  if (c > most) c = most;
+  const long c = wanted_row_splits(d, qdecode_counters(B, H, d));
   *crows = (int)(((d + c - 1) / c + 31) / 32 * 32);
   *csw = (d + *crows - 1) / *crows;
+}
+
+// The splits themselves go up and down with T, and with B they go down faster than it goes up: B ceil(x / B) <= x + B - 1, B floor(y / B) <= y, and a sequence has no more
+// splits in a larger batch than by itself.
+size_t qdecode_most_splits(int dtype, int B, int H, int T, int d) {
+  const int nb = (T + QUANT_ROWS - 1) / QUANT_ROWS;
+  const long units = weighted_units(dtype, H, d), alone = std::min<long>((nb + 1) / 2, wanted_splits(nb, units));
+  return std::min(B * alone, std::max((256 + units - 1) / units + B - 1, std::min((long)B * ((nb + 15) / 16), 1024 / units)));
+}
+// The same for the row splits of W, sixteen sequences at a time.
+size_t qdecode_most_row_splits(int B, int H, int d) {
+  const long tiles = qdecode_counters(1, H, d), least = (d + QP_MAX_ROWS - 1) / QP_MAX_ROWS, groups = (B + QP_BATCH - 1) / QP_BATCH;
+  const long alone = wanted_row_splits(d, tiles);
+  return alone > 1 ? std::min(B * alone, std::max(QP_BATCH * ((256 + tiles - 1) / tiles + groups - 1), B * least)) : 0;
 }
 
 void launch_qdecode_scores(int dtype, const QDecodeArgs& a, hipStream_t st) {

@@ -1002,26 +1002,26 @@ int quant_rows(bool write, const void* src, const int32_t* cu_rows, void* codes,
 
 struct QDecodePlan { size_t off_P, off_ref, off_sum, off_C, off_sref, off_ssum, off_part, off_counters, total; };
 
-// Every term grows with T: the splits of a context are bounded by those of a longer one.
+// Every term grows with T and B, so that a workspace sized for the largest batch and context serves every smaller one.  Splits and row splits do not by themselves:
+// their place is a bound that does, less than twice what the largest of these batches takes.
 QDecodePlan qdecode_layout(QDecodeArgs& a, int dtype) {
   a.NB = (a.T + QUANT_ROWS - 1) / QUANT_ROWS;
   a.Tp = a.NB * QUANT_ROWS;
-  int most;
-  qdecode_cut(dtype, a.B, a.H, a.T, a.d, &a.per, &a.nsplit, &most, &a.csw, &a.crows);
+  qdecode_cut(dtype, a.B, a.H, a.T, a.d, &a.per, &a.nsplit, &a.csw, &a.crows);
   QDecodePlan p;
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += up(bytes); return at; };
   take(sizeof(int) * CTRL_INTS);             // (a workspace's control block: what slim_status reads of a decode step on the same workspace stays)
-  const size_t BH = (size_t)a.B * a.H;
+  const size_t BH = (size_t)a.B * a.H, splits = qdecode_most_splits(dtype, a.B, a.H, a.T, a.d);
   a.ncounters = qdecode_counters(a.B, a.H, a.d);
   p.off_counters = take(sizeof(int) * a.ncounters);
   p.off_P = take((size_t)elem_bytes(dtype) * BH * a.Tp);
   p.off_ref = take(sizeof(float) * BH * a.NB);
   p.off_sum = take(sizeof(float) * BH * a.NB);
-  p.off_C = take(sizeof(float) * BH * most * a.d);
-  p.off_sref = take(sizeof(float) * BH * most);
-  p.off_ssum = take(sizeof(float) * BH * most);
-  p.off_part = take(a.csw > 1 ? sizeof(float) * (size_t)a.csw * a.B * a.d : 0);
+  p.off_C = take(sizeof(float) * splits * a.H * a.d);
+  p.off_sref = take(sizeof(float) * splits * a.H);
+  p.off_ssum = take(sizeof(float) * splits * a.H);
+  p.off_part = take(sizeof(float) * qdecode_most_row_splits(a.B, a.H, a.d) * a.d);
   p.total = o;
   return p;
 }

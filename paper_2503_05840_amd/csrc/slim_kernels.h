@@ -322,8 +322,11 @@ struct QDecodeArgs {
   int* counters; int ncounters;              // arrivals of the row splits
 };
 int qdecode_counters(int B, int H, int d);
-// blocks of a split, splits, their bound that grows with T, row splits of W and their rows
-void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* most, int* csw, int* crows);
+// blocks of a split, splits, row splits of W and their rows
+void qdecode_cut(int dtype, int B, int H, int T, int d, int* per, int* nsplit, int* csw, int* crows);
+// Sequences x splits, and sequences x row splits of W, at the most: bounds that grow with B and T
+size_t qdecode_most_splits(int dtype, int B, int H, int T, int d);
+size_t qdecode_most_row_splits(int B, int H, int d);
 void launch_qdecode_scores(int dtype, const QDecodeArgs& a, hipStream_t st);
 void launch_qdecode_weighted(int dtype, const QDecodeArgs& a, hipStream_t st);
 void launch_qdecode_project(int dtype, const QDecodeArgs& a, hipStream_t st);

@@ -62,3 +62,13 @@ def prompt_cut(dtype, B, rows_q, rows_k, H, H_kv, d_k):
     i = ctypes.c_int
     c = _rule("_ZN4slim10prompt_cutEiiiiiii", _PromptCut, *[i] * 7)(binding.DTYPES[dtype], B, rows_q, rows_k, H, H_kv, d_k)
     return c.rows, c.parts
+
+
+def quant_cut(dtype, B, H, T, d):
+    """Of the decode step over a cache in 4 or 8 bits: blocks of 64 rows a split, splits, row splits of W and their rows; then the sequences x splits and sequences x row
+    splits that a workspace has place for."""
+    i, p = ctypes.c_int, ctypes.POINTER(ctypes.c_int)
+    out = [i() for _ in range(4)]
+    _rule("_ZN4slim11qdecode_cutEiiiiiPiS0_S0_S0_", None, *[i] * 5, *[p] * 4)(binding.DTYPES[dtype], B, H, T, d, *[ctypes.byref(x) for x in out])
+    return (*[x.value for x in out], _rule("_ZN4slim19qdecode_most_splitsEiiiii", ctypes.c_size_t, *[i] * 5)(binding.DTYPES[dtype], B, H, T, d),
+            _rule("_ZN4slim23qdecode_most_row_splitsEiii", ctypes.c_size_t, *[i] * 3)(B, H, d))
