@@ -168,11 +168,12 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptA
 #pragma unroll
       for (int r = 0; r < 16; ++r) m = fmaxf(m, s[x][r]);
     m = max_of_halves(m) * a.scale;
-    // The reference moves only when a score leaves it 2^8 behind: numerators up to that are as exact, and the sums have room for them.
-    if (__any(m > ref + 8.f)) {
-      const float to = fmaxf(ref, m);
-      const float f = to == NEG_INF ? 1.f : exp2f(ref - to);
-      ref = to;
+    // The reference moves only when a score leaves it 2^8 behind: numerators up to that are as exact, and the sums have room for them.  (Each query's own: a
+    // neighbour's may have moved for a key that this one does not see, which shall not change a bit of its result.)
+    const bool moves = m > ref + 8.f;
+    if (__any(moves)) {
+      const float f = __builtin_amdgcn_exp2f(moves ? ref - m : 0.f);
+      ref = moves ? m : ref;
       sum *= f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)

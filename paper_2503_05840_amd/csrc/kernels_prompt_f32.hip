@@ -157,11 +157,11 @@ __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_f32_kernel(Pro
 #pragma unroll
         for (int r = 0; r < 4; ++r) m = fmaxf(m, s[y][x][r]);
       m = max_of_groups(m) * a.scale;
-      // (the reference moves only when a score leaves it 2^8 behind: numerators up to that are as exact)
-      if (__any(m > ref[y] + 8.f)) {
-        const float to = fmaxf(ref[y], m);
-        const float f = to == NEG_INF ? 1.f : exp2f(ref[y] - to);
-        ref[y] = to;
+      // (the reference moves only when a score leaves it 2^8 behind: numerators up to that are as exact; each query's own, or unseen keys would show in its bits)
+      const bool moves = m > ref[y] + 8.f;
+      if (__any(moves)) {
+        const float f = __builtin_amdgcn_exp2f(moves ? ref[y] - m : 0.f);
+        ref[y] = moves ? m : ref[y];
         sum[y] *= f;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
