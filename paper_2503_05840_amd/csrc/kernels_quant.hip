@@ -41,7 +41,7 @@ __device__ __forceinline__ void place_of(const QuantArgs& a, int r, int& b, long
     b = r / per;
     first = b * per;
   }
-  t = (long)(a.start ? a.start[b] : 0) + (r - first);
+  t = (long)(a.start ? a.start[b] : 0) + ((long)r - first);      // (offsets may be anything: 32 bits could wrap into the cache)
   if (t < 0 || t >= a.T) t = -1;
 }
 
