@@ -27,7 +27,7 @@ template <int PC> __device__ __forceinline__ int v_swap(int row) { return PC >= 
 // 16384 queries x 32 heads x 128, causal: 2.02 ms, 1.09 PFLOP/s, as a library product of 8192^3; heads of 96 and 64 columns have the same numerators for fewer products:
 // 0.70 to 0.88.
 // QW = 2: 64 queries a workgroup, for prompts that do not fill the chip: the waves are two pairs, each with half of every tile's keys, joined at the end.  A sequence's longest
-// workgroup then takes half as long (777 queries x 32 heads 23 -> 19 us).  With 128, four buffers, the next tile's scores beside the numerators, operands read further
+// workgroup then takes half as long (777 queries x 32 heads 22 -> 18 us).  With 128, four buffers, the next tile's scores beside the numerators, operands read further
 // ahead: no gain in any combination, a tile takes 1.1 us of the matrix cores' 0.9.
 template <int DKP, bool WHOLE, int QW>
 __global__ __launch_bounds__(256, DKP <= 128 ? 2 : 1) void prompt_kernel(PromptArgs a) {
@@ -375,9 +375,10 @@ void prompt_by_width(const PromptArgs& a, hipStream_t st) {
 
 // How a call is cut: queries a workgroup and parts of the keys, by what they are expected to take (us).  A workgroup's tiles come one after the other, and a compute
 // unit's workgroups share its matrix cores; parts have to be joined by another launch.  128 queries a tile of 128 columns: 1.13 one after the other, 0.88 of a compute
-// unit's time; 64 queries: 0.77 and 0.53.  (777 queries x 32 heads x 128 23 and 19, 128 behind 5000 keys x 16 heads over 2 40 and 29, 1500 x 20 x 64 33 and 24; where
-// 128 fill the chip, 4000 x 32 x 128, 147 and 166.)  Keys and values that the last-level cache does not keep come a tile of 64 keys in 1.05 us for either, and fewer queries
-// read them more often: 128 then (the last 300 of 8000 and 6854 rows x 24 heads x 96 74 and 85).  Over 147 shapes with all cuts timed this one takes 2 % longer than the best of each;
+// unit's time; 64 queries: 0.77 and 0.53.  (777 queries x 32 heads x 128 22 and 18, 128 behind 5000 keys x 16 heads over 2 40 and 30, each with its best parts, 1500 x 20 x 64
+// without a mask 33 and 23; where 128 fill the chip, 4000 x 32 x 128, 148 and 167.)  Keys and values that the last-level cache does not keep come a tile of 64 keys in 1.05 us for
+// either, and fewer queries read them more often: 128 then (the last 300 of 8000 and 6854 rows x 24 heads x 96 77 and 82).  Over 154 shapes with their cuts timed this one takes
+// 1.8 % longer than the best of each (profiles/prompt_cuts.txt);
 // the fp32 kernel has one form, and its own times.
 PromptCut prompt_cut(int dtype, int B, int rows_q, int rows_k, int H, int H_kv, int d_k) {
   const bool f32 = dtype == DT_F32;
