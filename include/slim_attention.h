@@ -417,8 +417,8 @@ int slim_quant_decode(const void* q, const void* codes, const void* scales, cons
  * H % H_kv == 0; d_k whole 16-byte vectors up to 256.  Offsets are clamped to the rows there are.  Rotary positions are the caller's (opts->rope_table,
  * seq_lens, t_stride and k_layout: SLIM_ERR_ARG).  Scores and sums are fp32; bf16 numerators are rounded where they enter the product with v.  Keys and values that
  * a query does not see have no effect on it, whatever they hold.  The same call gives the same bits.  opts->stage_ms: one figure.
- * Scratch, where keys are shared out over workgroups (few queries over many keys): slim_workspace_bytes_prompt (0 on invalid arguments), a bound that grows with rows_q and
- * rows_k and is the same for every B, up to 275 MB at 128 columns; else library-owned, which grows by what the calls take.  Calls of whole prompts need none. */
+ * Scratch, where keys are shared out over workgroups (too few queries and heads to fill the chip): slim_workspace_bytes_prompt (0 on invalid arguments), a bound that
+ * grows with rows_q and rows_k and is the same for every B, up to 275 MB at 128 columns; else library-owned, which grows by what the calls take. */
 size_t slim_workspace_bytes_prompt(int B, int rows_q, int rows_k, int H, int H_kv, int d_k, int dtype);
 int slim_prompt_attention(const void* q, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_k, void* out, int B, int rows_q,
                           int rows_k, int H, int H_kv, int d_k, int causal, int64_t q_pitch, int64_t k_pitch, int64_t v_pitch, const slim_opts* opts);
